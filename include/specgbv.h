@@ -419,6 +419,116 @@ specgbv_status specgbv_read_sample_intermediates(
     const void *workspace, size_t workspace_bytes, int rows, int V,
     double *u_host, double *margin_host, void *hip_stream);
 
+/*
+ * A decoding step around the verification: keys and values of new tokens are appended to a paged cache, their queries
+ * attend over it, draft tokens are drawn from truncated distributions and the rows handed to the verification are truncated
+ * the same way.  All three calls are asynchronous on hip_stream, allocate nothing and can be captured into a HIP graph.
+ *
+ * The cache.  Token t of sequence s lives in slot t % page_size of page table[s * table_stride + t / page_size]; element
+ * (page, head, slot, i) of k is k[page * k_page_stride + head * k_head_stride + slot * k_token_stride + i], so a page may hold its
+ * heads one after the other or its tokens; the same for v.  Strides are in elements.  Limits: head_dim a multiple of 8 up to 256,
+ * page_size a multiple of 8, k and v 16-byte aligned with strides of whole 16 bytes, at most 2^30 tokens in a sequence
+ * (offsets are 64-bit).  A table entry outside [0, pages) stands for a page that is not there: nothing is stored
+ * to it and no query sees its tokens.
+ */
+typedef struct {
+    void *k, *v;               /* device, bfloat16 or float32 as dtype says                        */
+    const int32_t *table;      /* device, [sequences, table_width], rows table_stride entries apart */
+    int64_t k_page_stride, k_head_stride, k_token_stride;
+    int64_t v_page_stride, v_head_stride, v_token_stride;
+    int64_t table_stride;
+    int32_t pages, kv_heads, page_size, head_dim, sequences, table_width;
+    int32_t dtype;             /* specgbv_dtype of k, v and of every q, k, v, out and weight used with them */
+    int32_t reserved;          /* 0 */
+} specgbv_paged_cache;
+
+/*
+ * specgbv_cache_append: per new token at position pos = positions[s, t], for every head x of q and k
+ *   y = x / sqrt(mean(x^2) + eps) * weight                    (where q_weight / k_weight are given)
+ *   (y_a, y_b) <- (y_a cos f - y_b sin f, y_b cos f + y_a sin f),   f = pos * inv_freq[i], i < pairs,
+ *       with (a, b) = (i, i + pairs), or (2 i, 2 i + 1) where interleaved != 0; the entries behind 2 * pairs stay as they are
+ * q goes to q_out, k and the untouched v to the token's place in the cache.  pos < 0 marks padding: its q_out is 0 and nothing
+ * is stored; nor is it where the position lies behind the table's width.  Angles are formed in float64 and reduced to one turn
+ * before they are rounded, norms and rotations in float32, each result is rounded once.  q_out may be q itself.
+ * No two tokens of a call may have the same place in the cache.
+ */
+typedef struct {
+    const void *q, *k, *v;     /* device, [sequences, tokens, heads or kv_heads, head_dim]; head_dim entries are adjacent */
+    void *q_out;
+    const int32_t *positions;  /* device, [sequences, tokens], rows positions_stride entries apart */
+    const double *inv_freq;    /* device, [pairs]; may be NULL where pairs = 0                      */
+    const void *q_weight, *k_weight;   /* device, [head_dim], or NULL                              */
+    int64_t q_stride[3], k_stride[3], v_stride[3], q_out_stride[3];   /* sequence, token, head; in elements */
+    int64_t positions_stride;
+    double eps;
+    int32_t tokens, heads, pairs, interleaved;
+} specgbv_append_args;
+
+specgbv_status specgbv_cache_append(const specgbv_paged_cache *cache, const specgbv_append_args *args, void *hip_stream);
+
+/*
+ * specgbv_attend_paged: for the query of head h at position pos = positions[s, t], with the keys and values of kv head
+ * h / (heads / kv_heads),
+ *   out = sum_j softmax_j(scale <q, k_j>) v_j   over the tokens j <= pos of sequence s (and j > pos - window where window > 0).
+ * pos < 0 marks padding.  A query that sees no token gets zeros, as does one whose weights are all zero.  Tokens that a query does
+ * not see do not enter its sums, whatever values they hold.  Scores, the running maximum and sum, and the sums of values are float32;
+ * with bfloat16 the weights 2^(x - reference) are rounded to bfloat16 for the matrix product that sums the values.
+ *
+ * Drafts of one prefix.  With prefixes > 0 the sequences are prefixes x drafts, a prefix's drafts next to each other, and
+ * shared_len[b] states how many of its first tokens lie in the same pages for all its drafts (a number of whole pages, say): they
+ * are read once for all drafts, through the first one's table row.  The tokens behind them are read per draft, by one workgroup
+ * per kv head, so shared_len should leave few.
+ *
+ * max_len is how far sequences reach at most, for the choice of the split alone (0: the table's width); the result does not
+ * depend on it beyond rounding.
+ */
+typedef struct {
+    const void *q;             /* device, [sequences, tokens, heads, head_dim], entries of a head adjacent */
+    void *out;                 /* device, the same shape                                                   */
+    const int32_t *positions;  /* device, [sequences, tokens], rows positions_stride entries apart          */
+    const int32_t *shared_len; /* device, [prefixes], or NULL                                              */
+    int64_t q_stride[3], out_stride[3];    /* sequence, token, head; in elements */
+    int64_t positions_stride;
+    int32_t tokens, heads, window, prefixes, max_len;
+    float scale;               /* 0: 1 / sqrt(head_dim) */
+} specgbv_attend_args;
+
+specgbv_status specgbv_attend_paged(const specgbv_paged_cache *cache, const specgbv_attend_args *args,
+                                    void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/* Bytes of device workspace (256-byte aligned, contents of no matter) specgbv_attend_paged needs for these arguments, whose
+ * pointers are not looked at; 0 if they are invalid, or if none is needed. */
+size_t specgbv_attend_workspace_bytes(const specgbv_paged_cache *cache, const specgbv_attend_args *args);
+
+/*
+ * specgbv_sample_filtered: truncated distributions and draws from them, by given uniforms.  The entries of a row that are not
+ * -inf are ordered by logit, the largest first, ties by the lowest index first, and weigh w = exp((z - max z) / temperature).  In
+ * this order
+ *   top_k > 0      keeps the first top_k entries,
+ *   min_p          keeps of these the entries with w >= min_p,
+ *   top_p < 1      keeps of these the entries in front of which less than top_p of their weight lies (never fewer than one);
+ * the token is the first kept entry up to and including which more than u times the kept weight lies (the last kept one where
+ * rounding leaves none).  temperature <= 0 keeps the first entry alone.  A row without entries gets token -1 and keeps nothing;
+ * where a logit is +inf, the entries at +inf weigh 1 and the others nothing.  NaN counts as -inf; min_p above 1 counts as 1.
+ * Weights are float64, or fixed point of 43 fractional bits, in an order that does not change from call to call.
+ *
+ *   logits       device, [rows, V], rows row_stride entries apart
+ *   temperature, top_p, min_p   device, [rows] float32, or NULL (1, 1, 0);   top_k  device, [rows] int32, or NULL (0)
+ *   u            device, [rows] float32 in [0, 1); may be NULL where out_tokens is
+ *   out_tokens   device out, [rows] int32, or NULL;   kept  device out, [rows, V] of the logits' type, rows kept_stride entries
+ *                apart, or NULL: the logits of the kept entries, -inf elsewhere (may be logits itself)
+ *   workspace    device, >= specgbv_filter_workspace_bytes(rows, V, dtype) bytes, 256-byte aligned (NULL where that is 0)
+ *   rows >= 0, 1 <= V <= 1048576
+ */
+specgbv_status specgbv_sample_filtered(
+    const void *logits, int64_t row_stride, int rows, int V, specgbv_dtype dtype,
+    const float *temperature, const int32_t *top_k, const float *top_p, const float *min_p, const float *u,
+    int32_t *out_tokens, void *kept, int64_t kept_stride,
+    void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/* Bytes of device workspace specgbv_sample_filtered needs; 0 if it needs none or the shape is invalid. */
+size_t specgbv_filter_workspace_bytes(int rows, int V, specgbv_dtype dtype);
+
 /* Message of the last failing call made by this thread ("" if none); static storage. */
 const char *specgbv_last_error(void);
 

@@ -10,6 +10,8 @@ from .binding import (ALGO_AUTO, ALGO_CHAIN, ALGO_SPLIT, MAX_PENDING, STATIC_SCR
                       specgbv_read_sample_intermediates, specgbv_sample_tokens, specgbv_sample_workspace_bytes,
                       specgbv_verify, specgbv_verify_ex, specgbv_verify_kseq, specgbv_read_kseq_intermediates, specgbv_verify_static, specgbv_version, specgbv_workspace_bytes,
                       specgbv_workspace_carry)
+from .decoding import (PagedCache, specgbv_attend_paged, specgbv_attend_workspace_bytes, specgbv_cache_append,
+                       specgbv_filter_workspace_bytes, specgbv_sample_filtered)
 
 __all__ = ["ALGO_AUTO", "ALGO_CHAIN", "ALGO_SPLIT", "MAX_PENDING", "STATIC_SCRATCH_BYTES", "SpecGBVError", "pending_state_views", "load_library", "specgbv_carry_advance",
            "specgbv_carry_workspace_bytes", "specgbv_last_error",
@@ -17,4 +19,5 @@ __all__ = ["ALGO_AUTO", "ALGO_CHAIN", "ALGO_SPLIT", "MAX_PENDING", "STATIC_SCRAT
            "specgbv_read_intermediates",
            "specgbv_read_sample_intermediates", "specgbv_sample_tokens", "specgbv_sample_workspace_bytes",
            "specgbv_verify", "specgbv_verify_ex", "specgbv_verify_kseq", "specgbv_read_kseq_intermediates", "specgbv_verify_static", "specgbv_version", "specgbv_workspace_bytes",
-           "specgbv_workspace_carry"]
+           "specgbv_workspace_carry", "PagedCache", "specgbv_cache_append", "specgbv_attend_paged", "specgbv_attend_workspace_bytes", "specgbv_sample_filtered",
+           "specgbv_filter_workspace_bytes"]

@@ -22,7 +22,8 @@ _ALGO = {"auto": ALGO_AUTO, "split": ALGO_SPLIT, "chain": ALGO_CHAIN}
 
 EXPORTS = ("specgbv_workspace_bytes", "specgbv_verify", "specgbv_verify_static", "specgbv_verify_ex", "specgbv_verify_kseq", "specgbv_read_kseq_intermediates", "specgbv_read_intermediates",
            "specgbv_workspace_carry", "specgbv_modify_target", "specgbv_modify_workspace_bytes", "specgbv_sample_tokens", "specgbv_sample_workspace_bytes",
-           "specgbv_read_sample_intermediates", "specgbv_carry_advance", "specgbv_carry_workspace_bytes", "specgbv_pending_state_bytes", "specgbv_last_error", "specgbv_version")
+           "specgbv_read_sample_intermediates", "specgbv_carry_advance", "specgbv_carry_workspace_bytes", "specgbv_pending_state_bytes", "specgbv_cache_append", "specgbv_attend_paged",
+           "specgbv_attend_workspace_bytes", "specgbv_sample_filtered", "specgbv_filter_workspace_bytes", "specgbv_last_error", "specgbv_version")
 
 
 class SpecGBVError(RuntimeError):
@@ -106,6 +107,17 @@ def load_library() -> ctypes.CDLL:
     L.specgbv_carry_advance.restype = c_int
     L.specgbv_carry_workspace_bytes.argtypes = [c_int, c_int]
     L.specgbv_carry_workspace_bytes.restype = c_size_t
+    L.specgbv_cache_append.argtypes = [c_void_p, c_void_p, c_void_p]
+    L.specgbv_cache_append.restype = c_int
+    L.specgbv_attend_paged.argtypes = [c_void_p, c_void_p, c_void_p, c_size_t, c_void_p]
+    L.specgbv_attend_paged.restype = c_int
+    L.specgbv_attend_workspace_bytes.argtypes = [c_void_p, c_void_p]
+    L.specgbv_attend_workspace_bytes.restype = c_size_t
+    L.specgbv_sample_filtered.argtypes = [c_void_p, ctypes.c_int64, c_int, c_int, c_int, c_void_p, c_void_p, c_void_p, c_void_p,
+                                          c_void_p, c_void_p, c_void_p, ctypes.c_int64, c_void_p, c_size_t, c_void_p]
+    L.specgbv_sample_filtered.restype = c_int
+    L.specgbv_filter_workspace_bytes.argtypes = [c_int, c_int, c_int]
+    L.specgbv_filter_workspace_bytes.restype = c_size_t
     L.specgbv_last_error.argtypes = []
     L.specgbv_last_error.restype = c_char_p
     L.specgbv_version.argtypes = []

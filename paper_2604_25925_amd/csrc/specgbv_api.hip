@@ -16,7 +16,7 @@ namespace specgbv {
 
 static thread_local char g_err[512] = "";
 
-static specgbv_status fail(specgbv_status st, const char *fmt, ...)
+specgbv_status fail(specgbv_status st, const char *fmt, ...)
 {
     va_list ap;
     va_start(ap, fmt);

@@ -1,0 +1,648 @@
+// Attention of new queries over a paged cache, split over the cache's length and joined.
+//
+//   out = sum_j w_j v_j / sum_j w_j,   w_j = 2^(c (<q, k_j> - m)),   c = scale log2(e),
+// in one pass over the keys with a running reference m per query (any m gives the same quotient; it is raised, and what has been
+// summed is scaled, only where a weight would exceed 2^8, so that tiles after the first few seldom pay for it).  m is subtracted from
+// the product before c is applied: c <q, k> - c m in one operation would leave the rounding of c m, which is vast where all scores lie
+// near the type's lowest value.
+//
+// Rows.  A kv head's queries of one sequence (tokens x heads of its group), or of all drafts of a prefix while the keys lie in pages
+// that the drafts share, are the rows of a matrix product: one read of a key serves them all.  A wave holds 16 RT rows.
+//
+// A tile is 32 keys (bfloat16; 16 in float32) and never leaves registers.  The product is formed as keys x rows: in the
+// result a lane holds scores of ONE row (lane % 16) and, because the product's row m is made key 8 (m / 4) + 4 h + m % 4 of the tile (h: which
+// half), of 8 ADJACENT keys, those of run lane / 16.  That is the layout in which the second product (values^T x weights) takes its
+// right operand, so the weights go from one product to the next without leaving their lane, and a lane loads the values of its own run
+// of keys: whole rows, each used entry by entry (two 16-bit halves put together by one byte permutation).  The order of entries within the
+// contraction over head_dim is free, so lanes take 16-byte pieces of keys.  Neither the keys nor the values pass through LDS,
+// and no barrier stands in the loop.
+//
+// WK = 4: the waves of a workgroup take the tiles in turn and join at the end through LDS; 1: each wave has rows of its own.
+#include "specgbv_internal.hpp"
+
+namespace specgbv {
+namespace {
+
+typedef float F4 __attribute__((ext_vector_type(4)));
+typedef __bf16 B8 __attribute__((ext_vector_type(8)));
+typedef __bf16 B2 __attribute__((ext_vector_type(2)));
+
+constexpr int kAttendThreads = 256, kWavesPerGroup = 4;
+
+template <typename T, int DP> struct Shape {
+    static constexpr bool kBf = sizeof(T) == 2;
+    static constexpr int kKeys = kBf ? 32 : 16;              // of a tile
+    static constexpr int kRun = kKeys / 4;                   // keys of a lane
+    static constexpr int kHalves = kBf ? 2 : 1;
+    static constexpr int kPiece = 16 / sizeof(T);            // entries of a 16-byte piece
+    static constexpr int kSteps = DP / (4 * kPiece);         // pieces of a key that a lane takes
+    static constexpr int kVec = kBf ? (DP >= 128 ? 8 : 4) : 4;   // adjacent entries of a value that a lane takes
+    static constexpr int kGroups = DP / (16 * kVec);         // such vectors per key
+    static constexpr int kCols = kGroups * kVec;             // result tiles of 16 entries
+    // waves per SIMD that the registers of a tile, its rows and their sums leave room for
+    static constexpr int waves(int RT) { return DP == 256 || (!kBf && DP == 128 && RT == 2) ? 1 : 2; }
+};
+
+__device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }      // (2^-126 and below: 0)
+
+__device__ __forceinline__ int wave_least(int x)
+{
+    for (int m = 32; m > 0; m >>= 1) x = min(x, __shfl_xor(x, m, 64));
+    return __builtin_amdgcn_readfirstlane(x);
+}
+__device__ __forceinline__ int wave_most(int x) { return -wave_least(-x); }
+
+// Largest and sum over the four lanes of a row (l, l ^ 16, l ^ 32, l ^ 48).
+__device__ __forceinline__ float row_largest(float x) { x = fmaxf(x, __shfl_xor(x, 16, 64)); return fmaxf(x, __shfl_xor(x, 32, 64)); }
+__device__ __forceinline__ float row_total(float x) { x += __shfl_xor(x, 16, 64); return x + __shfl_xor(x, 32, 64); }
+
+template <typename T> __device__ __forceinline__ bool not_finite(uint32_t w);      // any entry of a 32-bit word
+template <> __device__ __forceinline__ bool not_finite<float>(uint32_t w) { return (w & 0x7F800000u) == 0x7F800000u; }
+template <> __device__ __forceinline__ bool not_finite<uint16_t>(uint32_t w)
+{
+    return (w & 0x7F800000u) == 0x7F800000u || (w & 0x7F80u) == 0x7F80u;
+}
+
+// One entry's bits against a kind of value that is not finite: 0 not a number, 1 +inf, 2 -inf.
+template <typename T> __device__ __forceinline__ bool is_kind(uint32_t e, int kind)
+{
+    constexpr uint32_t inf = sizeof(T) == 2 ? 0x7F80u : 0x7F800000u, sign = sizeof(T) == 2 ? 0x8000u : 0x80000000u;
+    return kind == 0 ? (e & ~sign) > inf : e == (kind == 1 ? inf : (inf | sign));
+}
+
+template <typename T, int DP, int RT, int WK, bool FINAL>
+__global__ void __launch_bounds__(kAttendThreads, (Shape<T, DP>::waves(RT))) k_attend(AttendProblem p)
+{
+    using S = Shape<T, DP>;
+    constexpr int kKeys = S::kKeys, kRun = S::kRun, kHalves = S::kHalves, kSteps = S::kSteps, kVec = S::kVec, kGroups = S::kGroups,
+                  kCols = S::kCols, kWords = kVec * sizeof(T) / 4;
+    __shared__ F4 sh_acc[WK == 4 ? RT * DP * 16 : 1];         // [4 waves][RT][kGroups][4][kVec / 4][64]
+    __shared__ float sh_m[kWavesPerGroup][RT * 16], sh_l[kWavesPerGroup][RT * 16];
+
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int col = lane & 15, quad = lane >> 4;
+
+    // ---- which rows, which keys.  Row blocks of one item (they read the same keys) are 8 workgroups apart: on one XCD.
+    int item, block;
+    if (p.row_blocks == 1) { item = blockIdx.x; block = 0; }
+    else {
+        const int per = 8 * p.row_blocks, at = blockIdx.x % per;
+        item = blockIdx.x / per * 8 + at % 8; block = at / 8;
+        if (item >= p.items) return;
+    }
+    const int head0 = item % p.kv_heads, rest = item / p.kv_heads;
+    const int chunk = FINAL ? 0 : rest % p.chunks, unit = FINAL ? rest : rest / p.chunks;
+    const int first = unit * (FINAL ? 1 : p.drafts);          // its first sequence
+    const int rows = p.tokens * p.group * (FINAL ? 1 : p.drafts);
+    const int row0 = (block * (WK == 4 ? 1 : 4) + (WK == 4 ? 0 : wave)) * 16 * RT;
+
+    const int64_t held = capacity_of(p.map);
+    int low = 0, high = static_cast<int>(held);               // keys that this kernel looks at
+    int shared = 0;
+    if (p.shared_len) {
+        shared = p.shared_len[FINAL ? unit / p.drafts : unit];
+        shared = max(0, min(shared, high));
+        if (FINAL) low = shared; else high = shared;
+    }
+
+    int64_t q_at[RT], out_at[RT];
+    int row_low[RT], row_high[RT];
+    int part_row[RT];
+    int lo_all = INT32_MAX, lo_most = -1, hi_all = 0, hi_least = INT32_MAX;
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+        const int row = row0 + r * 16 + col;
+        row_low[r] = row_high[r] = 0;
+        q_at[r] = out_at[r] = -1;
+        part_row[r] = -1;
+        if (row < rows) {
+            const int k = row / (p.tokens * p.group), in = row - k * (p.tokens * p.group), t = in / p.group, h = in - t * p.group;
+            const int s = first + k;
+            const int pos = p.positions[s * p.positions_stride + t];
+            const int head = head0 * p.group + h;
+            out_at[r] = s * p.out_stride[0] + t * p.out_stride[1] + head * p.out_stride[2];
+            part_row[r] = FINAL ? (p.shared_len ? (s % p.drafts) * p.tokens * p.group + in : in) : row;
+            if (pos >= 0) {
+                q_at[r] = s * p.q_stride[0] + t * p.q_stride[1] + head * p.q_stride[2];
+                row_low[r] = max(low, p.window > 0 ? pos - (p.window - 1) : 0);
+                row_high[r] = min(high, pos < INT32_MAX ? pos + 1 : pos);
+                if (row_high[r] <= row_low[r]) row_low[r] = row_high[r] = hi_least = 0;       // sees nothing here: no tile is whole
+                else {
+                    lo_all = min(lo_all, row_low[r]); lo_most = max(lo_most, row_low[r]);
+                    hi_all = max(hi_all, row_high[r]); hi_least = min(hi_least, row_high[r]);
+                }
+            }
+        }
+    }
+    lo_all = wave_least(lo_all); hi_least = wave_least(hi_least);
+    lo_most = wave_most(lo_most); hi_all = wave_most(hi_all);
+    int start = lo_all >= hi_all ? 0 : lo_all / kKeys * kKeys, end = lo_all >= hi_all ? 0 : hi_all;
+    if (!FINAL) {
+        // chunks of the planned length, or longer ones where the sequence is longer than was planned for
+        const int span = end - start, least = (span + p.chunks - 1) / p.chunks;
+        const int length = max(p.chunk_keys, (least + kKeys - 1) / kKeys * kKeys);
+        const int64_t at = start + static_cast<int64_t>(chunk) * length;
+        start = static_cast<int>(min(at, static_cast<int64_t>(end)));
+        end = static_cast<int>(min(at + length, static_cast<int64_t>(end)));
+    }
+
+    // ---- queries
+    U4 qf[RT][kSteps];
+    const T *q = static_cast<const T *>(p.q);
+#pragma unroll
+    for (int r = 0; r < RT; ++r)
+#pragma unroll
+        for (int i = 0; i < kSteps; ++i) {
+            const int at = (4 * i + quad) * S::kPiece;
+            U4 v{0, 0, 0, 0};
+            if (q_at[r] >= 0 && at < p.head_dim) {
+                if (p.q_wide) v = *reinterpret_cast<const U4 *>(q + q_at[r] + at);
+                else {
+                    T e[S::kPiece];
+#pragma unroll
+                    for (int j = 0; j < S::kPiece; ++j) e[j] = q[q_at[r] + at + j];
+                    __builtin_memcpy(&v, e, 16);
+                }
+            }
+            qf[r][i] = v;
+        }
+
+    F4 acc[RT][kCols];
+    float ref[RT], sum[RT];                                   // sum: over the lane's own keys
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+        ref[r] = -INFINITY; sum[r] = 0.0f;
+#pragma unroll
+        for (int c = 0; c < kCols; ++c) acc[r][c] = F4{0, 0, 0, 0};
+    }
+
+    // ---- the keys
+    const int step = (WK == 4 ? 4 : 1) * kKeys;
+    int tile = start + (WK == 4 ? wave * kKeys : 0);
+    const T *kb = static_cast<const T *>(p.k) + head0 * static_cast<int64_t>(p.k_head_stride);
+    const T *vb = static_cast<const T *>(p.v) + head0 * static_cast<int64_t>(p.v_head_stride);
+    const int run_k = col >> 2, in_run = col & 3;
+
+    // The place of a run of keys: page_size is a multiple of a run, and so is where a tile starts.  Runs behind the last key take
+    // the last one's place, so that nothing is read outside pages that hold keys; their scores are masked.
+    auto run_place = [&](int t, int run) {
+        const int key = min(t + run * kRun, (end - 1) / kRun * kRun);
+        return place_of(p.map, first, key);
+    };
+    U4 kf[kHalves][kSteps];
+    uint32_t vf[kRun][kGroups][kWords];
+    auto load_keys = [&](Place at) {
+#pragma unroll
+        for (int h = 0; h < kHalves; ++h) {
+            const T *src = kb + max(at.page, 0) * static_cast<int64_t>(p.k_page_stride) +
+                           (at.slot + 4 * h + in_run) * static_cast<int64_t>(p.k_token_stride);
+#pragma unroll
+            for (int i = 0; i < kSteps; ++i) {
+                const int e = (4 * i + quad) * S::kPiece;
+                if (4 * i * S::kPiece >= p.head_dim) continue;                       // uniform
+                kf[h][i] = *reinterpret_cast<const U4 *>(src + (e < p.head_dim ? e : 0));
+            }
+        }
+    };
+    auto load_values = [&](Place at) {
+        const T *src = vb + max(at.page, 0) * static_cast<int64_t>(p.v_page_stride) + at.slot * static_cast<int64_t>(p.v_token_stride);
+#pragma unroll
+        for (int k = 0; k < kRun; ++k)
+#pragma unroll
+            for (int g = 0; g < kGroups; ++g) {
+                const int e = (g * 16 + col) * kVec;
+                struct alignas(4 * kWords) Words { uint32_t w[kWords]; };
+                const Words v = *reinterpret_cast<const Words *>(src + k * static_cast<int64_t>(p.v_token_stride) + (e < p.head_dim ? e : 0));
+#pragma unroll
+                for (int w = 0; w < kWords; ++w) vf[k][g][w] = v.w[w];
+            }
+    };
+
+    Place next_k{-1, 0}, next_v{-1, 0}, here_v{-1, 0};
+    if (tile < end) {
+        const Place a = run_place(tile, run_k);
+        here_v = run_place(tile, quad);
+        load_keys(a);
+        load_values(here_v);
+        if (tile + step < end) { next_k = run_place(tile + step, run_k); next_v = run_place(tile + step, quad); }
+    }
+    for (; tile < end; tile += step) {
+        // scores: keys x rows
+        F4 s[RT][kHalves];
+#pragma unroll
+        for (int r = 0; r < RT; ++r)
+#pragma unroll
+            for (int h = 0; h < kHalves; ++h) s[r][h] = F4{0, 0, 0, 0};
+        if (p.head_dim != DP) {
+#pragma unroll
+            for (int i = 0; i < kSteps; ++i)
+                if ((4 * i + quad) * S::kPiece >= p.head_dim)
+#pragma unroll
+                    for (int h = 0; h < kHalves; ++h) kf[h][i] = U4{0, 0, 0, 0};
+        }
+#pragma unroll
+        for (int i = 0; i < kSteps; ++i)
+#pragma unroll
+            for (int h = 0; h < kHalves; ++h)
+#pragma unroll
+                for (int r = 0; r < RT; ++r) {
+                    if constexpr (S::kBf)
+                        s[r][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(B8, kf[h][i]), __builtin_bit_cast(B8, qf[r][i]), s[r][h], 0, 0, 0);
+                    else {
+                        const F4 a = __builtin_bit_cast(F4, kf[h][i]), b = __builtin_bit_cast(F4, qf[r][i]);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) s[r][h] = __builtin_amdgcn_mfma_f32_16x16x4f32(a[e], b[e], s[r][h], 0, 0, 0);
+                    }
+                }
+        const Place cur_v = here_v;
+        const bool more = tile + step < end;
+        if (more) {
+            load_keys(next_k);
+            here_v = next_v;
+            if (tile + 2 * step < end) { next_k = run_place(tile + 2 * step, run_k); next_v = run_place(tile + 2 * step, quad); }
+        }
+
+        // weights
+        const bool lost = cur_v.page < 0;
+        const bool partial = tile < lo_most || tile + kKeys > hi_least || tile + kKeys > end || __any(lost);
+        uint32_t seen[RT];                                    // bits: which of the lane's keys its row sees
+#pragma unroll
+        for (int r = 0; r < RT; ++r) {
+            seen[r] = (1u << kRun) - 1;
+            if (partial) {
+                const int base = tile + quad * kRun;
+                seen[r] = 0;
+#pragma unroll
+                for (int k = 0; k < kRun; ++k)
+                    if (!lost && base + k >= row_low[r] && base + k < row_high[r]) seen[r] |= 1u << k;
+#pragma unroll
+                for (int k = 0; k < kRun; ++k)
+                    if (!(seen[r] >> k & 1)) s[r][k / 4][k % 4] = -INFINITY;
+            }
+            float top = s[r][0][0];
+#pragma unroll
+            for (int k = 1; k < kRun; ++k) top = fmaxf(top, s[r][k / 4][k % 4]);
+            if (__any(top > ref[r] + p.raise)) {
+                // (row by row: what a row gets does not hang on the rows next to it)
+                top = row_largest(top);
+                const float now = top > ref[r] + p.raise ? top : ref[r];
+                const float f = now == ref[r] ? 1.0f : exp2_of((ref[r] - now) * p.c);        // (-inf to -inf: nothing summed yet)
+                ref[r] = now;
+                sum[r] *= f;
+#pragma unroll
+                for (int c = 0; c < kCols; ++c) acc[r][c] *= f;
+            }
+            const float m = ref[r] == -INFINITY ? 0.0f : ref[r];
+#pragma unroll
+            for (int k = 0; k < kRun; ++k) {
+                const float w = exp2_of((s[r][k / 4][k % 4] - m) * p.c);
+                s[r][k / 4][k % 4] = w;
+                sum[r] += w;
+            }
+        }
+
+        // values that some rows do not see: a weight of 0 does not take out what is not finite.  Keys that no row sees are cleared;
+        // where another value is not finite, it is taken out and put back by products of marks alone, for the rows that see it.
+        bool odd = false;
+        if (partial) {
+            const int base = tile + quad * kRun;
+#pragma unroll
+            for (int k = 0; k < kRun; ++k)
+                if (lost || base + k < lo_all || base + k >= hi_all)
+#pragma unroll
+                    for (int g = 0; g < kGroups; ++g)
+#pragma unroll
+                        for (int w = 0; w < kWords; ++w) vf[k][g][w] = 0;
+#pragma unroll
+            for (int k = 0; k < kRun; ++k)
+#pragma unroll
+                for (int g = 0; g < kGroups; ++g)
+#pragma unroll
+                    for (int w = 0; w < kWords; ++w) odd = odd || not_finite<T>(vf[k][g][w]);
+            odd = __any(odd);
+        }
+        if (odd) {
+#pragma unroll 1
+            for (int kind = 0; kind < 3; ++kind) {
+                const float what = kind == 0 ? NAN : (kind == 1 ? INFINITY : -INFINITY);
+#pragma unroll
+                for (int g = 0; g < kGroups; ++g)
+#pragma unroll
+                    for (int j = 0; j < kVec; ++j) {
+                        uint32_t e[kRun];
+#pragma unroll
+                        for (int k = 0; k < kRun; ++k)
+                            e[k] = S::kBf ? (vf[k][g][j * sizeof(T) / 4] >> (j % 2 * 16)) & 0xFFFFu : vf[k][g][j * sizeof(T) / 4];
+#pragma unroll
+                        for (int r = 0; r < RT; ++r) {
+                            F4 n{0, 0, 0, 0};
+                            if constexpr (S::kBf) {
+                                B8 a, b;
+#pragma unroll
+                                for (int k = 0; k < kRun; ++k) {
+                                    a[k] = static_cast<__bf16>(is_kind<T>(e[k], kind) ? 1.0f : 0.0f);
+                                    b[k] = static_cast<__bf16>(seen[r] >> k & 1 ? 1.0f : 0.0f);
+                                }
+                                n = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, n, 0, 0, 0);
+                            } else {
+#pragma unroll
+                                for (int k = 0; k < kRun; ++k)
+                                    n = __builtin_amdgcn_mfma_f32_16x16x4f32(is_kind<T>(e[k], kind) ? 1.0f : 0.0f, seen[r] >> k & 1 ? 1.0f : 0.0f, n, 0, 0, 0);
+                            }
+#pragma unroll
+                            for (int i = 0; i < 4; ++i)
+                                if (n[i] > 0.0f) acc[r][g * kVec + j][i] += what;
+                        }
+                    }
+            }
+#pragma unroll
+            for (int k = 0; k < kRun; ++k)
+#pragma unroll
+                for (int g = 0; g < kGroups; ++g)
+#pragma unroll
+                    for (int w = 0; w < kWords; ++w) {
+                        uint32_t &x = vf[k][g][w];
+                        if (S::kBf) {
+                            if ((x & 0x7F80u) == 0x7F80u) x &= 0xFFFF0000u;
+                            if ((x & 0x7F800000u) == 0x7F800000u) x &= 0x0000FFFFu;
+                        } else if ((x & 0x7F800000u) == 0x7F800000u) x = 0;
+                    }
+        }
+
+        // sums of values: entries x rows
+        if constexpr (S::kBf) {
+            B8 w[RT];
+#pragma unroll
+            for (int r = 0; r < RT; ++r)
+#pragma unroll
+                for (int k = 0; k < kRun; ++k) w[r][k] = static_cast<__bf16>(s[r][k / 4][k % 4]);
+#pragma unroll
+            for (int g = 0; g < kGroups; ++g)
+#pragma unroll
+                for (int j = 0; j < kVec; ++j) {
+                    U4 a;
+                    uint32_t *aw = &a.x;
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        aw[k] = __builtin_amdgcn_perm(vf[2 * k + 1][g][j / 2], vf[2 * k][g][j / 2], j % 2 ? 0x07060302u : 0x05040100u);
+#pragma unroll
+                    for (int r = 0; r < RT; ++r)
+                        acc[r][g * kVec + j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(B8, a), w[r], acc[r][g * kVec + j], 0, 0, 0);
+                }
+        } else {
+#pragma unroll
+            for (int g = 0; g < kGroups; ++g)
+#pragma unroll
+                for (int j = 0; j < kVec; ++j)
+#pragma unroll
+                    for (int r = 0; r < RT; ++r)
+#pragma unroll
+                        for (int k = 0; k < kRun; ++k)
+                            acc[r][g * kVec + j] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(vf[k][g][j]), s[r][0][k], acc[r][g * kVec + j], 0, 0, 0);
+        }
+        if (more) load_values(here_v);
+    }
+#pragma unroll
+    for (int r = 0; r < RT; ++r) sum[r] = row_total(sum[r]);
+
+    // ---- sums of the chunks in front (the shared keys of a prefix).  Partial sums are held in the order in which lanes hold them:
+    // vector ((g 4 + i) kVec / 4 + n) 4 + quad of a row are entries (16 g + 4 quad + i) kVec + 4 n + 0..3.
+    if (FINAL && p.chunks > 0) {
+        const int64_t part0 = (static_cast<int64_t>(unit / p.drafts) * p.kv_heads + head0) * p.chunks;
+        const int rows_a = p.tokens * p.group * p.drafts;
+        for (int c = WK == 4 ? wave : 0; c < p.chunks; c += WK == 4 ? 4 : 1) {
+#pragma unroll
+            for (int r = 0; r < RT; ++r) {
+                if (part_row[r] < 0) continue;
+                const int64_t at = (part0 + c) * rows_a + part_row[r];
+                const float2 ml = p.ml[at];
+                if (!(ml.y != 0.0f)) continue;                                       // nothing summed (a sum that is no number goes on)
+                const float now = fmaxf(ref[r], ml.x);
+                const float f = now == ref[r] ? 1.0f : exp2_of((ref[r] - now) * p.c), g1 = now == ml.x ? 1.0f : exp2_of((ml.x - now) * p.c);
+                ref[r] = now;
+                sum[r] = sum[r] * f + ml.y * g1;
+                const F4 *part = reinterpret_cast<const F4 *>(p.acc + at * DP);
+#pragma unroll
+                for (int g = 0; g < kGroups; ++g)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+#pragma unroll
+                        for (int n = 0; n < kVec / 4; ++n) {
+                            const F4 v = part[((g * 4 + i) * (kVec / 4) + n) * 4 + quad];
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) {
+                                acc[r][g * kVec + 4 * n + e][i] = acc[r][g * kVec + 4 * n + e][i] * f + v[e] * g1;
+                            }
+                        }
+            }
+        }
+    }
+
+    // ---- the waves of a workgroup join: each brings its sums to the largest reference, then wave i adds up the entries i of all
+    if (WK == 4) {
+        if (quad == 0)
+#pragma unroll
+            for (int r = 0; r < RT; ++r) { sh_m[wave][r * 16 + col] = ref[r]; sh_l[wave][r * 16 + col] = sum[r]; }
+        __syncthreads();
+#pragma unroll
+        for (int r = 0; r < RT; ++r) {
+            float most = -INFINITY, total = 0.0f;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) most = fmaxf(most, sh_m[w][r * 16 + col]);
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                const float m = sh_m[w][r * 16 + col];
+                total += sh_l[w][r * 16 + col] * (m == most ? 1.0f : exp2_of((m - most) * p.c));
+            }
+            const float f = ref[r] == most ? 1.0f : exp2_of((ref[r] - most) * p.c);
+            ref[r] = most; sum[r] = total;
+#pragma unroll
+            for (int g = 0; g < kGroups; ++g)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int n = 0; n < kVec / 4; ++n) {
+                        F4 v;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) v[e] = acc[r][g * kVec + 4 * n + e][i] * f;
+                        sh_acc[((((wave * RT + r) * kGroups + g) * 4 + i) * (kVec / 4) + n) * 64 + lane] = v;
+                    }
+        }
+        __syncthreads();
+    }
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+        if (row0 + r * 16 + col >= rows) continue;
+        const float inv = sum[r] != 0.0f ? 1.0f / sum[r] : 0.0f;
+        const int64_t part = FINAL ? 0 : ((static_cast<int64_t>(unit) * p.kv_heads + head0) * p.chunks + chunk) * rows + part_row[r];
+        if (!FINAL && (WK == 1 || wave == 0) && quad == 0) p.ml[part] = make_float2(ref[r], sum[r]);
+#pragma unroll
+        for (int g = 0; g < kGroups; ++g)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (WK == 4 && i != wave) continue;
+                float x[kVec];
+#pragma unroll
+                for (int n = 0; n < kVec / 4; ++n) {
+                    F4 v{0, 0, 0, 0};
+                    if (WK == 4) {
+#pragma unroll
+                        for (int w = 0; w < 4; ++w) v += sh_acc[((((w * RT + r) * kGroups + g) * 4 + i) * (kVec / 4) + n) * 64 + lane];
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) v[e] = acc[r][g * kVec + 4 * n + e][i];
+                    }
+                    if (!FINAL) reinterpret_cast<F4 *>(p.acc + part * DP)[((g * 4 + i) * (kVec / 4) + n) * 4 + quad] = v;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) x[4 * n + e] = v[e];
+                }
+                const int d = (16 * g + 4 * quad + i) * kVec;
+                if (FINAL && d < p.head_dim) {
+                    T *dst = static_cast<T *>(p.out) + out_at[r] + d;
+                    struct alignas(kVec * sizeof(T)) Vec { T e[kVec]; } o;
+#pragma unroll
+                    for (int j = 0; j < kVec; ++j) {
+                        const float y = q_at[r] < 0 || sum[r] == 0.0f ? 0.0f : x[j] * inv;
+                        if constexpr (S::kBf) o.e[j] = __builtin_bit_cast(uint16_t, static_cast<__bf16>(y));
+                        else o.e[j] = y;
+                    }
+                    if (p.out_wide) *reinterpret_cast<Vec *>(dst) = o;
+                    else
+#pragma unroll
+                        for (int j = 0; j < kVec; ++j) dst[j] = o.e[j];
+                }
+            }
+    }
+}
+
+// Sums of chunks joined, one wave per row: DP / 4 lanes take a chunk's vectors, the others the next chunks'.
+template <typename T, int DP>
+__global__ void __launch_bounds__(kAttendThreads) k_attend_join(AttendProblem p)
+{
+    constexpr int kVec = Shape<T, DP>::kVec, kLanes = DP / 4, kSets = 64 / kLanes;
+    const int lane = threadIdx.x & 63, vec = lane % kLanes, set = lane / kLanes;
+    const int rows = p.tokens * p.group;
+    const int64_t all = static_cast<int64_t>(p.sequences) * p.kv_heads * rows;
+    const int64_t at = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);
+    if (at >= all) return;
+    const int row = static_cast<int>(at % rows);
+    const int64_t pair = at / rows;
+    const int head0 = static_cast<int>(pair % p.kv_heads), s = static_cast<int>(pair / p.kv_heads);
+    const int64_t part0 = pair * p.chunks * rows + row;
+
+    float most = -INFINITY;
+    for (int c = lane; c < p.chunks; c += 64) {
+        const float2 ml = p.ml[part0 + static_cast<int64_t>(c) * rows];
+        if (ml.y != 0.0f) most = fmaxf(most, ml.x);
+    }
+    for (int m = 32; m > 0; m >>= 1) most = fmaxf(most, __shfl_xor(most, m, 64));
+    float total = 0.0f;
+    F4 acc{0, 0, 0, 0};
+#pragma unroll 4
+    for (int c = set; c < p.chunks; c += kSets) {
+        const float2 ml = p.ml[part0 + static_cast<int64_t>(c) * rows];
+        const F4 v = reinterpret_cast<const F4 *>(p.acc + (part0 + static_cast<int64_t>(c) * rows) * DP)[vec];
+        const float f = !(ml.y != 0.0f) ? 0.0f : (ml.x == most ? 1.0f : exp2_of((ml.x - most) * p.c));
+        total += ml.y * f;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[e] += f == 0.0f && ml.y == ml.y ? 0.0f : v[e] * f;
+    }
+#pragma unroll
+    for (int m = 32; m >= kLanes; m >>= 1) {
+        total += __shfl_xor(total, m, 64);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[e] += __shfl_xor(acc[e], m, 64);
+    }
+    if (set != 0) return;
+    const int quad = vec & 3, piece = vec >> 2, n = piece % (kVec / 4), gi = piece / (kVec / 4), i = gi & 3, g = gi >> 2;
+    const int d = (16 * g + 4 * quad + i) * kVec + 4 * n;
+    if (d >= p.head_dim) return;
+    const int t = row / p.group, h = head0 * p.group + row % p.group;
+    T *dst = static_cast<T *>(p.out) + s * p.out_stride[0] + t * p.out_stride[1] + h * p.out_stride[2] + d;
+    const bool some = p.positions[s * p.positions_stride + t] >= 0 && total != 0.0f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const float y = some ? acc[e] / total : 0.0f;
+        if constexpr (sizeof(T) == 2) dst[e] = __builtin_bit_cast(uint16_t, static_cast<__bf16>(y));
+        else dst[e] = y;
+    }
+}
+
+template <typename T, int DP, int RT, int WK, bool FINAL>
+hipError_t launch_one(AttendProblem p, int units, hipStream_t stream)
+{
+    const int rows = p.tokens * p.group * (FINAL ? 1 : p.drafts), per = 16 * RT * (WK == 4 ? 1 : 4);
+    p.row_blocks = (rows + per - 1) / per;
+    p.items = units * p.kv_heads * (FINAL ? 1 : p.chunks);
+    const int64_t grid = p.row_blocks == 1 ? p.items : static_cast<int64_t>((p.items + 7) / 8 * 8) * p.row_blocks;
+    if (grid > INT32_MAX) return hipErrorInvalidConfiguration;
+    hipLaunchKernelGGL((k_attend<T, DP, RT, WK, FINAL>), dim3(static_cast<unsigned>(grid)), dim3(kAttendThreads), 0, stream, p);
+    return hipGetLastError();
+}
+
+template <typename T, int DP, bool FINAL>
+hipError_t launch_rows(const AttendProblem &p, int units, hipStream_t stream)
+{
+    const int rows = p.tokens * p.group * (FINAL ? 1 : p.drafts);
+    if (rows <= 16) return launch_one<T, DP, 1, 4, FINAL>(p, units, stream);
+    if constexpr (DP < 256) {
+        if (rows <= 64) return launch_one<T, DP, 2, 4, FINAL>(p, units, stream);
+        return launch_one<T, DP, 2, 1, FINAL>(p, units, stream);
+    } else {
+        if (rows <= 32) return launch_one<T, DP, 1, 4, FINAL>(p, units, stream);
+        return launch_one<T, DP, 1, 1, FINAL>(p, units, stream);
+    }
+}
+
+template <typename T, int DP>
+hipError_t launch_typed(const AttendProblem &p, hipStream_t stream)
+{
+    if (p.chunks == 0) return launch_rows<T, DP, true>(p, p.sequences, stream);
+    hipError_t e = launch_rows<T, DP, false>(p, p.sequences / p.drafts, stream);
+    if (e != hipSuccess) return e;
+    if (p.shared_len) return launch_rows<T, DP, true>(p, p.sequences, stream);
+    const int64_t rows = static_cast<int64_t>(p.sequences) * p.heads * p.tokens;
+    hipLaunchKernelGGL((k_attend_join<T, DP>), dim3(static_cast<unsigned>((rows + 3) / 4)), dim3(kAttendThreads), 0, stream, p);
+    return hipGetLastError();
+}
+
+template <typename T>
+hipError_t launch_dim(const AttendProblem &p, hipStream_t stream)
+{
+    if (p.head_dim <= 64) return launch_typed<T, 64>(p, stream);
+    if (p.head_dim <= 128) return launch_typed<T, 128>(p, stream);
+    return launch_typed<T, 256>(p, stream);
+}
+
+}  // namespace
+
+AttendPlan plan_attend(int sequences, int drafts, bool shared, int tokens, int heads, int kv_heads, int head_dim, int window,
+                       int64_t longest)
+{
+    AttendPlan a{};
+    const int dp = head_dim <= 64 ? 64 : (head_dim <= 128 ? 128 : 256);
+    const int rows = tokens * (heads / kv_heads) * drafts;
+    if (window > 0) longest = longest < static_cast<int64_t>(window) + tokens ? longest : static_cast<int64_t>(window) + tokens;
+    const int per = rows <= 64 ? 32 : 128;
+    const int64_t base = static_cast<int64_t>(sequences / drafts) * kv_heads * ((rows + per - 1) / per);
+    const int least = 256;                                     // keys of a chunk
+    int64_t chunks = (4 * compute_units() + base - 1) / (base < 1 ? 1 : base);
+    const int64_t most = (longest + least - 1) / least;
+    if (chunks > most) chunks = most;
+    if (chunks > 256) chunks = 256;
+    if (chunks < 1) chunks = 1;
+    if (chunks == 1 && !shared) return a;                      // one pass, nothing to join
+    a.chunks = static_cast<int>(chunks);
+    a.chunk_keys = static_cast<int>(((longest + chunks - 1) / chunks + 127) / 128 * 128);
+    const size_t parts = static_cast<size_t>(sequences / drafts) * kv_heads * a.chunks * rows;
+    a.ml_bytes = (parts * sizeof(float2) + 255) / 256 * 256;
+    a.bytes = a.ml_bytes + (parts * dp * sizeof(float) + 255) / 256 * 256;
+    return a;
+}
+
+hipError_t launch_attend(const AttendProblem &p, int dtype, hipStream_t stream)
+{
+    return dtype == 1 ? launch_dim<uint16_t>(p, stream) : launch_dim<float>(p, stream);
+}
+
+}  // namespace specgbv

@@ -5,7 +5,9 @@
 #include <stddef.h>
 #include <stdint.h>
 
+#include "../../include/specgbv.h"
 #include "specgbv_device.hpp"
+#include "specgbv_paged.hpp"
 
 namespace specgbv {
 
@@ -141,5 +143,61 @@ hipError_t launch_carry_advance(const void *rows_q, const void *rows_p, const in
                                 const int32_t *accepted_idx, const int32_t *out_tokens, int K, int M, int bonus, int V,
                                 int batch, int dtype, float c, double *carry, int32_t *count, double *delta,
                                 hipStream_t stream);
+
+// The message of this thread's last failing call; returns `st`.
+specgbv_status fail(specgbv_status st, const char *fmt, ...);
+
+// Appending to a paged cache (see specgbv_append_args); strides in elements, of the caches: page, head, slot.
+struct AppendProblem {
+    const void *q, *k, *v;
+    void *q_out, *k_cache, *v_cache;
+    const void *q_weight, *k_weight;
+    const int32_t *positions;
+    const double *inv_freq;
+    PageMap map;
+    Divider by_tokens, by_heads;   // tokens of a sequence; heads of q, k and v together
+    int64_t q_stride[3], k_stride[3], v_stride[3], q_out_stride[3], k_cache_stride[3], v_cache_stride[3];
+    int64_t positions_stride;
+    float eps, inv_dim;
+    int tokens_all, heads, kv_heads, head_dim, pairs, interleaved;
+    int lane_bits, block_tokens;   // set by launch_append
+};
+// width: entries of a vector, a power of two of at most 16 bytes that divides pairs and, twice, head_dim, and that every
+// stride and address allows.
+hipError_t launch_append(const AppendProblem &p, int dtype, int width, hipStream_t stream);
+
+// Attention over a paged cache (see specgbv_attend_args); strides in elements.
+struct AttendProblem {
+    const void *q, *k, *v;
+    void *out;
+    const int32_t *positions, *shared_len;
+    PageMap map;
+    int64_t q_stride[3], out_stride[3], positions_stride;
+    int32_t k_page_stride, k_head_stride, k_token_stride, v_page_stride, v_head_stride, v_token_stride;
+    float2 *ml;                    // [units][kv_heads][chunks][rows] reference and sum of a chunk; unit: sequence, or prefix with its drafts
+    float *acc;                    // the same, with the sums of values
+    float c;                       // scale * log2(e)
+    float raise;                   // a reference is raised where a score exceeds it by this: weights stay below 2^8
+    int sequences, tokens, heads, kv_heads, group, head_dim, drafts, window;
+    int chunks, chunk_keys;        // 0 chunks: one pass without partial sums
+    int q_wide, out_wide;          // 16-byte loads of q, stores of whole vectors to out
+    int items, row_blocks;         // set by the launches
+};
+struct AttendPlan { int chunks, chunk_keys; size_t ml_bytes, bytes; };
+AttendPlan plan_attend(int sequences, int drafts, bool shared, int tokens, int heads, int kv_heads, int head_dim, int window,
+                       int64_t longest);
+hipError_t launch_attend(const AttendProblem &p, int dtype, hipStream_t stream);
+
+// Truncated distributions and draws from them (see specgbv_sample_filtered).
+struct FilterProblem {
+    const void *logits;
+    void *kept;
+    int64_t row_stride, kept_stride;
+    const float *temperature, *top_p, *min_p, *u;
+    const int32_t *top_k;
+    int32_t *out_tokens;
+    int rows, V;
+};
+hipError_t launch_filter(const FilterProblem &p, int dtype, hipStream_t stream);
 
 }  // namespace specgbv
