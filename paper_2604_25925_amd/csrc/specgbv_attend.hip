@@ -43,6 +43,12 @@ template <typename T, int DP> struct Shape {
     static constexpr int waves(int RT) { return DP == 256 || (!kBf && DP == 128 && RT == 2) ? 1 : 2; }
 };
 
+constexpr int kMaxParts = 256;                // partial sums of a row at most: a workgroup's threads
+
+template <typename T> __device__ __forceinline__ T rounded(float x);
+template <> __device__ __forceinline__ float rounded<float>(float x) { return x; }
+template <> __device__ __forceinline__ uint16_t rounded<uint16_t>(float x) { return __builtin_bit_cast(uint16_t, static_cast<__bf16>(x)); }
+
 __device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }      // (2^-126 and below: 0)
 
 __device__ __forceinline__ int wave_least(int x)
@@ -70,7 +76,7 @@ template <typename T> __device__ __forceinline__ bool is_kind(uint32_t e, int ki
     return kind == 0 ? (e & ~sign) > inf : e == (kind == 1 ? inf : (inf | sign));
 }
 
-template <typename T, int DP, int RT, int WK, bool FINAL>
+template <typename T, int DP, int RT, int WK, bool PARTS>
 __global__ void __launch_bounds__(kAttendThreads, (Shape<T, DP>::waves(RT))) k_attend(AttendProblem p)
 {
     using S = Shape<T, DP>;
@@ -91,81 +97,65 @@ __global__ void __launch_bounds__(kAttendThreads, (Shape<T, DP>::waves(RT))) k_a
         if (item >= p.items) return;
     }
     const int head0 = item % p.kv_heads, rest = item / p.kv_heads;
-    const int chunk = FINAL ? 0 : rest % p.chunks, unit = FINAL ? rest : rest / p.chunks;
-    const int first = unit * (FINAL ? 1 : p.drafts);          // its first sequence
-    const int rows = p.tokens * p.group * (FINAL ? 1 : p.drafts);
+    const int part = PARTS ? rest % p.parts : 0, unit = PARTS ? rest / p.parts : rest;
+    const bool own = PARTS && p.shared_len && part == p.chunks;       // the drafts' own keys, behind the shared ones
+    const int first = unit * p.drafts;                        // its first sequence
+    const int in_draft = p.tokens * p.group, rows = in_draft * p.drafts;
     const int row0 = (block * (WK == 4 ? 1 : 4) + (WK == 4 ? 0 : wave)) * 16 * RT;
 
-    const int64_t held = capacity_of(p.map);
-    int low = 0, high = static_cast<int>(held);               // keys that this kernel looks at
-    int shared = 0;
-    if (p.shared_len) {
-        shared = p.shared_len[FINAL ? unit / p.drafts : unit];
-        shared = max(0, min(shared, high));
-        if (FINAL) low = shared; else high = shared;
-    }
+    const int held = static_cast<int>(capacity_of(p.map));
+    const int shared = p.shared_len ? max(0, min(p.shared_len[unit], held)) : held;
 
+    // Rows behind the last one take its place (their loads are those of the last row) and are nowhere stored.
     int64_t q_at[RT], out_at[RT];
-    int row_low[RT], row_high[RT];
-    int part_row[RT];
-    int lo_all = INT32_MAX, lo_most = -1, hi_all = 0, hi_least = INT32_MAX;
+    int pos[RT], draft[RT];
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
-        const int row = row0 + r * 16 + col;
-        row_low[r] = row_high[r] = 0;
-        q_at[r] = out_at[r] = -1;
-        part_row[r] = -1;
-        if (row < rows) {
-            const int k = row / (p.tokens * p.group), in = row - k * (p.tokens * p.group), t = in / p.group, h = in - t * p.group;
-            const int s = first + k;
-            const int pos = p.positions[s * p.positions_stride + t];
-            const int head = head0 * p.group + h;
-            out_at[r] = s * p.out_stride[0] + t * p.out_stride[1] + head * p.out_stride[2];
-            part_row[r] = FINAL ? (p.shared_len ? (s % p.drafts) * p.tokens * p.group + in : in) : row;
-            if (pos >= 0) {
-                q_at[r] = s * p.q_stride[0] + t * p.q_stride[1] + head * p.q_stride[2];
-                row_low[r] = max(low, p.window > 0 ? pos - (p.window - 1) : 0);
-                row_high[r] = min(high, pos < INT32_MAX ? pos + 1 : pos);
-                if (row_high[r] <= row_low[r]) row_low[r] = row_high[r] = hi_least = 0;       // sees nothing here: no tile is whole
-                else {
-                    lo_all = min(lo_all, row_low[r]); lo_most = max(lo_most, row_low[r]);
-                    hi_all = max(hi_all, row_high[r]); hi_least = min(hi_least, row_high[r]);
-                }
-            }
-        }
-    }
-    lo_all = wave_least(lo_all); hi_least = wave_least(hi_least);
-    lo_most = wave_most(lo_most); hi_all = wave_most(hi_all);
-    int start = lo_all >= hi_all ? 0 : lo_all / kKeys * kKeys, end = lo_all >= hi_all ? 0 : hi_all;
-    if (!FINAL) {
-        // chunks of the planned length, or longer ones where the sequence is longer than was planned for
-        const int span = end - start, least = (span + p.chunks - 1) / p.chunks;
-        const int length = max(p.chunk_keys, (least + kKeys - 1) / kKeys * kKeys);
-        const int64_t at = start + static_cast<int64_t>(chunk) * length;
-        start = static_cast<int>(min(at, static_cast<int64_t>(end)));
-        end = static_cast<int>(min(at + length, static_cast<int64_t>(end)));
+        const int row = min(row0 + r * 16 + col, rows - 1);
+        draft[r] = p.drafts == 1 ? 0 : row / in_draft;
+        const int in = row - draft[r] * in_draft, t = in / p.group, head = head0 * p.group + in - t * p.group, s = first + draft[r];
+        pos[r] = p.positions[s * p.positions_stride + t];
+        q_at[r] = s * p.q_stride[0] + t * p.q_stride[1] + head * p.q_stride[2];
+        if (!PARTS) out_at[r] = s * p.out_stride[0] + t * p.out_stride[1] + head * p.out_stride[2];
     }
 
     // ---- queries
     U4 qf[RT][kSteps];
     const T *q = static_cast<const T *>(p.q);
+    if (p.q_wide) {
+#pragma unroll
+        for (int r = 0; r < RT; ++r)
+#pragma unroll
+            for (int i = 0; i < kSteps; ++i) {
+                const int e = (4 * i + quad) * S::kPiece;
+                qf[r][i] = *reinterpret_cast<const U4 *>(q + q_at[r] + (e < p.head_dim ? e : 0));
+            }
+    } else {
+#pragma unroll
+        for (int r = 0; r < RT; ++r)
+#pragma unroll
+            for (int i = 0; i < kSteps; ++i) {
+                const int e = (4 * i + quad) * S::kPiece;
+                const T *src = q + q_at[r] + (e < p.head_dim ? e : 0);
+                uint32_t w[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    if constexpr (S::kBf) w[j] = src[2 * j] | static_cast<uint32_t>(src[2 * j + 1]) << 16;
+                    else w[j] = __float_as_uint(src[j]);
+                }
+                qf[r][i] = U4{w[0], w[1], w[2], w[3]};
+            }
+    }
+    if (p.head_dim != DP) {
+#pragma unroll
+        for (int i = 0; i < kSteps; ++i)
+            if ((4 * i + quad) * S::kPiece >= p.head_dim)
+#pragma unroll
+                for (int r = 0; r < RT; ++r) qf[r][i] = U4{0, 0, 0, 0};
+    }
 #pragma unroll
     for (int r = 0; r < RT; ++r)
-#pragma unroll
-        for (int i = 0; i < kSteps; ++i) {
-            const int at = (4 * i + quad) * S::kPiece;
-            U4 v{0, 0, 0, 0};
-            if (q_at[r] >= 0 && at < p.head_dim) {
-                if (p.q_wide) v = *reinterpret_cast<const U4 *>(q + q_at[r] + at);
-                else {
-                    T e[S::kPiece];
-#pragma unroll
-                    for (int j = 0; j < S::kPiece; ++j) e[j] = q[q_at[r] + at + j];
-                    __builtin_memcpy(&v, e, 16);
-                }
-            }
-            qf[r][i] = v;
-        }
+        if (row0 + r * 16 + col >= rows) pos[r] = -1;
 
     F4 acc[RT][kCols];
     float ref[RT], sum[RT];                                   // sum: over the lane's own keys
@@ -176,18 +166,49 @@ __global__ void __launch_bounds__(kAttendThreads, (Shape<T, DP>::waves(RT))) k_a
         for (int c = 0; c < kCols; ++c) acc[r][c] = F4{0, 0, 0, 0};
     }
 
-    // ---- the keys
-    const int step = (WK == 4 ? 4 : 1) * kKeys;
-    int tile = start + (WK == 4 ? wave * kKeys : 0);
+    // ---- the keys: one stretch of the unit's, or each draft's own ones in turn (the waves take the drafts in turn)
     const T *kb = static_cast<const T *>(p.k) + head0 * static_cast<int64_t>(p.k_head_stride);
     const T *vb = static_cast<const T *>(p.v) + head0 * static_cast<int64_t>(p.v_head_stride);
     const int run_k = col >> 2, in_run = col & 3;
+    const int step = WK == 4 && !own ? 4 * kKeys : kKeys;
+    bool any = own;                                           // something may have been summed
+#pragma unroll 1
+    for (int seg = own && WK == 4 ? wave : 0; seg < (own ? p.drafts : 1); seg += own && WK == 4 ? 4 : 1) {
+    const int sequence = first + seg;
+    int row_low[RT], row_high[RT];
+    int lo_all = INT32_MAX, lo_most = -1, hi_all = 0, hi_least = INT32_MAX;
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+        row_low[r] = row_high[r] = 0;
+        if (pos[r] >= 0 && (!own || draft[r] == seg)) {
+            row_low[r] = max(own ? shared : 0, p.window > 0 ? pos[r] - (p.window - 1) : 0);
+            row_high[r] = min(own ? held : shared, pos[r] < INT32_MAX ? pos[r] + 1 : pos[r]);
+            if (row_high[r] <= row_low[r]) row_low[r] = row_high[r] = hi_least = 0;       // sees nothing here: no tile is whole
+            else {
+                lo_all = min(lo_all, row_low[r]); lo_most = max(lo_most, row_low[r]);
+                hi_all = max(hi_all, row_high[r]); hi_least = min(hi_least, row_high[r]);
+            }
+        } else if (pos[r] >= 0) hi_least = 0;
+    }
+    lo_all = wave_least(lo_all); hi_least = wave_least(hi_least);
+    lo_most = wave_most(lo_most); hi_all = wave_most(hi_all);
+    int start = lo_all >= hi_all ? 0 : lo_all / kKeys * kKeys, end = lo_all >= hi_all ? 0 : hi_all;
+    if (PARTS && !own) {
+        // chunks of the planned length, or longer ones where the sequence is longer than was planned for
+        const int span = end - start, least = (span + p.chunks - 1) / p.chunks;
+        const int length = max(p.chunk_keys, (least + kKeys - 1) / kKeys * kKeys);
+        const int64_t at = start + static_cast<int64_t>(part) * length;
+        start = static_cast<int>(min(at, static_cast<int64_t>(end)));
+        end = static_cast<int>(min(at + length, static_cast<int64_t>(end)));
+    }
+    any = any || start < end;
+    int tile = start + (WK == 4 && !own ? wave * kKeys : 0);
 
     // The place of a run of keys: page_size is a multiple of a run, and so is where a tile starts.  Runs behind the last key take
     // the last one's place, so that nothing is read outside pages that hold keys; their scores are masked.
     auto run_place = [&](int t, int run) {
         const int key = min(t + run * kRun, (end - 1) / kRun * kRun);
-        return place_of(p.map, first, key);
+        return place_of(p.map, sequence, key);
     };
     U4 kf[kHalves][kSteps];
     uint32_t vf[kRun][kGroups][kWords];
@@ -402,41 +423,9 @@ __global__ void __launch_bounds__(kAttendThreads, (Shape<T, DP>::waves(RT))) k_a
         }
         if (more) load_values(here_v);
     }
+    }
 #pragma unroll
     for (int r = 0; r < RT; ++r) sum[r] = row_total(sum[r]);
-
-    // ---- sums of the chunks in front (the shared keys of a prefix).  Partial sums are held in the order in which lanes hold them:
-    // vector ((g 4 + i) kVec / 4 + n) 4 + quad of a row are entries (16 g + 4 quad + i) kVec + 4 n + 0..3.
-    if (FINAL && p.chunks > 0) {
-        const int64_t part0 = (static_cast<int64_t>(unit / p.drafts) * p.kv_heads + head0) * p.chunks;
-        const int rows_a = p.tokens * p.group * p.drafts;
-        for (int c = WK == 4 ? wave : 0; c < p.chunks; c += WK == 4 ? 4 : 1) {
-#pragma unroll
-            for (int r = 0; r < RT; ++r) {
-                if (part_row[r] < 0) continue;
-                const int64_t at = (part0 + c) * rows_a + part_row[r];
-                const float2 ml = p.ml[at];
-                if (!(ml.y != 0.0f)) continue;                                       // nothing summed (a sum that is no number goes on)
-                const float now = fmaxf(ref[r], ml.x);
-                const float f = now == ref[r] ? 1.0f : exp2_of((ref[r] - now) * p.c), g1 = now == ml.x ? 1.0f : exp2_of((ml.x - now) * p.c);
-                ref[r] = now;
-                sum[r] = sum[r] * f + ml.y * g1;
-                const F4 *part = reinterpret_cast<const F4 *>(p.acc + at * DP);
-#pragma unroll
-                for (int g = 0; g < kGroups; ++g)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-#pragma unroll
-                        for (int n = 0; n < kVec / 4; ++n) {
-                            const F4 v = part[((g * 4 + i) * (kVec / 4) + n) * 4 + quad];
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) {
-                                acc[r][g * kVec + 4 * n + e][i] = acc[r][g * kVec + 4 * n + e][i] * f + v[e] * g1;
-                            }
-                        }
-            }
-        }
-    }
 
     // ---- the waves of a workgroup join: each brings its sums to the largest reference, then wave i adds up the entries i of all
     if (WK == 4) {
@@ -473,9 +462,12 @@ __global__ void __launch_bounds__(kAttendThreads, (Shape<T, DP>::waves(RT))) k_a
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
         if (row0 + r * 16 + col >= rows) continue;
+        // Partial sums are held in the order in which lanes hold them: vector ((g 4 + i) kVec / 4 + n) 4 + quad of a row are entries
+        // (16 g + 4 quad + i) kVec + 4 n + 0..3.  Where nothing was summed they are not written: the sum of weights says so.
         const float inv = sum[r] != 0.0f ? 1.0f / sum[r] : 0.0f;
-        const int64_t part = FINAL ? 0 : ((static_cast<int64_t>(unit) * p.kv_heads + head0) * p.chunks + chunk) * rows + part_row[r];
-        if (!FINAL && (WK == 1 || wave == 0) && quad == 0) p.ml[part] = make_float2(ref[r], sum[r]);
+        const int64_t at = PARTS ? ((static_cast<int64_t>(unit) * p.kv_heads + head0) * p.parts + part) * rows + row0 + r * 16 + col : 0;
+        if (PARTS && (WK == 1 || wave == 0) && quad == 0) p.ml[at] = make_float2(ref[r], sum[r]);
+        if (PARTS && !any) continue;
 #pragma unroll
         for (int g = 0; g < kGroups; ++g)
 #pragma unroll
@@ -492,20 +484,16 @@ __global__ void __launch_bounds__(kAttendThreads, (Shape<T, DP>::waves(RT))) k_a
 #pragma unroll
                         for (int e = 0; e < 4; ++e) v[e] = acc[r][g * kVec + 4 * n + e][i];
                     }
-                    if (!FINAL) reinterpret_cast<F4 *>(p.acc + part * DP)[((g * 4 + i) * (kVec / 4) + n) * 4 + quad] = v;
+                    if (PARTS) reinterpret_cast<F4 *>(p.acc + at * DP)[((g * 4 + i) * (kVec / 4) + n) * 4 + quad] = v;
 #pragma unroll
                     for (int e = 0; e < 4; ++e) x[4 * n + e] = v[e];
                 }
                 const int d = (16 * g + 4 * quad + i) * kVec;
-                if (FINAL && d < p.head_dim) {
+                if (!PARTS && d < p.head_dim) {
                     T *dst = static_cast<T *>(p.out) + out_at[r] + d;
                     struct alignas(kVec * sizeof(T)) Vec { T e[kVec]; } o;
 #pragma unroll
-                    for (int j = 0; j < kVec; ++j) {
-                        const float y = q_at[r] < 0 || sum[r] == 0.0f ? 0.0f : x[j] * inv;
-                        if constexpr (S::kBf) o.e[j] = __builtin_bit_cast(uint16_t, static_cast<__bf16>(y));
-                        else o.e[j] = y;
-                    }
+                    for (int j = 0; j < kVec; ++j) o.e[j] = rounded<T>(pos[r] < 0 || sum[r] == 0.0f ? 0.0f : x[j] * inv);
                     if (p.out_wide) *reinterpret_cast<Vec *>(dst) = o;
                     else
 #pragma unroll
@@ -515,94 +503,124 @@ __global__ void __launch_bounds__(kAttendThreads, (Shape<T, DP>::waves(RT))) k_a
     }
 }
 
-// Sums of chunks joined, one wave per row: DP / 4 lanes take a chunk's vectors, the others the next chunks'.
-template <typename T, int DP>
+// The parts of a row joined: DP / 4 lanes take a part's vectors, the other lanes the next parts'; WAVES waves per row.
+template <typename T, int DP, int WAVES>
 __global__ void __launch_bounds__(kAttendThreads) k_attend_join(AttendProblem p)
 {
-    constexpr int kVec = Shape<T, DP>::kVec, kLanes = DP / 4, kSets = 64 / kLanes;
-    const int lane = threadIdx.x & 63, vec = lane % kLanes, set = lane / kLanes;
-    const int rows = p.tokens * p.group;
-    const int64_t all = static_cast<int64_t>(p.sequences) * p.kv_heads * rows;
-    const int64_t at = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);
+    constexpr int kVec = Shape<T, DP>::kVec, kLanes = DP / 4, kThreads = 64 * WAVES, kSets = kThreads / kLanes, kAhead = 4;
+    __shared__ float sh_f[WAVES > 1 ? kMaxParts : 1];
+    __shared__ float sh_most[kWavesPerGroup], sh_total[kWavesPerGroup];
+    __shared__ F4 sh_acc[WAVES > 1 ? kWavesPerGroup * kLanes : 1];
+    const int tid = WAVES > 1 ? threadIdx.x : threadIdx.x & 63, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int vec = tid % kLanes, set = tid / kLanes;
+    const int in_draft = p.tokens * p.group, rows = in_draft * p.drafts;
+    const int64_t all = static_cast<int64_t>(p.sequences) * p.kv_heads * in_draft;
+    const int64_t at = WAVES > 1 ? blockIdx.x : static_cast<int64_t>(blockIdx.x) * 4 + wave;
     if (at >= all) return;
-    const int row = static_cast<int>(at % rows);
     const int64_t pair = at / rows;
-    const int head0 = static_cast<int>(pair % p.kv_heads), s = static_cast<int>(pair / p.kv_heads);
-    const int64_t part0 = pair * p.chunks * rows + row;
+    const int row = static_cast<int>(at - pair * rows);
+    const int unit = static_cast<int>(pair / p.kv_heads), head0 = static_cast<int>(pair - static_cast<int64_t>(unit) * p.kv_heads);
+    const int draft = row / in_draft, in = row - draft * in_draft, s = unit * p.drafts + draft, t = in / p.group, h = head0 * p.group + in - t * p.group;
+    const int64_t part0 = pair * p.parts * rows + row;
 
-    float most = -INFINITY;
-    for (int c = lane; c < p.chunks; c += 64) {
-        const float2 ml = p.ml[part0 + static_cast<int64_t>(c) * rows];
-        if (ml.y != 0.0f) most = fmaxf(most, ml.x);
-    }
+    // the first parts' sums are on their way while the weights of all parts are looked at
+    F4 v[kAhead];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i)
+        v[i] = reinterpret_cast<const F4 *>(p.acc + (part0 + static_cast<int64_t>(min(set + i * kSets, p.parts - 1)) * rows) * DP)[vec];
+    float2 ml{-INFINITY, 0.0f};
+    if (tid < p.parts) ml = p.ml[part0 + static_cast<int64_t>(tid) * rows];          // (parts are at most the threads of a row)
+    const int pos = p.positions[s * p.positions_stride + t];
+    const bool some = ml.y != 0.0f;                                                   // (a sum that is no number goes on)
+    float most = some ? ml.x : -INFINITY;
     for (int m = 32; m > 0; m >>= 1) most = fmaxf(most, __shfl_xor(most, m, 64));
-    float total = 0.0f;
+    if (WAVES > 1) {
+        if (lane == 0) sh_most[wave] = most;
+        __syncthreads();
+        most = fmaxf(fmaxf(sh_most[0], sh_most[1]), fmaxf(sh_most[2], sh_most[3]));
+    }
+    const float f = !some ? 0.0f : (ml.x == most ? 1.0f : exp2_of((ml.x - most) * p.c));
+    float total = some ? ml.y * f : 0.0f;
+    for (int m = 32; m > 0; m >>= 1) total += __shfl_xor(total, m, 64);
+    if (WAVES > 1) {
+        if (lane == 0) sh_total[wave] = total;
+        if (tid < kMaxParts) sh_f[tid] = some ? f : -1.0f;                            // (-1: there is nothing to read)
+        __syncthreads();
+        total = (sh_total[0] + sh_total[1]) + (sh_total[2] + sh_total[3]);
+    }
+    const float mine = some ? f : -1.0f;
     F4 acc{0, 0, 0, 0};
-#pragma unroll 4
-    for (int c = set; c < p.chunks; c += kSets) {
-        const float2 ml = p.ml[part0 + static_cast<int64_t>(c) * rows];
-        const F4 v = reinterpret_cast<const F4 *>(p.acc + (part0 + static_cast<int64_t>(c) * rows) * DP)[vec];
-        const float f = !(ml.y != 0.0f) ? 0.0f : (ml.x == most ? 1.0f : exp2_of((ml.x - most) * p.c));
-        total += ml.y * f;
+    for (int c0 = set; c0 - set < p.parts; c0 += kAhead * kSets) {                    // the same count for all
 #pragma unroll
-        for (int e = 0; e < 4; ++e) acc[e] += f == 0.0f && ml.y == ml.y ? 0.0f : v[e] * f;
+        for (int i = 0; i < kAhead; ++i) {
+            const int c = c0 + i * kSets;
+            const float w = c >= p.parts ? -1.0f : (WAVES > 1 ? sh_f[c] : __shfl(mine, c, 64));
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[e] += w < 0.0f ? 0.0f : v[i][e] * w;
+            const int n = c + kAhead * kSets;
+            if (n < p.parts) v[i] = reinterpret_cast<const F4 *>(p.acc + (part0 + static_cast<int64_t>(n) * rows) * DP)[vec];
+        }
     }
 #pragma unroll
-    for (int m = 32; m >= kLanes; m >>= 1) {
-        total += __shfl_xor(total, m, 64);
+    for (int m = 32; m >= kLanes; m >>= 1)
 #pragma unroll
         for (int e = 0; e < 4; ++e) acc[e] += __shfl_xor(acc[e], m, 64);
-    }
-    if (set != 0) return;
+    if (WAVES > 1) {
+        if (lane < kLanes) sh_acc[wave * kLanes + vec] = acc;
+        __syncthreads();
+        if (tid >= kLanes) return;
+        acc = (sh_acc[vec] + sh_acc[kLanes + vec]) + (sh_acc[2 * kLanes + vec] + sh_acc[3 * kLanes + vec]);
+    } else if (set != 0) return;
     const int quad = vec & 3, piece = vec >> 2, n = piece % (kVec / 4), gi = piece / (kVec / 4), i = gi & 3, g = gi >> 2;
     const int d = (16 * g + 4 * quad + i) * kVec + 4 * n;
     if (d >= p.head_dim) return;
-    const int t = row / p.group, h = head0 * p.group + row % p.group;
     T *dst = static_cast<T *>(p.out) + s * p.out_stride[0] + t * p.out_stride[1] + h * p.out_stride[2] + d;
-    const bool some = p.positions[s * p.positions_stride + t] >= 0 && total != 0.0f;
+    const float inv = pos >= 0 && total != 0.0f ? 1.0f / total : 0.0f;
+    struct alignas(4 * sizeof(T)) Vec { T e[4]; } o;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        const float y = some ? acc[e] / total : 0.0f;
-        if constexpr (sizeof(T) == 2) dst[e] = __builtin_bit_cast(uint16_t, static_cast<__bf16>(y));
-        else dst[e] = y;
-    }
+    for (int e = 0; e < 4; ++e) o.e[e] = rounded<T>(inv == 0.0f ? 0.0f : acc[e] * inv);
+    if (p.out_wide) *reinterpret_cast<Vec *>(dst) = o;
+    else
+#pragma unroll
+        for (int e = 0; e < 4; ++e) dst[e] = o.e[e];
 }
 
-template <typename T, int DP, int RT, int WK, bool FINAL>
-hipError_t launch_one(AttendProblem p, int units, hipStream_t stream)
+template <typename T, int DP, int RT, int WK, bool PARTS>
+hipError_t launch_one(AttendProblem p, hipStream_t stream)
 {
-    const int rows = p.tokens * p.group * (FINAL ? 1 : p.drafts), per = 16 * RT * (WK == 4 ? 1 : 4);
+    const int rows = p.tokens * p.group * p.drafts, per = 16 * RT * (WK == 4 ? 1 : 4);
     p.row_blocks = (rows + per - 1) / per;
-    p.items = units * p.kv_heads * (FINAL ? 1 : p.chunks);
+    p.items = p.sequences / p.drafts * p.kv_heads * (PARTS ? p.parts : 1);
     const int64_t grid = p.row_blocks == 1 ? p.items : static_cast<int64_t>((p.items + 7) / 8 * 8) * p.row_blocks;
     if (grid > INT32_MAX) return hipErrorInvalidConfiguration;
-    hipLaunchKernelGGL((k_attend<T, DP, RT, WK, FINAL>), dim3(static_cast<unsigned>(grid)), dim3(kAttendThreads), 0, stream, p);
+    hipLaunchKernelGGL((k_attend<T, DP, RT, WK, PARTS>), dim3(static_cast<unsigned>(grid)), dim3(kAttendThreads), 0, stream, p);
     return hipGetLastError();
 }
 
-template <typename T, int DP, bool FINAL>
-hipError_t launch_rows(const AttendProblem &p, int units, hipStream_t stream)
+template <typename T, int DP, bool PARTS>
+hipError_t launch_rows(const AttendProblem &p, hipStream_t stream)
 {
-    const int rows = p.tokens * p.group * (FINAL ? 1 : p.drafts);
-    if (rows <= 16) return launch_one<T, DP, 1, 4, FINAL>(p, units, stream);
+    const int rows = p.tokens * p.group * p.drafts;
+    if (rows <= 16) return launch_one<T, DP, 1, 4, PARTS>(p, stream);
     if constexpr (DP < 256) {
-        if (rows <= 64) return launch_one<T, DP, 2, 4, FINAL>(p, units, stream);
-        return launch_one<T, DP, 2, 1, FINAL>(p, units, stream);
+        if (rows <= 64) return launch_one<T, DP, 2, 4, PARTS>(p, stream);
+        return launch_one<T, DP, 2, 1, PARTS>(p, stream);
     } else {
-        if (rows <= 32) return launch_one<T, DP, 1, 4, FINAL>(p, units, stream);
-        return launch_one<T, DP, 1, 1, FINAL>(p, units, stream);
+        if (rows <= 32) return launch_one<T, DP, 1, 4, PARTS>(p, stream);
+        return launch_one<T, DP, 1, 1, PARTS>(p, stream);
     }
 }
 
 template <typename T, int DP>
 hipError_t launch_typed(const AttendProblem &p, hipStream_t stream)
 {
-    if (p.chunks == 0) return launch_rows<T, DP, true>(p, p.sequences, stream);
-    hipError_t e = launch_rows<T, DP, false>(p, p.sequences / p.drafts, stream);
+    if (p.parts == 0) return launch_rows<T, DP, false>(p, stream);
+    const hipError_t e = launch_rows<T, DP, true>(p, stream);
     if (e != hipSuccess) return e;
-    if (p.shared_len) return launch_rows<T, DP, true>(p, p.sequences, stream);
+    // Few parts: a wave per row, so that all rows are on their way at once; many: a workgroup, so that a row's parts are.
     const int64_t rows = static_cast<int64_t>(p.sequences) * p.heads * p.tokens;
-    hipLaunchKernelGGL((k_attend_join<T, DP>), dim3(static_cast<unsigned>((rows + 3) / 4)), dim3(kAttendThreads), 0, stream, p);
+    if (p.parts <= 8) hipLaunchKernelGGL((k_attend_join<T, DP, 1>), dim3(static_cast<unsigned>((rows + 3) / 4)), dim3(kAttendThreads), 0, stream, p);
+    else hipLaunchKernelGGL((k_attend_join<T, DP, 4>), dim3(static_cast<unsigned>(rows)), dim3(kAttendThreads), 0, stream, p);
     return hipGetLastError();
 }
 
@@ -629,12 +647,13 @@ AttendPlan plan_attend(int sequences, int drafts, bool shared, int tokens, int h
     int64_t chunks = (4 * compute_units() + base - 1) / (base < 1 ? 1 : base);
     const int64_t most = (longest + least - 1) / least;
     if (chunks > most) chunks = most;
-    if (chunks > 256) chunks = 256;
+    if (chunks > kMaxParts - 1) chunks = kMaxParts - 1;
     if (chunks < 1) chunks = 1;
     if (chunks == 1 && !shared) return a;                      // one pass, nothing to join
     a.chunks = static_cast<int>(chunks);
+    a.parts = a.chunks + (shared ? 1 : 0);
     a.chunk_keys = static_cast<int>(((longest + chunks - 1) / chunks + 127) / 128 * 128);
-    const size_t parts = static_cast<size_t>(sequences / drafts) * kv_heads * a.chunks * rows;
+    const size_t parts = static_cast<size_t>(sequences / drafts) * kv_heads * a.parts * rows;
     a.ml_bytes = (parts * sizeof(float2) + 255) / 256 * 256;
     a.bytes = a.ml_bytes + (parts * dp * sizeof(float) + 255) / 256 * 256;
     return a;

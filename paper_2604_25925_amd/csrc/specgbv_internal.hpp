@@ -174,16 +174,16 @@ struct AttendProblem {
     PageMap map;
     int64_t q_stride[3], out_stride[3], positions_stride;
     int32_t k_page_stride, k_head_stride, k_token_stride, v_page_stride, v_head_stride, v_token_stride;
-    float2 *ml;                    // [units][kv_heads][chunks][rows] reference and sum of a chunk; unit: sequence, or prefix with its drafts
+    float2 *ml;                    // [units][kv_heads][parts][rows] reference and sum of a part; unit: sequence, or prefix with its drafts
     float *acc;                    // the same, with the sums of values
     float c;                       // scale * log2(e)
     float raise;                   // a reference is raised where a score exceeds it by this: weights stay below 2^8
     int sequences, tokens, heads, kv_heads, group, head_dim, drafts, window;
-    int chunks, chunk_keys;        // 0 chunks: one pass without partial sums
+    int parts, chunks, chunk_keys; // 0 parts: one pass without partial sums; else the chunks and, with drafts, their own keys
     int q_wide, out_wide;          // 16-byte loads of q, stores of whole vectors to out
     int items, row_blocks;         // set by the launches
 };
-struct AttendPlan { int chunks, chunk_keys; size_t ml_bytes, bytes; };
+struct AttendPlan { int parts, chunks, chunk_keys; size_t ml_bytes, bytes; };
 AttendPlan plan_attend(int sequences, int drafts, bool shared, int tokens, int heads, int kv_heads, int head_dim, int window,
                        int64_t longest);
 hipError_t launch_attend(const AttendProblem &p, int dtype, hipStream_t stream);

@@ -190,7 +190,7 @@ specgbv_status specgbv_attend_paged(const specgbv_paged_cache *cache, const spec
     p.raise = 8.0f / p.c;
     p.sequences = c.sequences; p.tokens = a.tokens; p.heads = a.heads; p.kv_heads = c.kv_heads; p.group = a.heads / c.kv_heads;
     p.head_dim = c.head_dim; p.drafts = a.prefixes > 0 ? c.sequences / a.prefixes : 1; p.window = a.window;
-    p.chunks = plan.chunks; p.chunk_keys = plan.chunk_keys;
+    p.parts = plan.parts; p.chunks = plan.chunks; p.chunk_keys = plan.chunk_keys;
     const int unit = static_cast<int>(16 / esz);
     p.q_wide = allowed_width(unit, a.q, a.q_stride, 3, esz) == unit;
     p.out_wide = allowed_width(unit, a.out, a.out_stride, 3, esz) == unit;
