@@ -2,22 +2,19 @@
 //
 // With the entries of a row in the order "largest logit first, ties by the lowest index", each of top-k, min-p and top-p keeps the
 // front of the order, and the draw looks for the entry at which the running weight passes a goal.  So everything asked for is a place in
-// that order, by rank or by running weight, and the row needs no sorting: a histogram by value (counts and sums of weights) says in which
-// bin the place lies, and only that bin's entries are put in order.
+// that order, by rank or by running weight, and the row needs no sorting: a histogram says in which bin the place lies, and only that
+// bin's entries are put in order.
 //
-// Weights decide which entry is drawn, and every entry counts: they are exponentials in float64, summed as integers of 43 fractional bits,
-// so that neither the order of the additions nor their rounding can move a border (2^20 entries of at most 1 stay below 2^64; what the
-// rounding of each leaves out is 2^-44 of the largest entry).
+// Weights decide which entry is drawn, and every entry counts, so they are held to more than float32: the histogram's sums are sums of
+// integers, which do not hang on the order of the additions, and running sums are float64 in a fixed order.
 #include "specgbv_internal.hpp"
 
 namespace specgbv {
 namespace {
 
 constexpr int kFilterThreads = 1024, kFilterWaves = kFilterThreads / 64;
-constexpr int kBins = 4096;                   // of the row's histogram, equally wide in the logit
+constexpr int kBins = 4096;                   // of the row's histogram: 1/64 of an octave of the weight each, the last one all below 2^-64
 constexpr int kList = 1024;                   // entries that are put in order at once; bins of a closer histogram
-constexpr float kSpan = 48.0f;                // the histogram's width in temperatures: e^-48 of the largest weight is less than 2^-44
-constexpr double kOne = 8796093022208.0;      // 2^43
 
 typedef unsigned long long u64;
 
@@ -29,6 +26,23 @@ __device__ __forceinline__ uint32_t key_of(float z)
 }
 __device__ __forceinline__ float value_of(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k & 0x7FFFFFFFu : ~k); }
 constexpr uint32_t kNothing = 0x007FFFFFu;    // key of -inf
+// The value of a key that bounds others from above: -0 has a key of its own, which no entry has, and equals the 0 above it.
+__device__ __forceinline__ float bound_of(uint32_t k) { return value_of(k == 0x7FFFFFFFu ? k - 1 : k); }
+
+// Running sum over the wave by moves between lanes, as wave_inclusive_sum.
+__device__ __forceinline__ uint32_t wave_inclusive_count(uint32_t v)
+{
+#define SPECGBV_COUNT_STEP(CTRL, ROW_MASK) \
+    v += static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(v), CTRL, ROW_MASK, 0xf, false))
+    SPECGBV_COUNT_STEP(0x111, 0xf);
+    SPECGBV_COUNT_STEP(0x112, 0xf);
+    SPECGBV_COUNT_STEP(0x114, 0xf);
+    SPECGBV_COUNT_STEP(0x118, 0xf);
+    SPECGBV_COUNT_STEP(0x142, 0xa);
+    SPECGBV_COUNT_STEP(0x143, 0xc);
+#undef SPECGBV_COUNT_STEP
+    return v;
+}
 
 // e^x for x <= 0 in float64: 2^n times the Taylor sum of e^r, |r| <= ln(2) / 2, to r^12 / 12!, whose remainder is 2 10^-16 of it.
 __device__ __forceinline__ double exp_of(double x)
@@ -53,165 +67,266 @@ __device__ __forceinline__ double exp_of(double x)
     return ldexp(s, static_cast<int>(n));
 }
 
-struct RowRule {                              // how a row's entries are weighed and binned
-    float top;                                // its largest logit
-    double inv_t;
-    float bins;                               // bins per unit of the logit
-    uint32_t least;                           // entries of lower keys do not take part
+// How the entries of a row are weighed and binned.  With y = 64 log2(e) (z - top) / T, a weight is 2^(y / 64) = 2^(-bin / 64) (1 + d), bin the
+// nearest integer to -y and |d| < 2^-7.  A bin's sum is 2^(-bin / 64) (n (1 - 2^-7) + sum of (d + 2^-7)), and n and that sum of
+// non-negative numbers share one 64-bit integer: the count in the bits from `shift` on, the sum in units of 2^-(bits + 6) below it.  So an
+// entry costs one addition in LDS.  V takes c bits, the sum of V numbers below 2^bits takes bits + c, which leaves bits = 64 - 2 c: 34 at
+// V = 32003, 28 at 152064 (a weight is then rounded to 2^-35 of itself).
+struct RowRule {
+    float top;                                // the row's largest logit
+    float least;                              // smaller entries do not take part
+    double inv_t, per;                        // 1 / T; y per unit of the logit
+    int shift, bits;
 
     __device__ __forceinline__ double weight(float z) const
     {
         if (z == top) return 1.0;
         return exp_of((static_cast<double>(z) - static_cast<double>(top)) * inv_t);
     }
-    __device__ __forceinline__ u64 fixed(float z) const { return static_cast<u64>(weight(z) * kOne + 0.5); }
-    __device__ __forceinline__ int bin(float z) const
+    __device__ __forceinline__ double scaled(float z) const
     {
-        return z == top ? 0 : static_cast<int>(fminf((top - z) * bins, static_cast<float>(kBins - 1)));
+        return z == top ? 0.0 : fmax((static_cast<double>(z) - static_cast<double>(top)) * per, -static_cast<double>(kBins - 1));
+    }
+    __device__ __forceinline__ int bin(float z) const { return -static_cast<int>(rint(scaled(z))); }
+    // one entry as its bin adds it up: the count of 1 and its part of the sum
+    __device__ __forceinline__ u64 packed(float z, int &bin) const
+    {
+        constexpr double a = 0.69314718055994530942 / 64.0;
+        const double y = scaled(z), k = rint(y), f = y - k;
+        bin = -static_cast<int>(k);
+        double d = a * a * a * a * a / 120.0;                // Taylor sum of 2^(f / 64) - 1; the remainder is below 2^-54
+        d = fma(d, f, a * a * a * a / 24.0);
+        d = fma(d, f, a * a * a / 6.0);
+        d = fma(d, f, a * a / 2.0);
+        d = fma(d, f, a);
+        d *= f;
+        // added to 2^52, the sum leaves its integer in the low bits
+        const u64 low = static_cast<u64>(__double_as_longlong(fma(d, ldexp(1.0, bits + 6), 4503599627370496.0 + ldexp(1.0, bits - 1)))) & 0xFFFFFFFFFFFFFull;
+        return (1ull << shift) + low;
+    }
+    __device__ __forceinline__ uint32_t count_of(u64 sums) const { return static_cast<uint32_t>(sums >> shift); }
+    // the weight of what `sums` adds up, over 2^(-bin / 64)
+    __device__ __forceinline__ double weight_of(u64 sums) const
+    {
+        return static_cast<double>(sums >> shift) * (1.0 - 0.0078125) + ldexp(static_cast<double>(sums & ((1ull << shift) - 1)), -(bits + 6));
+    }
+    // 2^(-bin / 64); what the last bin holds weighs nothing.  2^(-8 group / 64) times 2^(-i / 64), so that a thread with bins next to each
+    // other forms one exponential.
+    static __device__ __forceinline__ double weight_of_group(int group) { return exp_of(group * (-0.69314718055994530942 / 8.0)); }
+    static __device__ __forceinline__ double weight_in_group(int i)
+    {
+        constexpr double step[8] = {1.0, 0.9892280131939755, 0.9785720620877001, 0.9680308967461472, 0.9576032806985737,
+                                    0.9472879907934828, 0.93708381705515, 0.9269895625416927};
+        return step[i];
+    }
+    __device__ __forceinline__ double weight_of_bin(int bin) const
+    {
+        return bin == kBins - 1 ? 0.0 : weight_of_group(bin >> 3) * weight_in_group(bin & 7);
+    }
+    // The smallest value whose bin is at most `bin`: it lies within a step or two of where its weight says.  By a whole wave.
+    __device__ __forceinline__ float least_of(int bin) const
+    {
+        if (bin >= kBins - 1) return least;
+        const uint32_t top_key = key_of(top), low_key = key_of(least);
+        const float about = static_cast<float>(static_cast<double>(top) - (bin + 0.5) / per);
+        const uint32_t at = key_of(about == about ? about : top), from = max(at, low_key + 31u) - 31u;
+        const uint32_t mine = min(from + (threadIdx.x & 63), top_key);
+        const u64 passed = __ballot(this->bin(value_of(mine)) <= bin);
+        return value_of(min(from + (passed ? __ffsll(static_cast<long long>(passed)) - 1 : 63), top_key));
     }
 };
 
-// f(logit, index) for every entry of the row, by all threads of the workgroup: whole 16-byte vectors where the row allows.
-template <typename T, typename F>
+// f(logit, index) for every entry of the row, by all TH threads of the workgroup: whole 16-byte vectors where the row allows, AHEAD of
+// them on their way at once.
+template <int TH, int AHEAD, typename T, typename F>
 __device__ __forceinline__ void for_entries(const T *row, int V, F f)
 {
     constexpr int PV = Elem<T>::kPerVec;
+    const int tid = threadIdx.x;
     const int head = min(V, static_cast<int>((16 - (reinterpret_cast<uintptr_t>(row) & 15)) & 15) / static_cast<int>(sizeof(T)));
     const int vectors = (V - head) / PV, tail = head + vectors * PV;
-    if (static_cast<int>(threadIdx.x) < head) f(Elem<T>::scalar(row + threadIdx.x), static_cast<int>(threadIdx.x));
+    if (tid < head) f(Elem<T>::scalar(row + tid), tid);
     const U4 *vec = reinterpret_cast<const U4 *>(row + head);
-    for (int v = threadIdx.x; v < vectors; v += kFilterThreads) {
-        float z[PV];
-        Elem<T>::unpack(vec[v], z);
+    for (int v = tid; v < vectors; v += TH * AHEAD) {
+        U4 x[AHEAD];
 #pragma unroll
-        for (int j = 0; j < PV; ++j) f(z[j], head + v * PV + j);
+        for (int i = 0; i < AHEAD; ++i) x[i] = vec[min(v + i * TH, vectors - 1)];
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            if (v + i * TH >= vectors) break;
+            float z[PV];
+            Elem<T>::unpack(x[i], z);
+#pragma unroll
+            for (int j = 0; j < PV; ++j) f(z[j], head + (v + i * TH) * PV + j);
+        }
     }
-    if (static_cast<int>(threadIdx.x) < V - tail) f(Elem<T>::scalar(row + tail + threadIdx.x), tail + static_cast<int>(threadIdx.x));
+    if (tid < V - tail) f(Elem<T>::scalar(row + tail + tid), tail + tid);
 }
 
 struct Found {                                // a place in the order
     uint32_t key;
     int index;
-    u64 count, weight;                        // of the entries up to and including it
+    double weight;                            // of the entries up to and including it
 };
 
+struct alignas(16) Listed { u64 order, sums; };       // larger `order` stands in front
+
 struct FilterShared {
-    u64 weight[kBins];                        // after the scan: up to and including the bin
-    uint32_t count[kBins];
-    u64 list_weight[kList];                   // of the list, or of the closer histogram
-    uint32_t list_key[kList];
-    uint32_t list_index[kList];
-    u64 wave_weight[kFilterWaves];
+    u64 sums[kBins];
+    union {
+        Listed list[kList];                   // entries in question, as their bin adds them up
+        u64 closer[kList];                    // a closer histogram
+    };
+    double thread_weight[kFilterThreads];     // running sums over the threads of a wave, each with its bins
+    uint32_t thread_count[kFilterThreads];
+    double wave_weight[kFilterWaves];         // running sums over the waves
+    u64 wave_sums[kFilterWaves];
     uint32_t wave_count[kFilterWaves];
-    uint32_t n, lo, hi;
+    uint32_t n, lo, hi, count0;
+    double weight0;
+    float from, to;
     int bin;
     Found found;
 };
 
-// Running sums over n = kFilterThreads * PER bins in place.
-template <int PER>
-__device__ void scan_bins(FilterShared &sh, u64 *weight, uint32_t *count)
-{
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    u64 w = 0;
-    uint32_t c = 0;
-#pragma unroll
-    for (int i = 0; i < PER; ++i) { w += weight[tid * PER + i]; c += count[tid * PER + i]; }
-    u64 iw = w;
-    uint32_t ic = c;
-    for (int d = 1; d < 64; d <<= 1) {
-        const u64 ow = __shfl_up(iw, d, 64);
-        const uint32_t oc = __shfl_up(ic, d, 64);
-        if (lane >= d) { iw += ow; ic += oc; }
+// What is looked for: the first place whose count (0) or weight (1) reaches the goal, or whose weight exceeds it (2).
+struct Goal {
+    int how;
+    double goal;
+    __device__ __forceinline__ bool reached(uint32_t count, double weight) const
+    {
+        return how == 0 ? count >= goal : (how == 1 ? weight >= goal : weight > goal);
     }
-    if (lane == 63) { sh.wave_weight[wave] = iw; sh.wave_count[wave] = ic; }
-    __syncthreads();
-    for (int i = 0; i < wave; ++i) { iw += sh.wave_weight[i]; ic += sh.wave_count[i]; }
-    iw -= w; ic -= c;
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-        iw += weight[tid * PER + i]; ic += count[tid * PER + i];
-        weight[tid * PER + i] = iw; count[tid * PER + i] = ic;
-    }
-    __syncthreads();
-}
+};
 
-// The first place whose count (by_count) or weight reaches `goal` (at least 1 and at most the row's).
-template <typename T>
-__device__ Found find_place(FilterShared &sh, const T *row, int V, const RowRule &rule, bool by_count, u64 goal)
+// The first place of the row that reaches the goal, which the whole row does.
+template <int TH, typename T>
+__device__ Found find_place(FilterShared &sh, const T *row, int V, const RowRule &rule, Goal goal)
 {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    auto reached = [&](u64 count, u64 weight) { return (by_count ? count : weight) >= goal; };
-    for (int b = tid; b < kBins; b += kFilterThreads)
-        if (reached(sh.count[b], sh.weight[b]) && (b == 0 || !reached(sh.count[b - 1], sh.weight[b - 1]))) sh.bin = b;
+    constexpr int kPer = kBins / TH;
+    // One wave goes down from waves' bins to threads' bins to bins, to the first that holds entries and reaches the goal (where rounding
+    // leaves none: the last that holds some); the others would only take its issue slots.
+    if (wave == 0) {
+        auto first = [&](bool holds, uint32_t c, double w) {
+            const u64 hit = __ballot(holds && goal.reached(c, w)), some = __ballot(holds);
+            return hit ? __ffsll(static_cast<long long>(hit)) - 1 : 63 - __clzll(static_cast<long long>(some | 1));
+        };
+        const int l = lane & (TH / 64 - 1);
+        const double ww = sh.wave_weight[l];
+        const uint32_t wc = sh.wave_count[l], wb = l ? sh.wave_count[l - 1] : 0u;
+        const int block = first(lane < TH / 64 && wc != wb, wc, ww);
+        double w0 = block ? lane_value(ww, block - 1) : 0.0;
+        uint32_t c0 = block ? __builtin_amdgcn_readlane(wc, block - 1) : 0u;
+        const double tw = sh.thread_weight[block * 64 + lane];
+        const uint32_t tc = sh.thread_count[block * 64 + lane], tb = lane ? sh.thread_count[block * 64 + lane - 1] : 0u;
+        const int t = first(tc != tb, c0 + tc, w0 + tw);
+        if (t) { w0 += lane_value(tw, t - 1); c0 += __builtin_amdgcn_readlane(tc, t - 1); }
+        const int b0 = (block * 64 + t) * kPer, b = b0 + (lane & (kPer - 1));
+        const u64 sums = lane < kPer ? sh.sums[b] : 0ull;
+        const uint32_t c = rule.count_of(sums);
+        const double w = c ? rule.weight_of_bin(b) * rule.weight_of(sums) : 0.0;
+        const double iw = wave_inclusive_sum(w);
+        const uint32_t ic = wave_inclusive_count(c);
+        const int i = first(c != 0, c0 + ic, w0 + iw);
+        const uint32_t n = __builtin_amdgcn_readlane(c, i);
+        if (i) { w0 += lane_value(iw, i - 1); c0 += __builtin_amdgcn_readlane(ic, i) - n; }
+        const float from = rule.least_of(b0 + i);
+        const float to = b0 + i == 0 ? rule.top : bound_of(key_of(rule.least_of(b0 + i - 1)) - 1);
+        if (lane == 0) { sh.bin = b0 + i; sh.n = n; sh.count0 = c0; sh.weight0 = w0; sh.from = from; sh.to = to; }
+    }
     __syncthreads();
-    const int bin = sh.bin;
-    u64 count0 = bin ? sh.count[bin - 1] : 0, weight0 = bin ? sh.weight[bin - 1] : 0;
-    uint32_t n = sh.count[bin] - static_cast<uint32_t>(count0);
-    uint32_t lo = 0, hi = 0xFFFFFFFFu;
-    bool closer = false;                                    // the keys in question are [lo, hi], else the bin
-    auto inside = [&](float z, uint32_t key) { return key >= rule.least && (closer ? key >= lo && key <= hi : rule.bin(z) == bin); };
+    const uint32_t count0 = sh.count0;
+    const double weight0 = sh.weight0, factor = rule.weight_of_bin(sh.bin);
+    uint32_t n = sh.n;
+    u64 front = 0;                                          // of the bin's entries in front of those in question
+    float from_z = sh.from, to_z = sh.to;                   // the entries in question
+    auto inside = [&](float z) { return z >= from_z && z <= to_z; };
+    auto weight_at = [&](u64 sums) { return weight0 + factor * rule.weight_of(sums); };
+    auto reached = [&](u64 sums) { return goal.reached(count0 + rule.count_of(sums), weight_at(sums)); };
 
     while (n > kList) {
         // keys of the entries in question, and a closer histogram over them
         __syncthreads();
-        if (tid == 0) { sh.lo = 0xFFFFFFFFu; sh.hi = 0; }
+        if (tid == 0) { sh.lo = 0xFFFFFFFFu; sh.hi = 0; sh.bin = -1; }
         __syncthreads();
         uint32_t least = 0xFFFFFFFFu, most = 0;
-        for_entries(row, V, [&](float z, int) {
+        for_entries<TH, 4>(row, V, [&](float z, int) {
             const uint32_t key = key_of(z);
-            if (inside(z, key)) { least = min(least, key); most = max(most, key); }
+            if (inside(z)) { least = min(least, key); most = max(most, key); }
         });
         atomicMin(&sh.lo, least);
         atomicMax(&sh.hi, most);
-        sh.list_weight[tid] = 0; sh.list_key[tid] = 0;
+        for (int i = tid; i < kList; i += TH) sh.closer[i] = 0;
         __syncthreads();
         const uint32_t from = sh.lo, to = sh.hi;
-        if (from == to) { lo = hi = from; closer = true; break; }                  // ties alone
+        if (from == to) { from_z = to_z = value_of(from); break; }                  // ties alone
         int shift = 0;
         while (((to - from) >> shift) >= kList) ++shift;
-        for_entries(row, V, [&](float z, int) {
+        for_entries<TH, 1>(row, V, [&](float z, int) {
             const uint32_t key = key_of(z);
-            if (inside(z, key)) {
-                atomicAdd(&sh.list_key[(to - key) >> shift], 1u);
-                atomicAdd(&sh.list_weight[(to - key) >> shift], rule.fixed(z));
+            if (inside(z)) {
+                int b;
+                atomicAdd(&sh.closer[(to - key) >> shift], rule.packed(z, b));
             }
         });
         __syncthreads();
-        scan_bins<1>(sh, sh.list_weight, sh.list_key);
-        if (reached(count0 + sh.list_key[tid], weight0 + sh.list_weight[tid]) &&
-            (tid == 0 || !reached(count0 + sh.list_key[tid - 1], weight0 + sh.list_weight[tid - 1]))) sh.bin = tid;
+        // running sums
+        u64 own[kList / TH], run = 0;
+#pragma unroll
+        for (int i = 0; i < kList / TH; ++i) own[i] = run += sh.closer[tid * (kList / TH) + i];
+        u64 incl = run;
+        for (int d = 1; d < 64; d <<= 1) {
+            const u64 o = __shfl_up(incl, d, 64);
+            if (lane >= d) incl += o;
+        }
+        if (lane == 63) sh.wave_sums[wave] = incl;
         __syncthreads();
-        const int b = sh.bin;
-        n = sh.list_key[b] - (b ? sh.list_key[b - 1] : 0u);
-        if (b) { count0 += sh.list_key[b - 1]; weight0 += sh.list_weight[b - 1]; }
+        u64 before = front + incl - run;
+        for (int i = 0; i < wave; ++i) before += sh.wave_sums[i];
+#pragma unroll
+        for (int i = 0; i < kList / TH; ++i) sh.closer[tid * (kList / TH) + i] = before + own[i];
+        __syncthreads();
+        for (int i = tid; i < kList; i += TH) {
+            const u64 before_i = i ? sh.closer[i - 1] : front;
+            if (sh.closer[i] != before_i && reached(sh.closer[i]) && (before_i == front || !reached(before_i))) sh.bin = i;
+        }
+        __syncthreads();
+        int b = sh.bin;
+        if (b < 0) b = static_cast<int>((to - from) >> shift);                     // (rounding: the last one)
+        const u64 upto = sh.closer[b];
+        if (b) front = sh.closer[b - 1];
+        n = rule.count_of(upto - front);
         const uint32_t top = to - (static_cast<uint32_t>(b) << shift), width = (1u << shift) - 1;
-        hi = top; lo = top - from >= width ? top - width : from;
-        closer = true;
+        to_z = bound_of(top); from_z = value_of(top - from >= width ? top - width : from);
     }
     __syncthreads();
 
     if (n > kList) {                                        // more ties than the list holds: by index, a stretch of the row per wave
-        const u64 each = rule.fixed(value_of(lo));
-        const u64 nth = by_count ? goal - count0 : (goal - weight0 + each - 1) / each;         // from 1 on
-        const int stretch = (V + kFilterWaves - 1) / kFilterWaves, from = min(V, wave * stretch), to = min(V, from + stretch);
+        int b;
+        const u64 one = rule.packed(to_z, b);
+        const double each = factor * rule.weight_of(one), gone = weight_at(front);
+        double nth = goal.how == 0 ? goal.goal - (count0 + rule.count_of(front)) : (goal.goal - gone) / each;
+        nth = goal.how == 0 ? nth : (goal.how == 1 ? ceil(nth) : floor(nth) + 1.0);
+        nth = nth >= 1.0 ? nth : 1.0;
+        const uint32_t place = nth < n ? static_cast<uint32_t>(nth) : n;
+        const int stretch = (V + TH / 64 - 1) / (TH / 64), from = min(V, wave * stretch), to = min(V, from + stretch);
         uint32_t mine = 0;
         for (int i = from; i < to; i += 64) {
-            const bool is = i + lane < to && key_of(Elem<T>::scalar(row + min(i + lane, V - 1))) == lo;
+            const bool is = i + lane < to && Elem<T>::scalar(row + min(i + lane, V - 1)) == to_z;
             mine += __popcll(__ballot(is));
         }
-        if (lane == 0) sh.wave_count[wave] = mine;
+        if (lane == 0) sh.wave_sums[wave] = mine;
         __syncthreads();
-        u64 before = 0;
-        for (int i = 0; i < wave; ++i) before += sh.wave_count[i];
-        if (before < nth && nth <= before + mine) {         // one wave
+        uint32_t before = 0;
+        for (int i = 0; i < wave; ++i) before += static_cast<uint32_t>(sh.wave_sums[i]);
+        if (before < place && place <= before + mine) {     // one wave
             for (int i = from; i < to; i += 64) {
-                const bool is = i + lane < to && key_of(Elem<T>::scalar(row + min(i + lane, V - 1))) == lo;
+                const bool is = i + lane < to && Elem<T>::scalar(row + min(i + lane, V - 1)) == to_z;
                 const u64 all = __ballot(is);
                 const uint32_t here = __popcll(all);
-                if (nth <= before + here) {
-                    if (is && before + __popcll(all & ((2ull << lane) - 1)) == nth)
-                        sh.found = Found{lo, i + lane, count0 + nth, weight0 + nth * each};
+                if (place <= before + here) {
+                    if (is && before + __popcll(all & ((2ull << lane) - 1)) == place) sh.found = Found{key_of(to_z), i + lane, weight_at(front + place * one)};
                     break;
                 }
                 before += here;
@@ -224,23 +339,30 @@ __device__ Found find_place(FilterShared &sh, const T *row, int V, const RowRule
     // the entries in question in order: each thread counts what stands in front of its own
     if (tid == 0) sh.n = 0;
     __syncthreads();
-    for_entries(row, V, [&](float z, int i) {
-        const uint32_t key = key_of(z);
-        if (inside(z, key)) {
+    for_entries<TH, 8>(row, V, [&](float z, int i) {
+        if (inside(z)) {
             const uint32_t at = atomicAdd(&sh.n, 1u);
-            if (at < kList) { sh.list_key[at] = key; sh.list_index[at] = i; sh.list_weight[at] = rule.fixed(z); }
+            if (at < kList) sh.list[at].order = static_cast<u64>(key_of(z)) << 32 | ~static_cast<uint32_t>(i);
         }
     });
     __syncthreads();
-    if (tid < static_cast<int>(n)) {
-        const uint32_t key = sh.list_key[tid], index = sh.list_index[tid];
-        const u64 own = sh.list_weight[tid];
-        u64 count = count0, weight = weight0;
+    for (uint32_t e = tid; e < n; e += TH) {
+        int b;
+        sh.list[e].sums = rule.packed(value_of(static_cast<uint32_t>(sh.list[e].order >> 32)), b);
+    }
+    __syncthreads();
+    for (uint32_t e = tid; e < n; e += TH) {
+        const Listed own = sh.list[e];
+        u64 sums = front;
+#pragma unroll 4
         for (uint32_t i = 0; i < n; ++i) {
-            const uint32_t k = sh.list_key[i];
-            if (k > key || (k == key && sh.list_index[i] < index)) { ++count; weight += sh.list_weight[i]; }
+            const Listed x = sh.list[i];
+            sums += x.order > own.order ? x.sums : 0ull;
         }
-        if (reached(count + 1, weight + own) && !reached(count, weight)) sh.found = Found{key, static_cast<int>(index), count + 1, weight + own};
+        const u64 incl = sums + own.sums;
+        const bool last = rule.count_of(incl - front) == n;                        // (where rounding leaves none)
+        if ((reached(incl) || last) && (sums == front || !reached(sums)))
+            sh.found = Found{static_cast<uint32_t>(own.order >> 32), static_cast<int>(~static_cast<uint32_t>(own.order)), weight_at(incl)};
     }
     __syncthreads();
     return sh.found;
@@ -263,7 +385,7 @@ struct RowAsked {
 };
 
 // A row of any length and type, read from memory in every step.
-template <typename T>
+template <int TH, typename T>
 __device__ __forceinline__ void filter_row(const FilterProblem &p, int r, FilterShared &sh)
 {
     const int tid = threadIdx.x;
@@ -273,11 +395,12 @@ __device__ __forceinline__ void filter_row(const FilterProblem &p, int r, Filter
     const float temperature = asked.temperature, top_p = asked.top_p, min_p = asked.min_p;
     const int k = asked.k;
 
-    for (int b = tid; b < kBins; b += kFilterThreads) { sh.count[b] = 0; sh.weight[b] = 0; }
+    for (int b = tid; b < kBins; b += TH) sh.sums[b] = 0;
     if (tid == 0) sh.hi = kNothing;
     __syncthreads();
-    uint32_t most = kNothing;
-    for_entries(row, V, [&](float z, int) { most = max(most, key_of(z)); });
+    float highest = -INFINITY;
+    for_entries<TH, 8>(row, V, [&](float z, int) { highest = fmaxf(highest, z); });          // (what is no number is passed over)
+    uint32_t most = key_of(highest);
     for (int m = 32; m > 0; m >>= 1) most = max(most, static_cast<uint32_t>(__shfl_xor(static_cast<int>(most), m, 64)));
     if ((tid & 63) == 0) atomicMax(&sh.hi, most);
     __syncthreads();
@@ -290,8 +413,11 @@ __device__ __forceinline__ void filter_row(const FilterProblem &p, int r, Filter
         RowRule rule;
         rule.top = value_of(most);
         rule.inv_t = 1.0 / static_cast<double>(temperature);
-        rule.bins = fminf((kBins - 1) / (kSpan * temperature), 3.0e38f);
-        rule.least = kNothing + 1;
+        rule.per = rule.inv_t * (64.0 * 1.44269504088896340736);
+        const int length = 32 - __clz(V);                   // bits of V
+        rule.shift = 64 - length;
+        rule.bits = min(44, 64 - 2 * length);
+        rule.least = -3.402823466e38f;
         if (min_p > 0.0f) {
             // the lowest key whose weight is at least min_p, among the keys around top + temperature ln min_p
             const float about = static_cast<float>(static_cast<double>(rule.top) + static_cast<double>(temperature) * log(static_cast<double>(min_p)));
@@ -299,71 +425,111 @@ __device__ __forceinline__ void filter_row(const FilterProblem &p, int r, Filter
             const uint32_t mine = min(centre - 31u + (tid & 63), most);
             const u64 passed = __ballot(rule.weight(value_of(mine)) >= static_cast<double>(min_p));
             const int first = passed ? __ffsll(static_cast<long long>(passed)) - 1 : 63;
-            rule.least = min(centre - 31u + first, most);
+            rule.least = value_of(min(centre - 31u + first, most));
         }
-        for_entries(row, V, [&](float z, int) {
-            if (key_of(z) >= rule.least) {
-                const int b = rule.bin(z);
-                atomicAdd(&sh.count[b], 1u);
-                atomicAdd(&sh.weight[b], rule.fixed(z));
+        cut_key = key_of(rule.least);
+        for_entries<TH, 2>(row, V, [&](float z, int) {
+            if (z >= rule.least) {
+                int b;
+                const u64 one = rule.packed(z, b);
+                atomicAdd(&sh.sums[b], one);
             }
         });
         __syncthreads();
-        scan_bins<kBins / kFilterThreads>(sh, sh.weight, sh.count);
-        u64 total = sh.weight[kBins - 1];
-        cut_key = rule.least;
-        if (static_cast<uint32_t>(k) < sh.count[kBins - 1]) {
-            const Found f = find_place(sh, row, V, rule, true, static_cast<u64>(k));
-            cut_key = f.key; cut_index = f.index; total = f.weight;
+        // ---- running counts and weights over the threads' bins
+        constexpr int kPer = kBins / TH;
+        static_assert(8 % kPer == 0, "a thread's bins lie in one group");
+        const int lane = tid & 63, wave = tid >> 6;
+        const double group = RowRule::weight_of_group(tid * kPer >> 3);
+        uint32_t run_c = 0;
+        double run_w = 0.0;
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            const u64 sums = sh.sums[tid * kPer + i];
+            run_c += rule.count_of(sums);
+            if (tid * kPer + i < kBins - 1) run_w += group * (kPer == 8 ? RowRule::weight_in_group(i) : (tid & 1 ? RowRule::weight_in_group(4 + i % 4) : RowRule::weight_in_group(i % 4))) * rule.weight_of(sums);
         }
-        if (top_p < 1.0f) {
-            const double goal = ceil(static_cast<double>(top_p) * static_cast<double>(total));
-            const Found f = find_place(sh, row, V, rule, false, goal < 1.0 ? 1 : min(static_cast<u64>(goal), total));
-            cut_key = f.key; cut_index = f.index; total = f.weight;
+        const double iw = wave_inclusive_sum(run_w);
+        const uint32_t ic = wave_inclusive_count(run_c);
+        sh.thread_weight[tid] = iw;
+        sh.thread_count[tid] = ic;
+        if (lane == 63) { sh.wave_weight[wave] = iw; sh.wave_count[wave] = ic; }
+        __syncthreads();
+        if (wave == 0) {
+            const double ww = wave_inclusive_sum(lane < TH / 64 ? sh.wave_weight[lane & (TH / 64 - 1)] : 0.0);
+            const uint32_t wc = wave_inclusive_count(lane < TH / 64 ? sh.wave_count[lane & (TH / 64 - 1)] : 0u);
+            if (lane < TH / 64) { sh.wave_weight[lane] = ww; sh.wave_count[lane] = wc; }
         }
-        if (p.out_tokens) {
-            const double goal = static_cast<double>(p.u[r]) * static_cast<double>(total);
-            token = find_place(sh, row, V, rule, false, goal >= 0.0 ? (goal < static_cast<double>(total) ? min(static_cast<u64>(goal) + 1, total) : total) : 1).index;
+        __syncthreads();
+        const uint32_t all = sh.wave_count[TH / 64 - 1];
+        double total = sh.wave_weight[TH / 64 - 1];
+        bool cut = false;
+        Found last{};
+#pragma unroll 1
+        for (int mode = 0; mode < 3; ++mode) {              // top_k, top_p, the draw
+            Goal goal{mode, 0.0};
+            if (mode == 0) {
+                if (static_cast<uint32_t>(k) >= all) continue;
+                goal.goal = k;
+            } else if (mode == 1) {
+                if (!(top_p < 1.0f)) continue;
+                goal.goal = fmin(fmax(static_cast<double>(top_p) * total, 1e-300), total);
+            } else {
+                if (!p.out_tokens) continue;
+                goal.goal = fmax(static_cast<double>(p.u[r]) * total, 0.0);
+                if (!(goal.goal < total)) {                 // the last place
+                    if (cut) { token = last.index; continue; }
+                    goal = Goal{0, static_cast<double>(all)};
+                }
+            }
+            const Found f = find_place<TH>(sh, row, V, rule, goal);
+            if (mode == 2) token = f.index;
+            else { last = f; cut = true; total = f.weight; cut_key = f.key; cut_index = f.index; }
         }
     }
     if (p.out_tokens && tid == 0) p.out_tokens[r] = token;
     if (!p.kept) return;
     T *kept = static_cast<T *>(p.kept) + r * p.kept_stride;
     constexpr int PV = Elem<T>::kPerVec;
-    auto stays = [&](float z, int i) {
-        const uint32_t key = key_of(z);
-        return key > cut_key || (key == cut_key && i <= cut_index);
-    };
+    const float cut_z = value_of(cut_key);                  // (where the row is empty: the lowest finite value)
+    auto stays = [&](float z, int i) { return z > cut_z || (z == cut_z && i <= cut_index); };
     const T gone = sizeof(T) == 2 ? static_cast<T>(0xFF80u) : __builtin_bit_cast(float, 0xFF800000u);
     const int head = min(V, static_cast<int>((16 - (reinterpret_cast<uintptr_t>(row) & 15)) & 15) / static_cast<int>(sizeof(T)));
     const bool wide = ((reinterpret_cast<uintptr_t>(row) ^ reinterpret_cast<uintptr_t>(kept)) & 15) == 0;
     const int vectors = wide ? (V - head) / PV : 0;
-    for (int v = tid; v < vectors; v += kFilterThreads) {
-        const int i = head + v * PV;
-        const U4 raw = *reinterpret_cast<const U4 *>(row + i);
-        float z[PV];
-        T e[PV];
-        Elem<T>::unpack(raw, z);
-        __builtin_memcpy(e, &raw, 16);
+    constexpr int kAtOnce = 4;
+    for (int v0 = tid; v0 < vectors; v0 += TH * kAtOnce) {
+        U4 raw[kAtOnce];
 #pragma unroll
-        for (int j = 0; j < PV; ++j) e[j] = stays(z[j], i + j) ? e[j] : gone;
-        U4 out;
-        __builtin_memcpy(&out, e, 16);
-        *reinterpret_cast<U4 *>(kept + i) = out;
+        for (int n = 0; n < kAtOnce; ++n) raw[n] = *reinterpret_cast<const U4 *>(row + head + min(v0 + n * TH, vectors - 1) * PV);
+#pragma unroll
+        for (int n = 0; n < kAtOnce; ++n) {
+            const int i = head + (v0 + n * TH) * PV;
+            if (v0 + n * TH >= vectors) break;
+            float z[PV];
+            T e[PV];
+            Elem<T>::unpack(raw[n], z);
+            __builtin_memcpy(e, &raw[n], 16);
+#pragma unroll
+            for (int j = 0; j < PV; ++j) e[j] = stays(z[j], i + j) ? e[j] : gone;
+            U4 out;
+            __builtin_memcpy(&out, e, 16);
+            *reinterpret_cast<U4 *>(kept + i) = out;
+        }
     }
     const int done = vectors * PV;                          // entries in front of and behind the vectors
-    for (int j = tid; j < V - done; j += kFilterThreads) {
+    for (int j = tid; j < V - done; j += TH) {
         const int i = j < head || !wide ? j : j + done;
         const T e = row[i];
         kept[i] = stays(Elem<T>::scalar(row + i), i) ? e : gone;
     }
 }
 
-template <typename T>
-__global__ void __launch_bounds__(kFilterThreads) k_filter(FilterProblem p)
+template <int TH, typename T>
+__global__ void __launch_bounds__(TH, 4) k_filter(FilterProblem p)
 {
     __shared__ FilterShared sh;
-    filter_row<T>(p, blockIdx.x, sh);
+    filter_row<TH, T>(p, blockIdx.x, sh);
 }
 
 // bfloat16 rows of up to NV 8192 - 8 entries.
@@ -397,21 +563,6 @@ struct Value {                                // the n-th of `all` entries of on
     uint32_t nth, all;
     double weight;                            // of the entries up to and including it
 };
-
-// Running sum over the wave by moves between lanes, as wave_inclusive_sum.
-__device__ __forceinline__ uint32_t wave_inclusive_count(uint32_t v)
-{
-#define SPECGBV_COUNT_STEP(CTRL, ROW_MASK) \
-    v += static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(v), CTRL, ROW_MASK, 0xf, false))
-    SPECGBV_COUNT_STEP(0x111, 0xf);
-    SPECGBV_COUNT_STEP(0x112, 0xf);
-    SPECGBV_COUNT_STEP(0x114, 0xf);
-    SPECGBV_COUNT_STEP(0x118, 0xf);
-    SPECGBV_COUNT_STEP(0x142, 0xa);
-    SPECGBV_COUNT_STEP(0x143, 0xc);
-#undef SPECGBV_COUNT_STEP
-    return v;
-}
 
 __device__ __forceinline__ u64 lane_bits_of(u64 v, int src)
 {
@@ -795,10 +946,11 @@ __global__ void __launch_bounds__(kFilterThreads) k_filter_counts(FilterProblem 
         }
         __syncthreads();
     }
+    if constexpr (!kMayOverflow) return;
     __syncthreads();
     for (int i = 0; i <= nth_row; ++i)
         if (again[i / 32] >> i % 32 & 1) {                         // uniform
-            filter_row<uint16_t>(p, blockIdx.x + i * gridDim.x, shared.f);
+            filter_row<kFilterThreads, uint16_t>(p, blockIdx.x + i * gridDim.x, shared.f);
             __syncthreads();
         }
 }
@@ -821,8 +973,13 @@ hipError_t launch_filter(const FilterProblem &p, int dtype, hipStream_t stream)
     if (dtype == 1 && span <= 8 * 8192) return launch_counts<8>(p, stream);
     if (dtype == 1 && span <= 16 * 8192) return launch_counts<16>(p, stream);
     if (dtype == 1 && span <= 20 * 8192) return launch_counts<20>(p, stream);
-    if (dtype == 1) hipLaunchKernelGGL((k_filter<uint16_t>), dim3(p.rows), dim3(kFilterThreads), 0, stream, p);
-    else hipLaunchKernelGGL((k_filter<float>), dim3(p.rows), dim3(kFilterThreads), 0, stream, p);
+    // A row a compute unit: 16 waves each; more: 8, so that two rows share a unit and one's waits are the other's work.
+    const bool few = p.rows <= compute_units();
+    const dim3 grid(p.rows);
+    if (dtype == 1 && few) hipLaunchKernelGGL((k_filter<1024, uint16_t>), grid, dim3(1024), 0, stream, p);
+    else if (dtype == 1) hipLaunchKernelGGL((k_filter<512, uint16_t>), grid, dim3(512), 0, stream, p);
+    else if (few) hipLaunchKernelGGL((k_filter<1024, float>), grid, dim3(1024), 0, stream, p);
+    else hipLaunchKernelGGL((k_filter<512, float>), grid, dim3(512), 0, stream, p);
     return hipGetLastError();
 }
 
