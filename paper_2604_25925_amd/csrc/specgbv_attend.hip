@@ -40,7 +40,7 @@ template <typename T, int DP> struct Shape {
     static constexpr int kGroups = DP / (16 * kVec);         // such vectors per key
     static constexpr int kCols = kGroups * kVec;             // result tiles of 16 entries
     // waves per SIMD that the registers of a tile, its rows and their sums leave room for
-    static constexpr int waves(int RT) { return DP == 256 || (!kBf && DP == 128 && RT == 2) ? 1 : 2; }
+    static constexpr int waves(int RT) { return DP == 256 || (!kBf && DP == 128 && RT == 2) ? 1 : (kBf && DP == 128 && RT == 1 ? 3 : 2); }
 };
 
 constexpr int kMaxParts = 256;                // partial sums of a row at most: a workgroup's threads
@@ -51,22 +51,34 @@ template <> __device__ __forceinline__ uint16_t rounded<uint16_t>(float x) { ret
 
 __device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }      // (2^-126 and below: 0)
 
-__device__ __forceinline__ int wave_least(int x)
+// Over the 16 rows of a wave, which its four quarters hold alike: by moves between the lanes of a quarter.
+__device__ __forceinline__ int rows_least(int x)
 {
-    for (int m = 32; m > 0; m >>= 1) x = min(x, __shfl_xor(x, m, 64));
-    return __builtin_amdgcn_readfirstlane(x);
+    x = min(x, __builtin_amdgcn_update_dpp(x, x, 0x111, 0xf, 0xf, false));
+    x = min(x, __builtin_amdgcn_update_dpp(x, x, 0x112, 0xf, 0xf, false));
+    x = min(x, __builtin_amdgcn_update_dpp(x, x, 0x114, 0xf, 0xf, false));
+    x = min(x, __builtin_amdgcn_update_dpp(x, x, 0x118, 0xf, 0xf, false));
+    return __builtin_amdgcn_readlane(x, 15);
 }
-__device__ __forceinline__ int wave_most(int x) { return -wave_least(-x); }
+__device__ __forceinline__ int rows_most(int x) { return ~rows_least(~x); }
 
 // Largest and sum over the four lanes of a row (l, l ^ 16, l ^ 32, l ^ 48).
 __device__ __forceinline__ float row_largest(float x) { x = fmaxf(x, __shfl_xor(x, 16, 64)); return fmaxf(x, __shfl_xor(x, 32, 64)); }
 __device__ __forceinline__ float row_total(float x) { x += __shfl_xor(x, 16, 64); return x + __shfl_xor(x, 32, 64); }
 
-template <typename T> __device__ __forceinline__ bool not_finite(uint32_t w);      // any entry of a 32-bit word
-template <> __device__ __forceinline__ bool not_finite<float>(uint32_t w) { return (w & 0x7F800000u) == 0x7F800000u; }
-template <> __device__ __forceinline__ bool not_finite<uint16_t>(uint32_t w)
+// Not 0 where an entry of a 32-bit word is not finite: its exponent's bits, all ones, carry out of it when one is added.
+template <typename T> __device__ __forceinline__ uint32_t exponents_full(uint32_t w)
 {
-    return (w & 0x7F800000u) == 0x7F800000u || (w & 0x7F80u) == 0x7F80u;
+    if constexpr (sizeof(T) == 4) return ((w & 0x7FFFFFFFu) + 0x00800000u) & 0x80000000u;
+    else return (((w & 0x7FFF7FFFu) + 0x00800080u) & 0x80008000u);
+}
+
+// A sequence's row of the table through scalar loads: it is read by whole waves, and nothing in the kernel writes it.
+typedef const int32_t __attribute__((address_space(4))) *ConstTable;
+__device__ __forceinline__ Place place_in(const PageMap &m, ConstTable table, int32_t pos)
+{
+    const int32_t n = m.page.div(pos), page = table[n];         // pos lies in front of the table's end
+    return {static_cast<uint32_t>(page) < static_cast<uint32_t>(m.pages) ? page : -1, m.page.mod(pos, n)};
 }
 
 // One entry's bits against a kind of value that is not finite: 0 not a number, 1 +inf, 2 -inf.
@@ -92,12 +104,12 @@ __global__ void __launch_bounds__(kAttendThreads, (Shape<T, DP>::waves(RT))) k_a
     int item, block;
     if (p.row_blocks == 1) { item = blockIdx.x; block = 0; }
     else {
-        const int per = 8 * p.row_blocks, at = blockIdx.x % per;
-        item = blockIdx.x / per * 8 + at % 8; block = at / 8;
+        const int set = p.by_blocks.div(blockIdx.x >> 3);
+        item = set * 8 + (blockIdx.x & 7); block = p.by_blocks.mod(blockIdx.x >> 3, set);
         if (item >= p.items) return;
     }
-    const int head0 = item % p.kv_heads, rest = item / p.kv_heads;
-    const int part = PARTS ? rest % p.parts : 0, unit = PARTS ? rest / p.parts : rest;
+    const int rest = p.by_kv_heads.div(item), head0 = p.by_kv_heads.mod(item, rest);
+    const int unit = PARTS ? p.by_parts.div(rest) : rest, part = PARTS ? p.by_parts.mod(rest, unit) : 0;
     const bool own = PARTS && p.shared_len && part == p.chunks;       // the drafts' own keys, behind the shared ones
     const int first = unit * p.drafts;                        // its first sequence
     const int in_draft = p.tokens * p.group, rows = in_draft * p.drafts;
@@ -106,14 +118,23 @@ __global__ void __launch_bounds__(kAttendThreads, (Shape<T, DP>::waves(RT))) k_a
     const int held = static_cast<int>(capacity_of(p.map));
     const int shared = p.shared_len ? max(0, min(p.shared_len[unit], held)) : held;
 
+    // Nothing is left for this part where the planned chunks in front of it cover all that the drafts share.
+    if (PARTS && !own && p.shared_len && part > 0 && static_cast<int64_t>(part) * p.chunk_keys >= shared) {
+        for (int i = threadIdx.x; i < 16 * RT * (WK == 4 ? 1 : 4); i += kAttendThreads) {
+            const int row = block * 16 * RT * (WK == 4 ? 1 : 4) + i;
+            if (row < rows) p.ml[((static_cast<int64_t>(unit) * p.kv_heads + head0) * p.parts + part) * rows + row] = make_float2(-INFINITY, 0.0f);
+        }
+        return;
+    }
+
     // Rows behind the last one take its place (their loads are those of the last row) and are nowhere stored.
     int64_t q_at[RT], out_at[RT];
     int pos[RT], draft[RT];
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
         const int row = min(row0 + r * 16 + col, rows - 1);
-        draft[r] = p.drafts == 1 ? 0 : row / in_draft;
-        const int in = row - draft[r] * in_draft, t = in / p.group, head = head0 * p.group + in - t * p.group, s = first + draft[r];
+        draft[r] = p.by_in_draft.div(row);
+        const int in = p.by_in_draft.mod(row, draft[r]), t = p.by_group.div(in), head = head0 * p.group + p.by_group.mod(in, t), s = first + draft[r];
         pos[r] = p.positions[s * p.positions_stride + t];
         q_at[r] = s * p.q_stride[0] + t * p.q_stride[1] + head * p.q_stride[2];
         if (!PARTS) out_at[r] = s * p.out_stride[0] + t * p.out_stride[1] + head * p.out_stride[2];
@@ -190,8 +211,8 @@ __global__ void __launch_bounds__(kAttendThreads, (Shape<T, DP>::waves(RT))) k_a
             }
         } else if (pos[r] >= 0) hi_least = 0;
     }
-    lo_all = wave_least(lo_all); hi_least = wave_least(hi_least);
-    lo_most = wave_most(lo_most); hi_all = wave_most(hi_all);
+    lo_all = rows_least(lo_all); hi_least = rows_least(hi_least);
+    lo_most = rows_most(lo_most); hi_all = rows_most(hi_all);
     int start = lo_all >= hi_all ? 0 : lo_all / kKeys * kKeys, end = lo_all >= hi_all ? 0 : hi_all;
     if (PARTS && !own) {
         // chunks of the planned length, or longer ones where the sequence is longer than was planned for
@@ -204,48 +225,71 @@ __global__ void __launch_bounds__(kAttendThreads, (Shape<T, DP>::waves(RT))) k_a
     any = any || start < end;
     int tile = start + (WK == 4 && !own ? wave * kKeys : 0);
 
-    // The place of a run of keys: page_size is a multiple of a run, and so is where a tile starts.  Runs behind the last key take
-    // the last one's place, so that nothing is read outside pages that hold keys; their scores are masked.
-    auto run_place = [&](int t, int run) {
-        const int key = min(t + run * kRun, (end - 1) / kRun * kRun);
-        return place_of(p.map, sequence, key);
+    // The places of a tile's four runs of keys: page_size is a multiple of a run, and so is where a tile starts.  Runs behind the last key
+    // take the last one's place, so that nothing is read outside pages that hold keys; their scores are masked.  All of it is the same for
+    // the whole wave and goes through scalar loads, which do not queue behind the keys and values on their way.
+    struct Pages { int page[4]; };
+    const ConstTable row_table = reinterpret_cast<ConstTable>(reinterpret_cast<uintptr_t>(p.map.table + sequence * p.map.table_stride));
+    auto run_key = [&](int t, int r) { return min(t + r * kRun, (end - 1) / kRun * kRun); };
+    auto pages_of = [&](int t) {                              // as they stand in the table: nothing waits for them here
+        Pages at;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) at.page[r] = row_table[p.map.page.div(run_key(t, r))];
+        return at;
+    };
+    auto run_of = [&](const Pages &at, int t, int run) {
+        int page[4], slot[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int key = run_key(t, r);
+            page[r] = static_cast<uint32_t>(at.page[r]) < static_cast<uint32_t>(p.map.pages) ? at.page[r] : -1;
+            slot[r] = p.map.page.mod(key, p.map.page.div(key));
+        }
+        const bool odd = run & 1, upper = run & 2;
+        const int p0 = odd ? page[1] : page[0], p1 = odd ? page[3] : page[2];
+        const int s0 = odd ? slot[1] : slot[0], s1 = odd ? slot[3] : slot[2];
+        return Place{upper ? p1 : p0, upper ? s1 : s0};
     };
     U4 kf[kHalves][kSteps];
     uint32_t vf[kRun][kGroups][kWords];
-    auto load_keys = [&](Place at) {
+    // (`there` false: the loads go to one line and nobody uses them.  They are issued all the same, or the waits for what was loaded
+    // before them would have to allow for their absence and wait for everything.)
+    auto load_keys = [&](Place at, bool there) {
 #pragma unroll
         for (int h = 0; h < kHalves; ++h) {
-            const T *src = kb + max(at.page, 0) * static_cast<int64_t>(p.k_page_stride) +
-                           (at.slot + 4 * h + in_run) * static_cast<int64_t>(p.k_token_stride);
+            const int64_t off = max(at.page, 0) * static_cast<int64_t>(p.k_page_stride) + (at.slot + 4 * h + in_run) * static_cast<int64_t>(p.k_token_stride);
+            const T *src = kb + (there ? off : 0);
 #pragma unroll
             for (int i = 0; i < kSteps; ++i) {
                 const int e = (4 * i + quad) * S::kPiece;
-                if (4 * i * S::kPiece >= p.head_dim) continue;                       // uniform
                 kf[h][i] = *reinterpret_cast<const U4 *>(src + (e < p.head_dim ? e : 0));
             }
         }
     };
-    auto load_values = [&](Place at) {
-        const T *src = vb + max(at.page, 0) * static_cast<int64_t>(p.v_page_stride) + at.slot * static_cast<int64_t>(p.v_token_stride);
+    auto load_values = [&](Place at, bool there) {
+        const int64_t off = max(at.page, 0) * static_cast<int64_t>(p.v_page_stride) + at.slot * static_cast<int64_t>(p.v_token_stride);
+        const T *src = vb + (there ? off : 0);
+        const int64_t next_key = there ? p.v_token_stride : 0;
 #pragma unroll
         for (int k = 0; k < kRun; ++k)
 #pragma unroll
             for (int g = 0; g < kGroups; ++g) {
                 const int e = (g * 16 + col) * kVec;
                 struct alignas(4 * kWords) Words { uint32_t w[kWords]; };
-                const Words v = *reinterpret_cast<const Words *>(src + k * static_cast<int64_t>(p.v_token_stride) + (e < p.head_dim ? e : 0));
+                const Words v = *reinterpret_cast<const Words *>(src + k * next_key + (e < p.head_dim ? e : 0));
 #pragma unroll
                 for (int w = 0; w < kWords; ++w) vf[k][g][w] = v.w[w];
             }
     };
 
-    Place next_k{-1, 0}, next_v{-1, 0}, here_v{-1, 0};
+    Pages next{};
+    Place here_v{-1, 0};
     if (tile < end) {
-        const Place a = run_place(tile, run_k);
-        here_v = run_place(tile, quad);
-        load_keys(a);
-        load_values(here_v);
-        if (tile + step < end) { next_k = run_place(tile + step, run_k); next_v = run_place(tile + step, quad); }
+        const Pages at = pages_of(tile);
+        here_v = run_of(at, tile, quad);
+        load_keys(run_of(at, tile, run_k), true);
+        load_values(here_v, true);
+        next = pages_of(tile + step);                         // (behind the end: the last run's page)
     }
     for (; tile < end; tile += step) {
         // scores: keys x rows
@@ -277,11 +321,11 @@ __global__ void __launch_bounds__(kAttendThreads, (Shape<T, DP>::waves(RT))) k_a
                 }
         const Place cur_v = here_v;
         const bool more = tile + step < end;
-        if (more) {
-            load_keys(next_k);
-            here_v = next_v;
-            if (tile + 2 * step < end) { next_k = run_place(tile + 2 * step, run_k); next_v = run_place(tile + 2 * step, quad); }
-        }
+        __builtin_amdgcn_sched_barrier(0);
+        load_keys(run_of(next, tile + step, run_k), more);
+        here_v = run_of(next, tile + step, quad);
+        next = pages_of(tile + 2 * step);
+        __builtin_amdgcn_sched_barrier(0);
 
         // weights
         const bool lost = cur_v.page < 0;
@@ -292,13 +336,10 @@ __global__ void __launch_bounds__(kAttendThreads, (Shape<T, DP>::waves(RT))) k_a
             seen[r] = (1u << kRun) - 1;
             if (partial) {
                 const int base = tile + quad * kRun;
-                seen[r] = 0;
+                const int from = max(row_low[r] - base, 0), to = lost ? 0 : min(max(row_high[r] - base, 0), kRun);
+                seen[r] = from < to ? ((1u << to) - 1) & ~((1u << from) - 1) : 0u;
 #pragma unroll
-                for (int k = 0; k < kRun; ++k)
-                    if (!lost && base + k >= row_low[r] && base + k < row_high[r]) seen[r] |= 1u << k;
-#pragma unroll
-                for (int k = 0; k < kRun; ++k)
-                    if (!(seen[r] >> k & 1)) s[r][k / 4][k % 4] = -INFINITY;
+                for (int k = 0; k < kRun; ++k) s[r][k / 4][k % 4] = seen[r] >> k & 1 ? s[r][k / 4][k % 4] : -INFINITY;
             }
             float top = s[r][0][0];
 #pragma unroll
@@ -327,20 +368,16 @@ __global__ void __launch_bounds__(kAttendThreads, (Shape<T, DP>::waves(RT))) k_a
         bool odd = false;
         if (partial) {
             const int base = tile + quad * kRun;
+            uint32_t bad = 0;
 #pragma unroll
-            for (int k = 0; k < kRun; ++k)
-                if (lost || base + k < lo_all || base + k >= hi_all)
-#pragma unroll
-                    for (int g = 0; g < kGroups; ++g)
-#pragma unroll
-                        for (int w = 0; w < kWords; ++w) vf[k][g][w] = 0;
-#pragma unroll
-            for (int k = 0; k < kRun; ++k)
+            for (int k = 0; k < kRun; ++k) {
+                const uint32_t keep = lost | (base + k < lo_all) | (base + k >= hi_all) ? 0u : 0xFFFFFFFFu;
 #pragma unroll
                 for (int g = 0; g < kGroups; ++g)
 #pragma unroll
-                    for (int w = 0; w < kWords; ++w) odd = odd || not_finite<T>(vf[k][g][w]);
-            odd = __any(odd);
+                    for (int w = 0; w < kWords; ++w) { vf[k][g][w] &= keep; bad |= exponents_full<T>(vf[k][g][w]); }
+            }
+            odd = __any(bad != 0);
         }
         if (odd) {
 #pragma unroll 1
@@ -421,7 +458,7 @@ __global__ void __launch_bounds__(kAttendThreads, (Shape<T, DP>::waves(RT))) k_a
                         for (int k = 0; k < kRun; ++k)
                             acc[r][g * kVec + j] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(vf[k][g][j]), s[r][0][k], acc[r][g * kVec + j], 0, 0, 0);
         }
-        if (more) load_values(here_v);
+        load_values(here_v, more);
     }
     }
 #pragma unroll
@@ -591,6 +628,11 @@ hipError_t launch_one(AttendProblem p, hipStream_t stream)
     const int rows = p.tokens * p.group * p.drafts, per = 16 * RT * (WK == 4 ? 1 : 4);
     p.row_blocks = (rows + per - 1) / per;
     p.items = p.sequences / p.drafts * p.kv_heads * (PARTS ? p.parts : 1);
+    p.by_blocks = Divider::of(p.row_blocks);
+    p.by_kv_heads = Divider::of(p.kv_heads);
+    p.by_parts = Divider::of(PARTS ? p.parts : 1);
+    p.by_in_draft = Divider::of(p.tokens * p.group);
+    p.by_group = Divider::of(p.group);
     const int64_t grid = p.row_blocks == 1 ? p.items : static_cast<int64_t>((p.items + 7) / 8 * 8) * p.row_blocks;
     if (grid > INT32_MAX) return hipErrorInvalidConfiguration;
     hipLaunchKernelGGL((k_attend<T, DP, RT, WK, PARTS>), dim3(static_cast<unsigned>(grid)), dim3(kAttendThreads), 0, stream, p);

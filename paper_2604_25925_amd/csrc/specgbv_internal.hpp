@@ -181,7 +181,8 @@ struct AttendProblem {
     int sequences, tokens, heads, kv_heads, group, head_dim, drafts, window;
     int parts, chunks, chunk_keys; // 0 parts: one pass without partial sums; else the chunks and, with drafts, their own keys
     int q_wide, out_wide;          // 16-byte loads of q, stores of whole vectors to out
-    int items, row_blocks;         // set by the launches
+    int items, row_blocks;         // set by the launches, with what divides block and row numbers
+    Divider by_blocks, by_kv_heads, by_parts, by_in_draft, by_group;
 };
 struct AttendPlan { int parts, chunks, chunk_keys; size_t ml_bytes, bytes; };
 AttendPlan plan_attend(int sequences, int drafts, bool shared, int tokens, int heads, int kv_heads, int head_dim, int window,
