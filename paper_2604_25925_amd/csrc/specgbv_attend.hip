@@ -17,7 +17,11 @@
 // contraction over head_dim is free, so lanes take 16-byte pieces of keys.  Neither the keys nor the values pass through LDS,
 // and no barrier stands in the loop.
 //
-// WK = 4: the waves of a workgroup take the tiles in turn and join at the end through LDS; 1: each wave has rows of its own.
+// WK = 4: the waves of a workgroup take the tiles in turn and join at the end through LDS; 1: each wave has rows of its own, and the
+// waves share the tiles, which come into LDS by asynchronous loads two tiles ahead.  Straight into registers each 16-byte piece of a key is
+// a line of its own for the cache (16 neighbouring lanes hold 16 rows), 750 accesses a tile, which bounded it with many rows; through LDS
+// neighbouring lanes load neighbouring pieces, once for four waves.  In LDS piece n of key m lies in slot n ^ m, so that 8 lanes that read one
+// piece of 8 keys meet 8 groups of banks.
 #include "specgbv_internal.hpp"
 
 namespace specgbv {
@@ -88,14 +92,34 @@ template <typename T> __device__ __forceinline__ bool is_kind(uint32_t e, int ki
     return kind == 0 ? (e & ~sign) > inf : e == (kind == 1 ? inf : (inf | sign));
 }
 
+// Asynchronous 16-byte load per lane into LDS bytes [dst + 16 lane, ...), dst the same for the wave; it counts as a vector load.
+// (In assembly because the compiler makes every later wait one for all loads once it sees such a load itself.)
+__device__ __forceinline__ void load_to_lds(const void *src, uint32_t dst)
+{
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(src), "s"(dst) : "memory", "m0");
+}
+template <int N> __device__ __forceinline__ void wait_for_loads() { asm volatile("s_waitcnt vmcnt(%0)" : : "n"(N) : "memory"); }
+
+// A barrier that waits for nothing but the waves, and that no access to memory is moved across.
+__device__ __forceinline__ void meet()
+{
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
 template <typename T, int DP, int RT, int WK, bool PARTS>
 __global__ void __launch_bounds__(kAttendThreads, (Shape<T, DP>::waves(RT))) k_attend(AttendProblem p)
 {
     using S = Shape<T, DP>;
     constexpr int kKeys = S::kKeys, kRun = S::kRun, kHalves = S::kHalves, kSteps = S::kSteps, kVec = S::kVec, kGroups = S::kGroups,
                   kCols = S::kCols, kWords = kVec * sizeof(T) / 4;
-    __shared__ F4 sh_acc[WK == 4 ? RT * DP * 16 : 1];         // [4 waves][RT][kGroups][4][kVec / 4][64]
+    // WK = 4: sums to be joined, [4 waves][RT][kGroups][4][kVec / 4][64]; 1: the tiles, [3][keys, values][kKeys][DP]
+    constexpr int kPieces = DP / S::kPiece, kHalfTile = kKeys * DP * static_cast<int>(sizeof(T)), kStages = 3;
+    constexpr int kFills = kKeys * kPieces / kAttendThreads;  // of a wave, for the keys and again for the values
+    __shared__ F4 sh_acc[WK == 4 ? RT * DP * 16 : kStages * 2 * kHalfTile / 16];
     __shared__ float sh_m[kWavesPerGroup][RT * 16], sh_l[kWavesPerGroup][RT * 16];
+    __shared__ int sh_range[8];
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = lane & 15, quad = lane >> 4;
@@ -195,6 +219,10 @@ __global__ void __launch_bounds__(kAttendThreads, (Shape<T, DP>::waves(RT))) k_a
     bool any = own;                                           // something may have been summed
 #pragma unroll 1
     for (int seg = own && WK == 4 ? wave : 0; seg < (own ? p.drafts : 1); seg += own && WK == 4 ? 4 : 1) {
+    if (WK == 1 && own) {                                     // drafts without rows in this workgroup
+        const int row = block * 64 * RT, last = min(row + 64 * RT, rows) - 1;
+        if (seg < p.by_in_draft.div(row) || seg > p.by_in_draft.div(last)) continue;
+    }
     const int sequence = first + seg;
     int row_low[RT], row_high[RT];
     int lo_all = INT32_MAX, lo_most = -1, hi_all = 0, hi_least = INT32_MAX;
@@ -213,6 +241,14 @@ __global__ void __launch_bounds__(kAttendThreads, (Shape<T, DP>::waves(RT))) k_a
     }
     lo_all = rows_least(lo_all); hi_least = rows_least(hi_least);
     lo_most = rows_most(lo_most); hi_all = rows_most(hi_all);
+    const bool active = lo_all < hi_all;                      // this wave has rows that see something
+    if (WK == 1) {
+        __syncthreads();                                      // (and nobody reads the tiles of what was before any longer)
+        if (lane == 0) { sh_range[wave] = lo_all; sh_range[4 + wave] = hi_all; }
+        __syncthreads();
+        lo_all = __builtin_amdgcn_readfirstlane(min(min(sh_range[0], sh_range[1]), min(sh_range[2], sh_range[3])));
+        hi_all = __builtin_amdgcn_readfirstlane(max(max(sh_range[4], sh_range[5]), max(sh_range[6], sh_range[7])));
+    }
     int start = lo_all >= hi_all ? 0 : lo_all / kKeys * kKeys, end = lo_all >= hi_all ? 0 : hi_all;
     if (PARTS && !own) {
         // chunks of the planned length, or longer ones where the sequence is longer than was planned for
@@ -282,16 +318,90 @@ __global__ void __launch_bounds__(kAttendThreads, (Shape<T, DP>::waves(RT))) k_a
             }
     };
 
+    // the tile at t into stage `to` of LDS, by all waves
+    auto fill = [&](const Pages &at, int t, int to) {
+        const uint32_t base = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(sh_acc)) + to * 2 * kHalfTile;
+#pragma unroll
+        for (int n = 0; n < kFills; ++n) {
+            const int unit = (wave * kFills + n) * 64 + lane, row = unit / kPieces, slot = unit % kPieces, run = row / kRun;
+            const Place x = run_of(at, t, run);
+            const int64_t page = max(x.page, 0);
+            const int in_page = x.slot + row % kRun;
+            const int of_key = S::kBf ? row >> 3 << 2 | (row & 3) : row;                   // its row in the product
+            const int e = (slot ^ (of_key & (kPieces < 16 ? kPieces - 1 : 15))) * S::kPiece, ev = slot * S::kPiece;
+            load_to_lds(kb + page * p.k_page_stride + in_page * static_cast<int64_t>(p.k_token_stride) + (e < p.head_dim ? e : 0),
+                        base + (wave * kFills + n) * 1024);
+            load_to_lds(vb + page * p.v_page_stride + in_page * static_cast<int64_t>(p.v_token_stride) + (ev < p.head_dim ? ev : 0),
+                        base + kHalfTile + (wave * kFills + n) * 1024);
+        }
+    };
+    auto missing = [&](const Pages &at) {                     // bits: which runs' pages are not there
+        uint32_t m = 0;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) m |= static_cast<uint32_t>(at.page[r]) < static_cast<uint32_t>(p.map.pages) ? 0u : 1u << r;
+        return m;
+    };
+    auto read_keys = [&](int from) {
+        const char *base = reinterpret_cast<const char *>(sh_acc) + from * 2 * kHalfTile;
+#pragma unroll
+        for (int h = 0; h < kHalves; ++h)
+#pragma unroll
+            for (int i = 0; i < kSteps; ++i) {
+                const int slot = (4 * i + quad) ^ (col & (kPieces < 16 ? kPieces - 1 : 15));
+                kf[h][i] = *reinterpret_cast<const U4 *>(base + ((run_k * kRun + 4 * h + in_run) * kPieces + slot) * 16);
+            }
+    };
+    auto read_values = [&](int from) {
+        const char *base = reinterpret_cast<const char *>(sh_acc) + from * 2 * kHalfTile + kHalfTile;
+#pragma unroll
+        for (int k = 0; k < kRun; ++k)
+#pragma unroll
+            for (int g = 0; g < kGroups; ++g) {
+                struct alignas(4 * kWords) Words { uint32_t w[kWords]; };
+                const Words v = *reinterpret_cast<const Words *>(base + ((quad * kRun + k) * DP + (g * 16 + col) * kVec) * static_cast<int>(sizeof(T)));
+#pragma unroll
+                for (int w = 0; w < kWords; ++w) vf[k][g][w] = v.w[w];
+            }
+    };
+
     Pages next{};
     Place here_v{-1, 0};
+    int stage = 0;                                            // of the tile at hand
+    uint32_t lost_now = 0, lost_then = 0;                     // WK = 1: runs without a page, of this tile and of the next one
     if (tile < end) {
         const Pages at = pages_of(tile);
-        here_v = run_of(at, tile, quad);
-        load_keys(run_of(at, tile, run_k), true);
-        load_values(here_v, true);
-        next = pages_of(tile + step);                         // (behind the end: the last run's page)
+        if constexpr (WK == 4) {
+            here_v = run_of(at, tile, quad);
+            load_keys(run_of(at, tile, run_k), true);
+            load_values(here_v, true);
+            next = pages_of(tile + step);                     // (behind the end: the last run's page)
+        } else {
+            const Pages second = pages_of(tile + step);
+            next = pages_of(tile + 2 * step);
+            fill(at, tile, 0);
+            if (tile + step < end) fill(second, tile + step, 1);
+            lost_now = missing(at);
+            lost_then = missing(second);
+        }
     }
     for (; tile < end; tile += step) {
+        const bool more = tile + step < end;
+        const int here = stage;
+        uint32_t lost_runs = 0;
+        if constexpr (WK == 1) {
+            if (more) wait_for_loads<2 * kFills>();           // this tile is there, the next one may be on its way
+            else wait_for_loads<0>();
+            meet();                                           // for all waves, and nobody reads the tile before it any longer
+            stage = stage == kStages - 1 ? 0 : stage + 1;
+            lost_runs = lost_now; lost_now = lost_then;
+            if (tile + 2 * step < end) {
+                fill(next, tile + 2 * step, stage == kStages - 1 ? 0 : stage + 1);
+                lost_then = missing(next);
+                next = pages_of(tile + 3 * step);
+            }
+            if (!active) continue;                            // uniform
+            read_keys(here);
+        }
         // scores: keys x rows
         F4 s[RT][kHalves];
 #pragma unroll
@@ -320,16 +430,17 @@ __global__ void __launch_bounds__(kAttendThreads, (Shape<T, DP>::waves(RT))) k_a
                     }
                 }
         const Place cur_v = here_v;
-        const bool more = tile + step < end;
-        __builtin_amdgcn_sched_barrier(0);
-        load_keys(run_of(next, tile + step, run_k), more);
-        here_v = run_of(next, tile + step, quad);
-        next = pages_of(tile + 2 * step);
-        __builtin_amdgcn_sched_barrier(0);
+        if constexpr (WK == 4) {
+            __builtin_amdgcn_sched_barrier(0);
+            load_keys(run_of(next, tile + step, run_k), more);
+            here_v = run_of(next, tile + step, quad);
+            next = pages_of(tile + 2 * step);
+            __builtin_amdgcn_sched_barrier(0);
+        } else read_values(here);
 
         // weights
-        const bool lost = cur_v.page < 0;
-        const bool partial = tile < lo_most || tile + kKeys > hi_least || tile + kKeys > end || __any(lost);
+        const bool lost = WK == 4 ? cur_v.page < 0 : (lost_runs >> quad & 1) != 0;
+        const bool partial = tile < lo_most || tile + kKeys > hi_least || tile + kKeys > end || (WK == 4 ? __any(lost) : lost_runs != 0);
         uint32_t seen[RT];                                    // bits: which of the lane's keys its row sees
 #pragma unroll
         for (int r = 0; r < RT; ++r) {
@@ -458,7 +569,7 @@ __global__ void __launch_bounds__(kAttendThreads, (Shape<T, DP>::waves(RT))) k_a
                         for (int k = 0; k < kRun; ++k)
                             acc[r][g * kVec + j] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(vf[k][g][j]), s[r][0][k], acc[r][g * kVec + j], 0, 0, 0);
         }
-        load_values(here_v, more);
+        if constexpr (WK == 4) load_values(here_v, more);
     }
     }
 #pragma unroll
