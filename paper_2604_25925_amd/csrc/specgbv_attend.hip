@@ -1,10 +1,10 @@
 // Attention of new queries over a paged cache, split over the cache's length and joined.
 //
-//   out = sum_j w_j v_j / sum_j w_j,   w_j = 2^(c (<q, k_j> - m)),   c = scale log2(e),
+//   out = sum_j w_j v_j / sum_j w_j,   w_j = 2^(c <q, k_j> - m),   c = scale log2(e),
 // in one pass over the keys with a running reference m per query (any m gives the same quotient; it is raised, and what has been
-// summed is scaled, only where a weight would exceed 2^8, so that tiles after the first few seldom pay for it).  m is subtracted from
-// the product before c is applied: c <q, k> - c m in one operation would leave the rounding of c m, which is vast where all scores lie
-// near the type's lowest value.
+// summed is scaled, only where a weight would exceed 2^8, so that tiles after the first few seldom pay for it).  One operation gives
+// c <q, k> - m; what the rounding of m leaves out is a factor of all weights, but a vast one where scores lie near the type's lowest
+// value, so there (|m| > 2^20) the product is rounded before m is taken off.
 //
 // Rows.  A kv head's queries of one sequence (tokens x heads of its group), or of all drafts of a prefix while the keys lie in pages
 // that the drafts share, are the rows of a matrix product: one read of a key serves them all.  A wave holds 16 RT rows.
@@ -44,9 +44,10 @@ template <typename T, int DP> struct Shape {
     static constexpr int kGroups = DP / (16 * kVec);         // such vectors per key
     static constexpr int kCols = kGroups * kVec;             // result tiles of 16 entries
     // waves per SIMD that the registers of a tile, its rows and their sums leave room for
-    static constexpr int waves(int RT) { return DP == 256 || (!kBf && DP == 128 && RT == 2) ? 1 : (kBf && DP == 128 && RT == 1 ? 3 : 2); }
+    static constexpr int waves(int RT) { return DP == 256 || (!kBf && DP == 128 && RT == 2) ? 1 : 2; }
 };
 
+constexpr float kRaise = 8.0f;                // a reference is raised where a score is this far above it
 constexpr int kMaxParts = 256;                // partial sums of a row at most: a workgroup's threads
 
 template <typename T> __device__ __forceinline__ T rounded(float x);
@@ -92,11 +93,23 @@ template <typename T> __device__ __forceinline__ bool is_kind(uint32_t e, int ki
     return kind == 0 ? (e & ~sign) > inf : e == (kind == 1 ? inf : (inf | sign));
 }
 
+// Four entries of a result, over the sum of weights (inv 0: there is none, and the result is 0).
+template <typename T> __device__ __forceinline__ void store_entries(T *dst, F4 v, float inv, int wide)
+{
+    struct alignas(4 * sizeof(T)) Vec { T e[4]; } o;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) o.e[j] = rounded<T>(inv == 0.0f ? 0.0f : v[j] * inv);
+    if (wide) *reinterpret_cast<Vec *>(dst) = o;
+    else
+#pragma unroll
+        for (int j = 0; j < 4; ++j) dst[j] = o.e[j];
+}
+
 // Asynchronous 16-byte load per lane into LDS bytes [dst + 16 lane, ...), dst the same for the wave; it counts as a vector load.
 // (In assembly because the compiler makes every later wait one for all loads once it sees such a load itself.)
-__device__ __forceinline__ void load_to_lds(const void *src, uint32_t dst)
+__device__ __forceinline__ void load_to_lds(const void *base, uint32_t byte_offset, uint32_t dst)
 {
-    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(src), "s"(dst) : "memory", "m0");
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(byte_offset), "s"(base), "s"(dst) : "memory", "m0");
 }
 template <int N> __device__ __forceinline__ void wait_for_loads() { asm volatile("s_waitcnt vmcnt(%0)" : : "n"(N) : "memory"); }
 
@@ -216,7 +229,21 @@ __global__ void __launch_bounds__(kAttendThreads, (Shape<T, DP>::waves(RT))) k_a
     const T *vb = static_cast<const T *>(p.v) + head0 * static_cast<int64_t>(p.v_head_stride);
     const int run_k = col >> 2, in_run = col & 3;
     const int step = WK == 4 && !own ? 4 * kKeys : kKeys;
+    constexpr bool kTurned = S::kBf && WK == 1;               // values come out of LDS turned: entry 16 c + col of the lane's run of keys
+    // WK = 1: which bytes of a run this lane brings to LDS, [n]: row (n 64 + lane) / kPieces of the run, piece ^ what spreads the banks
+    uint32_t fill_k[WK == 1 ? kFills : 1], fill_v[WK == 1 ? kFills : 1];
+    if constexpr (WK == 1) {
+#pragma unroll
+        for (int n = 0; n < kFills; ++n) {
+            const int unit = (wave * kFills + n) * 64 + lane, row = unit / kPieces, slot = unit % kPieces;
+            const int of_key = S::kBf ? row >> 3 << 2 | (row & 3) : row;                   // its row in the product
+            const int e = (slot ^ (of_key & (kPieces < 16 ? kPieces - 1 : 15))) * S::kPiece, ev = (kTurned ? slot ^ (row & 3) << 1 : slot) * S::kPiece;
+            fill_k[n] = static_cast<uint32_t>(row % kRun * p.k_token_stride + (e < p.head_dim ? e : 0)) * static_cast<uint32_t>(sizeof(T));
+            fill_v[n] = static_cast<uint32_t>(row % kRun * p.v_token_stride + (ev < p.head_dim ? ev : 0)) * static_cast<uint32_t>(sizeof(T));
+        }
+    }
     bool any = own;                                           // something may have been summed
+    bool vast = false;                                        // a row of this wave has a reference beyond 2^20
 #pragma unroll 1
     for (int seg = own && WK == 4 ? wave : 0; seg < (own ? p.drafts : 1); seg += own && WK == 4 ? 4 : 1) {
     if (WK == 1 && own) {                                     // drafts without rows in this workgroup
@@ -318,21 +345,19 @@ __global__ void __launch_bounds__(kAttendThreads, (Shape<T, DP>::waves(RT))) k_a
             }
     };
 
-    // the tile at t into stage `to` of LDS, by all waves
+    // the tile at t into stage `to` of LDS: a run of keys by each wave, so that what differs between the lanes stays the same for all tiles
     auto fill = [&](const Pages &at, int t, int to) {
-        const uint32_t base = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(sh_acc)) + to * 2 * kHalfTile;
+        const int key = run_key(t, wave);
+        const int a0 = at.page[0], a1 = at.page[1], a2 = at.page[2], a3 = at.page[3];
+        const int lower = wave & 1 ? a1 : a0, upper = wave & 1 ? a3 : a2, own_page = __builtin_amdgcn_readfirstlane(wave & 2 ? upper : lower);
+        const int64_t page = static_cast<uint32_t>(own_page) < static_cast<uint32_t>(p.map.pages) ? own_page : 0;
+        const int64_t slot = p.map.page.mod(key, p.map.page.div(key));
+        const T *keys = kb + page * p.k_page_stride + slot * p.k_token_stride, *values = vb + page * p.v_page_stride + slot * p.v_token_stride;
+        const uint32_t base = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(sh_acc)) + to * 2 * kHalfTile + wave * kFills * 1024;
 #pragma unroll
         for (int n = 0; n < kFills; ++n) {
-            const int unit = (wave * kFills + n) * 64 + lane, row = unit / kPieces, slot = unit % kPieces, run = row / kRun;
-            const Place x = run_of(at, t, run);
-            const int64_t page = max(x.page, 0);
-            const int in_page = x.slot + row % kRun;
-            const int of_key = S::kBf ? row >> 3 << 2 | (row & 3) : row;                   // its row in the product
-            const int e = (slot ^ (of_key & (kPieces < 16 ? kPieces - 1 : 15))) * S::kPiece, ev = slot * S::kPiece;
-            load_to_lds(kb + page * p.k_page_stride + in_page * static_cast<int64_t>(p.k_token_stride) + (e < p.head_dim ? e : 0),
-                        base + (wave * kFills + n) * 1024);
-            load_to_lds(vb + page * p.v_page_stride + in_page * static_cast<int64_t>(p.v_token_stride) + (ev < p.head_dim ? ev : 0),
-                        base + kHalfTile + (wave * kFills + n) * 1024);
+            load_to_lds(keys, fill_k[n], base + n * 1024);
+            load_to_lds(values, fill_v[n], base + kHalfTile + n * 1024);
         }
     };
     auto missing = [&](const Pages &at) {                     // bits: which runs' pages are not there
@@ -351,17 +376,53 @@ __global__ void __launch_bounds__(kAttendThreads, (Shape<T, DP>::waves(RT))) k_a
                 kf[h][i] = *reinterpret_cast<const U4 *>(base + ((run_k * kRun + 4 * h + in_run) * kPieces + slot) * 16);
             }
     };
+    U4 va[kTurned ? kCols : 1];                               // kTurned: eight keys' entries 16 c + col
     auto read_values = [&](int from) {
         const char *base = reinterpret_cast<const char *>(sh_acc) + from * 2 * kHalfTile + kHalfTile;
+        if constexpr (kTurned) {
+            // 16 lanes read 4 keys of 16 entries, four entries each, and get one entry of the 4 keys each
+            typedef short S4 __attribute__((ext_vector_type(4)));
+            typedef S4 __attribute__((address_space(3))) *Turn;
+            const int spread = col >> 2;
+            const char *mine = base + (quad * kRun + spread) * DP * 2 + (col & 3) * 8;
 #pragma unroll
-        for (int k = 0; k < kRun; ++k)
-#pragma unroll
-            for (int g = 0; g < kGroups; ++g) {
-                struct alignas(4 * kWords) Words { uint32_t w[kWords]; };
-                const Words v = *reinterpret_cast<const Words *>(base + ((quad * kRun + k) * DP + (g * 16 + col) * kVec) * static_cast<int>(sizeof(T)));
-#pragma unroll
-                for (int w = 0; w < kWords; ++w) vf[k][g][w] = v.w[w];
+            for (int c = 0; c < kCols; ++c) {
+                const char *at = mine + ((c & 3) ^ spread) * 32 + (c & ~3) * 32;
+                const S4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Turn)(uint32_t)(uintptr_t)at);
+                const S4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Turn)(uint32_t)(uintptr_t)(at + 4 * DP * 2));
+                __builtin_memcpy(&va[c].x, &lo, 8);
+                __builtin_memcpy(&va[c].z, &hi, 8);
             }
+        } else {
+#pragma unroll
+            for (int k = 0; k < kRun; ++k)
+#pragma unroll
+                for (int g = 0; g < kGroups; ++g) {
+                    struct alignas(4 * kWords) Words { uint32_t w[kWords]; };
+                    const Words v = *reinterpret_cast<const Words *>(base + ((quad * kRun + k) * DP + (g * 16 + col) * kVec) * static_cast<int>(sizeof(T)));
+#pragma unroll
+                    for (int w = 0; w < kWords; ++w) vf[k][g][w] = v.w[w];
+                }
+        }
+    };
+    // bfloat16: one entry of the lane's eight keys, the left operand of the second product
+    auto entry_of = [&](int c) {
+        if constexpr (kTurned) return va[c];
+        else {
+            const int g = c / kVec, j = c % kVec;
+            uint32_t w[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) w[k] = __builtin_amdgcn_perm(vf[2 * k + 1][g][j / 2], vf[2 * k][g][j / 2], j % 2 ? 0x07060302u : 0x05040100u);
+            return U4{w[0], w[1], w[2], w[3]};
+        }
+    };
+    auto without_odd = [](uint32_t x) {                       // entries that are not finite made 0
+        if (S::kBf) {
+            if ((x & 0x7F80u) == 0x7F80u) x &= 0xFFFF0000u;
+            if ((x & 0x7F800000u) == 0x7F800000u) x &= 0x0000FFFFu;
+            return x;
+        }
+        return (x & 0x7F800000u) == 0x7F800000u ? 0u : x;
     };
 
     Pages next{};
@@ -455,23 +516,32 @@ __global__ void __launch_bounds__(kAttendThreads, (Shape<T, DP>::waves(RT))) k_a
             float top = s[r][0][0];
 #pragma unroll
             for (int k = 1; k < kRun; ++k) top = fmaxf(top, s[r][k / 4][k % 4]);
-            if (__any(top > ref[r] + p.raise)) {
+            top *= p.c;
+            if (__any(top > ref[r] + kRaise)) {
                 // (row by row: what a row gets does not hang on the rows next to it)
                 top = row_largest(top);
-                const float now = top > ref[r] + p.raise ? top : ref[r];
-                const float f = now == ref[r] ? 1.0f : exp2_of((ref[r] - now) * p.c);        // (-inf to -inf: nothing summed yet)
+                const float now = top > ref[r] + kRaise ? top : ref[r];
+                const float f = now == ref[r] ? 1.0f : exp2_of(ref[r] - now);        // (-inf to -inf: nothing summed yet)
+                vast = vast || __any(fabsf(now) > 1048576.0f && now != -INFINITY);
                 ref[r] = now;
                 sum[r] *= f;
 #pragma unroll
                 for (int c = 0; c < kCols; ++c) acc[r][c] *= f;
             }
             const float m = ref[r] == -INFINITY ? 0.0f : ref[r];
+            if (vast) {
 #pragma unroll
-            for (int k = 0; k < kRun; ++k) {
-                const float w = exp2_of((s[r][k / 4][k % 4] - m) * p.c);
-                s[r][k / 4][k % 4] = w;
-                sum[r] += w;
+                for (int k = 0; k < kRun; ++k) {
+                    float x = s[r][k / 4][k % 4] * p.c;
+                    asm volatile("" : "+v"(x));                // (rounded by itself)
+                    s[r][k / 4][k % 4] = exp2_of(x - m);
+                }
+            } else {
+#pragma unroll
+                for (int k = 0; k < kRun; ++k) s[r][k / 4][k % 4] = exp2_of(fmaf(s[r][k / 4][k % 4], p.c, -m));
             }
+#pragma unroll
+            for (int k = 0; k < kRun; ++k) sum[r] += s[r][k / 4][k % 4];
         }
 
         // values that some rows do not see: a weight of 0 does not take out what is not finite.  Keys that no row sees are cleared;
@@ -479,14 +549,26 @@ __global__ void __launch_bounds__(kAttendThreads, (Shape<T, DP>::waves(RT))) k_a
         bool odd = false;
         if (partial) {
             const int base = tile + quad * kRun;
-            uint32_t bad = 0;
+            uint32_t bad = 0, keep[kRun];
 #pragma unroll
-            for (int k = 0; k < kRun; ++k) {
-                const uint32_t keep = lost | (base + k < lo_all) | (base + k >= hi_all) ? 0u : 0xFFFFFFFFu;
+            for (int k = 0; k < kRun; ++k) keep[k] = lost | (base + k < lo_all) | (base + k >= hi_all) ? 0u : 0xFFFFFFFFu;
+            if constexpr (kTurned) {
 #pragma unroll
-                for (int g = 0; g < kGroups; ++g)
+                for (int c = 0; c < kCols; ++c) {
+                    uint32_t *w = &va[c].x;
 #pragma unroll
-                    for (int w = 0; w < kWords; ++w) { vf[k][g][w] &= keep; bad |= exponents_full<T>(vf[k][g][w]); }
+                    for (int k = 0; k < 4; ++k) {
+                        w[k] &= (keep[2 * k] & 0xFFFFu) | (keep[2 * k + 1] & 0xFFFF0000u);
+                        bad |= exponents_full<T>(w[k]);
+                    }
+                }
+            } else {
+#pragma unroll
+                for (int k = 0; k < kRun; ++k)
+#pragma unroll
+                    for (int g = 0; g < kGroups; ++g)
+#pragma unroll
+                        for (int w = 0; w < kWords; ++w) { vf[k][g][w] &= keep[k]; bad |= exponents_full<T>(vf[k][g][w]); }
             }
             odd = __any(bad != 0);
         }
@@ -495,47 +577,39 @@ __global__ void __launch_bounds__(kAttendThreads, (Shape<T, DP>::waves(RT))) k_a
             for (int kind = 0; kind < 3; ++kind) {
                 const float what = kind == 0 ? NAN : (kind == 1 ? INFINITY : -INFINITY);
 #pragma unroll
-                for (int g = 0; g < kGroups; ++g)
+                for (int c = 0; c < kCols; ++c) {
+                    uint32_t e[kRun];
+                    if constexpr (S::kBf) {
+                        const U4 x = entry_of(c);
+                        const uint32_t *w = &x.x;
 #pragma unroll
-                    for (int j = 0; j < kVec; ++j) {
-                        uint32_t e[kRun];
+                        for (int k = 0; k < kRun; ++k) e[k] = w[k / 2] >> (k % 2 * 16) & 0xFFFFu;
+                    } else {
 #pragma unroll
-                        for (int k = 0; k < kRun; ++k)
-                            e[k] = S::kBf ? (vf[k][g][j * sizeof(T) / 4] >> (j % 2 * 16)) & 0xFFFFu : vf[k][g][j * sizeof(T) / 4];
+                        for (int k = 0; k < kRun; ++k) e[k] = vf[k][c / kVec][c % kVec];
+                    }
 #pragma unroll
-                        for (int r = 0; r < RT; ++r) {
-                            F4 n{0, 0, 0, 0};
-                            if constexpr (S::kBf) {
-                                B8 a, b;
+                    for (int r = 0; r < RT; ++r) {
+                        F4 n{0, 0, 0, 0};
+                        if constexpr (S::kBf) {
+                            B8 a, b;
 #pragma unroll
-                                for (int k = 0; k < kRun; ++k) {
-                                    a[k] = static_cast<__bf16>(is_kind<T>(e[k], kind) ? 1.0f : 0.0f);
-                                    b[k] = static_cast<__bf16>(seen[r] >> k & 1 ? 1.0f : 0.0f);
-                                }
-                                n = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, n, 0, 0, 0);
-                            } else {
-#pragma unroll
-                                for (int k = 0; k < kRun; ++k)
-                                    n = __builtin_amdgcn_mfma_f32_16x16x4f32(is_kind<T>(e[k], kind) ? 1.0f : 0.0f, seen[r] >> k & 1 ? 1.0f : 0.0f, n, 0, 0, 0);
+                            for (int k = 0; k < kRun; ++k) {
+                                a[k] = static_cast<__bf16>(is_kind<T>(e[k], kind) ? 1.0f : 0.0f);
+                                b[k] = static_cast<__bf16>(seen[r] >> k & 1 ? 1.0f : 0.0f);
                             }
+                            n = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, n, 0, 0, 0);
+                        } else {
 #pragma unroll
-                            for (int i = 0; i < 4; ++i)
-                                if (n[i] > 0.0f) acc[r][g * kVec + j][i] += what;
+                            for (int k = 0; k < kRun; ++k)
+                                n = __builtin_amdgcn_mfma_f32_16x16x4f32(is_kind<T>(e[k], kind) ? 1.0f : 0.0f, seen[r] >> k & 1 ? 1.0f : 0.0f, n, 0, 0, 0);
                         }
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            if (n[i] > 0.0f) acc[r][c][i] += what;
                     }
+                }
             }
-#pragma unroll
-            for (int k = 0; k < kRun; ++k)
-#pragma unroll
-                for (int g = 0; g < kGroups; ++g)
-#pragma unroll
-                    for (int w = 0; w < kWords; ++w) {
-                        uint32_t &x = vf[k][g][w];
-                        if (S::kBf) {
-                            if ((x & 0x7F80u) == 0x7F80u) x &= 0xFFFF0000u;
-                            if ((x & 0x7F800000u) == 0x7F800000u) x &= 0x0000FFFFu;
-                        } else if ((x & 0x7F800000u) == 0x7F800000u) x = 0;
-                    }
         }
 
         // sums of values: entries x rows
@@ -546,28 +620,28 @@ __global__ void __launch_bounds__(kAttendThreads, (Shape<T, DP>::waves(RT))) k_a
 #pragma unroll
                 for (int k = 0; k < kRun; ++k) w[r][k] = static_cast<__bf16>(s[r][k / 4][k % 4]);
 #pragma unroll
-            for (int g = 0; g < kGroups; ++g)
+            for (int c = 0; c < kCols; ++c) {
+                U4 a = entry_of(c);
+                if (odd) a = U4{without_odd(a.x), without_odd(a.y), without_odd(a.z), without_odd(a.w)};       // uniform
 #pragma unroll
-                for (int j = 0; j < kVec; ++j) {
-                    U4 a;
-                    uint32_t *aw = &a.x;
-#pragma unroll
-                    for (int k = 0; k < 4; ++k)
-                        aw[k] = __builtin_amdgcn_perm(vf[2 * k + 1][g][j / 2], vf[2 * k][g][j / 2], j % 2 ? 0x07060302u : 0x05040100u);
-#pragma unroll
-                    for (int r = 0; r < RT; ++r)
-                        acc[r][g * kVec + j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(B8, a), w[r], acc[r][g * kVec + j], 0, 0, 0);
-                }
+                for (int r = 0; r < RT; ++r) acc[r][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(B8, a), w[r], acc[r][c], 0, 0, 0);
+            }
         } else {
+            if (odd) {
 #pragma unroll
-            for (int g = 0; g < kGroups; ++g)
+                for (int k = 0; k < kRun; ++k)
 #pragma unroll
-                for (int j = 0; j < kVec; ++j)
+                    for (int g = 0; g < kGroups; ++g)
 #pragma unroll
-                    for (int r = 0; r < RT; ++r)
+                        for (int w = 0; w < kWords; ++w) vf[k][g][w] = without_odd(vf[k][g][w]);
+            }
 #pragma unroll
-                        for (int k = 0; k < kRun; ++k)
-                            acc[r][g * kVec + j] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(vf[k][g][j]), s[r][0][k], acc[r][g * kVec + j], 0, 0, 0);
+            for (int c = 0; c < kCols; ++c)
+#pragma unroll
+                for (int r = 0; r < RT; ++r)
+#pragma unroll
+                    for (int k = 0; k < kRun; ++k)
+                        acc[r][c] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(vf[k][c / kVec][c % kVec]), s[r][0][k], acc[r][c], 0, 0, 0);
         }
         if constexpr (WK == 4) load_values(here_v, more);
     }
@@ -589,9 +663,9 @@ __global__ void __launch_bounds__(kAttendThreads, (Shape<T, DP>::waves(RT))) k_a
 #pragma unroll
             for (int w = 0; w < 4; ++w) {
                 const float m = sh_m[w][r * 16 + col];
-                total += sh_l[w][r * 16 + col] * (m == most ? 1.0f : exp2_of((m - most) * p.c));
+                total += sh_l[w][r * 16 + col] * (m == most ? 1.0f : exp2_of(m - most));
             }
-            const float f = ref[r] == most ? 1.0f : exp2_of((ref[r] - most) * p.c);
+            const float f = ref[r] == most ? 1.0f : exp2_of(ref[r] - most);
             ref[r] = most; sum[r] = total;
 #pragma unroll
             for (int g = 0; g < kGroups; ++g)
@@ -610,18 +684,27 @@ __global__ void __launch_bounds__(kAttendThreads, (Shape<T, DP>::waves(RT))) k_a
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
         if (row0 + r * 16 + col >= rows) continue;
-        // Partial sums are held in the order in which lanes hold them: vector ((g 4 + i) kVec / 4 + n) 4 + quad of a row are entries
-        // (16 g + 4 quad + i) kVec + 4 n + 0..3.  Where nothing was summed they are not written: the sum of weights says so.
+        // Partial sums are held in the order in which lanes hold them: in order (kTurned), or vector ((g 4 + i) kVec / 4 + n) 4 + quad of
+        // a row are entries (16 g + 4 quad + i) kVec + 4 n + 0..3.  Where nothing was summed they are not written: the sum of weights says so.
         const float inv = sum[r] != 0.0f ? 1.0f / sum[r] : 0.0f;
         const int64_t at = PARTS ? ((static_cast<int64_t>(unit) * p.kv_heads + head0) * p.parts + part) * rows + row0 + r * 16 + col : 0;
         if (PARTS && (WK == 1 || wave == 0) && quad == 0) p.ml[at] = make_float2(ref[r], sum[r]);
         if (PARTS && !any) continue;
+        if constexpr (kTurned) {                              // result c of a lane is entries 16 c + 4 quad + 0..3
+#pragma unroll
+            for (int c = 0; c < kCols; ++c) {
+                const int d = 16 * c + 4 * quad;
+                if (PARTS) reinterpret_cast<F4 *>(p.acc + at * DP)[d / 4] = acc[r][c];
+                else if (d < p.head_dim) store_entries(static_cast<T *>(p.out) + out_at[r] + d, acc[r][c], pos[r] < 0 ? 0.0f : inv, p.out_wide);
+            }
+            continue;
+        }
 #pragma unroll
         for (int g = 0; g < kGroups; ++g)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 if (WK == 4 && i != wave) continue;
-                float x[kVec];
+                const int d = (16 * g + 4 * quad + i) * kVec;
 #pragma unroll
                 for (int n = 0; n < kVec / 4; ++n) {
                     F4 v{0, 0, 0, 0};
@@ -633,19 +716,8 @@ __global__ void __launch_bounds__(kAttendThreads, (Shape<T, DP>::waves(RT))) k_a
                         for (int e = 0; e < 4; ++e) v[e] = acc[r][g * kVec + 4 * n + e][i];
                     }
                     if (PARTS) reinterpret_cast<F4 *>(p.acc + at * DP)[((g * 4 + i) * (kVec / 4) + n) * 4 + quad] = v;
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) x[4 * n + e] = v[e];
-                }
-                const int d = (16 * g + 4 * quad + i) * kVec;
-                if (!PARTS && d < p.head_dim) {
-                    T *dst = static_cast<T *>(p.out) + out_at[r] + d;
-                    struct alignas(kVec * sizeof(T)) Vec { T e[kVec]; } o;
-#pragma unroll
-                    for (int j = 0; j < kVec; ++j) o.e[j] = rounded<T>(pos[r] < 0 || sum[r] == 0.0f ? 0.0f : x[j] * inv);
-                    if (p.out_wide) *reinterpret_cast<Vec *>(dst) = o;
-                    else
-#pragma unroll
-                        for (int j = 0; j < kVec; ++j) dst[j] = o.e[j];
+                    else if (d + 4 * n < p.head_dim)
+                        store_entries(static_cast<T *>(p.out) + out_at[r] + d + 4 * n, v, pos[r] < 0 ? 0.0f : inv, p.out_wide);
                 }
             }
     }
@@ -687,7 +759,7 @@ __global__ void __launch_bounds__(kAttendThreads) k_attend_join(AttendProblem p)
         __syncthreads();
         most = fmaxf(fmaxf(sh_most[0], sh_most[1]), fmaxf(sh_most[2], sh_most[3]));
     }
-    const float f = !some ? 0.0f : (ml.x == most ? 1.0f : exp2_of((ml.x - most) * p.c));
+    const float f = !some ? 0.0f : (ml.x == most ? 1.0f : exp2_of(ml.x - most));
     float total = some ? ml.y * f : 0.0f;
     for (int m = 32; m > 0; m >>= 1) total += __shfl_xor(total, m, 64);
     if (WAVES > 1) {
@@ -720,17 +792,10 @@ __global__ void __launch_bounds__(kAttendThreads) k_attend_join(AttendProblem p)
         acc = (sh_acc[vec] + sh_acc[kLanes + vec]) + (sh_acc[2 * kLanes + vec] + sh_acc[3 * kLanes + vec]);
     } else if (set != 0) return;
     const int quad = vec & 3, piece = vec >> 2, n = piece % (kVec / 4), gi = piece / (kVec / 4), i = gi & 3, g = gi >> 2;
-    const int d = (16 * g + 4 * quad + i) * kVec + 4 * n;
+    const int d = p.in_order ? 4 * vec : (16 * g + 4 * quad + i) * kVec + 4 * n;
     if (d >= p.head_dim) return;
-    T *dst = static_cast<T *>(p.out) + s * p.out_stride[0] + t * p.out_stride[1] + h * p.out_stride[2] + d;
     const float inv = pos >= 0 && total != 0.0f ? 1.0f / total : 0.0f;
-    struct alignas(4 * sizeof(T)) Vec { T e[4]; } o;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) o.e[e] = rounded<T>(inv == 0.0f ? 0.0f : acc[e] * inv);
-    if (p.out_wide) *reinterpret_cast<Vec *>(dst) = o;
-    else
-#pragma unroll
-        for (int e = 0; e < 4; ++e) dst[e] = o.e[e];
+    store_entries(static_cast<T *>(p.out) + s * p.out_stride[0] + t * p.out_stride[1] + h * p.out_stride[2] + d, acc, inv, p.out_wide);
 }
 
 template <typename T, int DP, int RT, int WK, bool PARTS>
@@ -750,23 +815,26 @@ hipError_t launch_one(AttendProblem p, hipStream_t stream)
     return hipGetLastError();
 }
 
+constexpr int kFewRows = 64;                  // up to here the waves of a workgroup share the rows, beyond they share the keys
+
 template <typename T, int DP, bool PARTS>
 hipError_t launch_rows(const AttendProblem &p, hipStream_t stream)
 {
     const int rows = p.tokens * p.group * p.drafts;
     if (rows <= 16) return launch_one<T, DP, 1, 4, PARTS>(p, stream);
     if constexpr (DP < 256) {
-        if (rows <= 64) return launch_one<T, DP, 2, 4, PARTS>(p, stream);
+        if (rows <= kFewRows) return launch_one<T, DP, 2, 4, PARTS>(p, stream);
         return launch_one<T, DP, 2, 1, PARTS>(p, stream);
     } else {
-        if (rows <= 32) return launch_one<T, DP, 1, 4, PARTS>(p, stream);
+        if (rows <= kFewRows) return launch_one<T, DP, 1, 4, PARTS>(p, stream);
         return launch_one<T, DP, 1, 1, PARTS>(p, stream);
     }
 }
 
 template <typename T, int DP>
-hipError_t launch_typed(const AttendProblem &p, hipStream_t stream)
+hipError_t launch_typed(AttendProblem p, hipStream_t stream)
 {
+    p.in_order = Shape<T, DP>::kBf && p.tokens * p.group * p.drafts > kFewRows;
     if (p.parts == 0) return launch_rows<T, DP, false>(p, stream);
     const hipError_t e = launch_rows<T, DP, true>(p, stream);
     if (e != hipSuccess) return e;

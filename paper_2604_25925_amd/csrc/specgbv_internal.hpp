@@ -177,11 +177,11 @@ struct AttendProblem {
     float2 *ml;                    // [units][kv_heads][parts][rows] reference and sum of a part; unit: sequence, or prefix with its drafts
     float *acc;                    // the same, with the sums of values
     float c;                       // scale * log2(e)
-    float raise;                   // a reference is raised where a score exceeds it by this: weights stay below 2^8
     int sequences, tokens, heads, kv_heads, group, head_dim, drafts, window;
     int parts, chunks, chunk_keys; // 0 parts: one pass without partial sums; else the chunks and, with drafts, their own keys
     int q_wide, out_wide;          // 16-byte loads of q, stores of whole vectors to out
     int items, row_blocks;         // set by the launches, with what divides block and row numbers
+    int in_order;                  // partial sums are held in the entries' order
     Divider by_blocks, by_kv_heads, by_parts, by_in_draft, by_group;
 };
 struct AttendPlan { int parts, chunks, chunk_keys; size_t ml_bytes, bytes; };

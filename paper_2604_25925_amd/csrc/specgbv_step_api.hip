@@ -30,6 +30,8 @@ static specgbv_status check_cache(const specgbv_paged_cache *c, bool pointers)
         if (s % unit) return fail(SPECGBV_EUNSUPPORTED, "the cache's strides are not whole 16 bytes");
         if (s > INT32_MAX) return fail(SPECGBV_EUNSUPPORTED, "a stride of the cache exceeds 2^31 - 1 entries");
     }
+    if (c->k_token_stride > (1 << 26) || c->v_token_stride > (1 << 26))
+        return fail(SPECGBV_EUNSUPPORTED, "tokens of the cache lie more than 2^26 entries apart");
     if (pointers) {
         if (!c->k || !c->v || !c->table) return fail(SPECGBV_EINVAL, "null pointer in the cache");
         if (!aligned(c->k, 16) || !aligned(c->v, 16)) return fail(SPECGBV_EUNSUPPORTED, "the cache is not 16-byte aligned");
@@ -187,7 +189,6 @@ specgbv_status specgbv_attend_paged(const specgbv_paged_cache *cache, const spec
     p.ml = static_cast<float2 *>(workspace);
     p.acc = reinterpret_cast<float *>(static_cast<char *>(workspace) + plan.ml_bytes);
     p.c = static_cast<float>((a.scale > 0.0f ? static_cast<double>(a.scale) : 1.0 / std::sqrt(static_cast<double>(c.head_dim))) * 1.4426950408889634074);
-    p.raise = 8.0f / p.c;
     p.sequences = c.sequences; p.tokens = a.tokens; p.heads = a.heads; p.kv_heads = c.kv_heads; p.group = a.heads / c.kv_heads;
     p.head_dim = c.head_dim; p.drafts = a.prefixes > 0 ? c.sequences / a.prefixes : 1; p.window = a.window;
     p.parts = plan.parts; p.chunks = plan.chunks; p.chunk_keys = plan.chunk_keys;
