@@ -346,11 +346,9 @@ __global__ void __launch_bounds__(kAttendThreads, (Shape<T, DP>::waves(RT))) k_a
     };
 
     // the tile at t into stage `to` of LDS: a run of keys by each wave, so that what differs between the lanes stays the same for all tiles
-    auto fill = [&](const Pages &at, int t, int to) {
+    auto fill = [&](int table_page, int t, int to) {
         const int key = run_key(t, wave);
-        const int a0 = at.page[0], a1 = at.page[1], a2 = at.page[2], a3 = at.page[3];
-        const int lower = wave & 1 ? a1 : a0, upper = wave & 1 ? a3 : a2, own_page = __builtin_amdgcn_readfirstlane(wave & 2 ? upper : lower);
-        const int64_t page = static_cast<uint32_t>(own_page) < static_cast<uint32_t>(p.map.pages) ? own_page : 0;
+        const int64_t page = static_cast<uint32_t>(table_page) < static_cast<uint32_t>(p.map.pages) ? table_page : 0;
         const int64_t slot = p.map.page.mod(key, p.map.page.div(key));
         const T *keys = kb + page * p.k_page_stride + slot * p.k_token_stride, *values = vb + page * p.v_page_stride + slot * p.v_token_stride;
         const uint32_t base = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(sh_acc)) + to * 2 * kHalfTile + wave * kFills * 1024;
@@ -360,12 +358,7 @@ __global__ void __launch_bounds__(kAttendThreads, (Shape<T, DP>::waves(RT))) k_a
             load_to_lds(values, fill_v[n], base + kHalfTile + n * 1024);
         }
     };
-    auto missing = [&](const Pages &at) {                     // bits: which runs' pages are not there
-        uint32_t m = 0;
-#pragma unroll
-        for (int r = 0; r < 4; ++r) m |= static_cast<uint32_t>(at.page[r]) < static_cast<uint32_t>(p.map.pages) ? 0u : 1u << r;
-        return m;
-    };
+    auto own_page = [&](int t) { return row_table[p.map.page.div(run_key(t, wave))]; };
     auto read_keys = [&](int from) {
         const char *base = reinterpret_cast<const char *>(sh_acc) + from * 2 * kHalfTile;
 #pragma unroll
@@ -428,40 +421,42 @@ __global__ void __launch_bounds__(kAttendThreads, (Shape<T, DP>::waves(RT))) k_a
     Pages next{};
     Place here_v{-1, 0};
     int stage = 0;                                            // of the tile at hand
-    uint32_t lost_now = 0, lost_then = 0;                     // WK = 1: runs without a page, of this tile and of the next one
+    int next_page = 0;                                        // WK = 1: of this wave's run two tiles on
+    bool bad_pages = false;                                   // WK = 1: some page between start and end is not there
     if (tile < end) {
-        const Pages at = pages_of(tile);
         if constexpr (WK == 4) {
+            const Pages at = pages_of(tile);
             here_v = run_of(at, tile, quad);
             load_keys(run_of(at, tile, run_k), true);
             load_values(here_v, true);
             next = pages_of(tile + step);                     // (behind the end: the last run's page)
         } else {
-            const Pages second = pages_of(tile + step);
-            next = pages_of(tile + 2 * step);
-            fill(at, tile, 0);
+            const int second = own_page(tile + step);
+            fill(own_page(tile), tile, 0);
             if (tile + step < end) fill(second, tile + step, 1);
-            lost_now = missing(at);
-            lost_then = missing(second);
+            next_page = own_page(tile + 2 * step);
+            uint32_t bad = 0;
+            for (int n = p.map.page.div(start) + lane, last = p.map.page.div(end - 1); n <= last; n += 64)
+                bad |= static_cast<uint32_t>(p.map.table[sequence * p.map.table_stride + n]) < static_cast<uint32_t>(p.map.pages) ? 0u : 1u;
+            bad_pages = __any(bad != 0);
         }
     }
     for (; tile < end; tile += step) {
         const bool more = tile + step < end;
         const int here = stage;
-        uint32_t lost_runs = 0;
+        bool lost_here = false;                               // WK = 1: the lane's run has no page
         if constexpr (WK == 1) {
             if (more) wait_for_loads<2 * kFills>();           // this tile is there, the next one may be on its way
             else wait_for_loads<0>();
             meet();                                           // for all waves, and nobody reads the tile before it any longer
             stage = stage == kStages - 1 ? 0 : stage + 1;
-            lost_runs = lost_now; lost_now = lost_then;
             if (tile + 2 * step < end) {
-                fill(next, tile + 2 * step, stage == kStages - 1 ? 0 : stage + 1);
-                lost_then = missing(next);
-                next = pages_of(tile + 3 * step);
+                fill(next_page, tile + 2 * step, stage == kStages - 1 ? 0 : stage + 1);
+                next_page = own_page(tile + 3 * step);
             }
             if (!active) continue;                            // uniform
             read_keys(here);
+            if (bad_pages) lost_here = run_of(pages_of(tile), tile, quad).page < 0;
         }
         // scores: keys x rows
         F4 s[RT][kHalves];
@@ -470,9 +465,11 @@ __global__ void __launch_bounds__(kAttendThreads, (Shape<T, DP>::waves(RT))) k_a
 #pragma unroll
             for (int h = 0; h < kHalves; ++h) s[r][h] = F4{0, 0, 0, 0};
         if (p.head_dim != DP) {
+            int mine = quad;
+            asm volatile("" : "+v"(mine));                    // (the comparisons stay here: kept over the loop they cost scalar registers)
 #pragma unroll
             for (int i = 0; i < kSteps; ++i)
-                if ((4 * i + quad) * S::kPiece >= p.head_dim)
+                if ((4 * i + mine) * S::kPiece >= p.head_dim)
 #pragma unroll
                     for (int h = 0; h < kHalves; ++h) kf[h][i] = U4{0, 0, 0, 0};
         }
@@ -500,8 +497,8 @@ __global__ void __launch_bounds__(kAttendThreads, (Shape<T, DP>::waves(RT))) k_a
         } else read_values(here);
 
         // weights
-        const bool lost = WK == 4 ? cur_v.page < 0 : (lost_runs >> quad & 1) != 0;
-        const bool partial = tile < lo_most || tile + kKeys > hi_least || tile + kKeys > end || (WK == 4 ? __any(lost) : lost_runs != 0);
+        const bool lost = WK == 4 ? cur_v.page < 0 : lost_here;
+        const bool partial = tile < lo_most || tile + kKeys > hi_least || tile + kKeys > end || (WK == 4 ? __any(lost) : bad_pages);
         uint32_t seen[RT];                                    // bits: which of the lane's keys its row sees
 #pragma unroll
         for (int r = 0; r < RT; ++r) {
