@@ -48,6 +48,7 @@ template <typename T, int DP> struct Shape {
 };
 
 constexpr float kRaise = 8.0f;                // a reference is raised where a score is this far above it
+constexpr int kFewRows = 64;                  // up to here the waves of a workgroup share the rows, beyond they share the keys
 constexpr int kMaxParts = 256;                // partial sums of a row at most: a workgroup's threads
 
 template <typename T> __device__ __forceinline__ T rounded(float x);
@@ -91,6 +92,44 @@ template <typename T> __device__ __forceinline__ bool is_kind(uint32_t e, int ki
 {
     constexpr uint32_t inf = sizeof(T) == 2 ? 0x7F80u : 0x7F800000u, sign = sizeof(T) == 2 ? 0x8000u : 0x80000000u;
     return kind == 0 ? (e & ~sign) > inf : e == (kind == 1 ? inf : (inf | sign));
+}
+
+// Which part of which unit (a sequence, or a prefix with its drafts) a workgroup has, and how many parts the unit is in.
+struct Share { int unit, part, parts, at, length; };          // at: place of the unit's first part among all; length: keys of a part
+
+// Units differ in length, and a launch lasts as long as its last workgroup.  So every workgroup looks at all units' lengths (one a lane)
+// and takes its part of a division into equal lengths, the shortest for which all workgroups fit onto the card at once.  With more units
+// than lanes each is cut into the same number of parts.
+__device__ __forceinline__ Share share_of(const AttendProblem &p, int index, int held, int lane)
+{
+    if (!p.balanced) {
+        const int unit = p.by_chunks.div(index);
+        if (unit >= p.units) return Share{-1, 0, 0, 0, 0};
+        return Share{unit, p.by_chunks.mod(index, unit), p.chunks, unit * p.chunks, p.chunk_keys};
+    }
+    int length = 0;
+    if (lane < p.units) {
+        if (p.shared_len) length = max(0, min(p.shared_len[lane], held));
+        else
+            for (int t = 0; t < p.tokens; ++t) length = max(length, min(p.positions[lane * p.positions_stride + t], held - 1) + 1);
+        if (p.window > 0) length = min(length, min(p.window, held) + p.tokens);
+        length = max(length + p.own_keys, 1);
+    }
+    const double all = wave_sum(static_cast<double>(length));
+    int part = static_cast<int>(all / p.most_parts) / p.grain * p.grain + p.grain;            // at most most_parts + units parts
+    part = max(part, p.chunk_keys);
+    uint32_t n = 0, run = 0;
+    for (int i = 0; i < 8; ++i) {
+        n = (static_cast<uint32_t>(length) + static_cast<uint32_t>(part) - 1u) / static_cast<uint32_t>(part);
+        run = wave_inclusive_count(n);
+        if (__builtin_amdgcn_readlane(run, 63) <= static_cast<uint32_t>(p.most_parts)) break;
+        part += (part / 8 + p.grain - 1) / p.grain * p.grain;
+    }
+    const unsigned long long above = __ballot(run > static_cast<uint32_t>(index));
+    if (above == 0) return Share{-1, 0, 0, 0, 0};
+    const int unit = __ffsll(static_cast<long long>(above)) - 1;
+    const int parts = __builtin_amdgcn_readlane(n, unit), at = __builtin_amdgcn_readlane(run, unit) - parts;
+    return Share{unit, index - at, parts, at, part};
 }
 
 // Four entries of a result, over the sum of weights (inv 0: there is none, and the result is 0).
@@ -146,30 +185,28 @@ __global__ void __launch_bounds__(kAttendThreads, (Shape<T, DP>::waves(RT))) k_a
         if (item >= p.items) return;
     }
     const int rest = p.by_kv_heads.div(item), head0 = p.by_kv_heads.mod(item, rest);
-    const int unit = PARTS ? p.by_parts.div(rest) : rest, part = PARTS ? p.by_parts.mod(rest, unit) : 0;
-    const bool own = PARTS && p.shared_len && part == p.chunks;       // the drafts' own keys, behind the shared ones
+    const int held = static_cast<int>(capacity_of(p.map));
+    Share share{rest, 0, 1, rest, 0};
+    if (PARTS) {
+        share = share_of(p, rest, held, lane);
+        if (share.unit < 0) return;                           // (the same for the whole workgroup)
+        if (share.part == 0 && head0 == 0 && block == 0 && threadIdx.x == 0) p.places[share.unit] = make_int2(share.at, share.parts);
+    }
+    const int unit = share.unit, part = share.part;
+    const bool last_part = PARTS && p.shared_len && part == share.parts - 1;           // takes the drafts' own keys, behind the shared ones, too
     const int first = unit * p.drafts;                        // its first sequence
     const int in_draft = p.tokens * p.group, rows = in_draft * p.drafts;
-    const int row0 = (block * (WK == 4 ? 1 : 4) + (WK == 4 ? 0 : wave)) * 16 * RT;
+    const int row0 = block * p.block_rows + (WK == 4 ? 0 : wave * 16 * RT);
+    const int row_end = min(rows, (block + 1) * p.block_rows);
 
-    const int held = static_cast<int>(capacity_of(p.map));
     const int shared = p.shared_len ? max(0, min(p.shared_len[unit], held)) : held;
-
-    // Nothing is left for this part where the planned chunks in front of it cover all that the drafts share.
-    if (PARTS && !own && p.shared_len && part > 0 && static_cast<int64_t>(part) * p.chunk_keys >= shared) {
-        for (int i = threadIdx.x; i < 16 * RT * (WK == 4 ? 1 : 4); i += kAttendThreads) {
-            const int row = block * 16 * RT * (WK == 4 ? 1 : 4) + i;
-            if (row < rows) p.ml[((static_cast<int64_t>(unit) * p.kv_heads + head0) * p.parts + part) * rows + row] = make_float2(-INFINITY, 0.0f);
-        }
-        return;
-    }
 
     // Rows behind the last one take its place (their loads are those of the last row) and are nowhere stored.
     int64_t q_at[RT], out_at[RT];
     int pos[RT], draft[RT];
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
-        const int row = min(row0 + r * 16 + col, rows - 1);
+        const int row = min(row0 + r * 16 + col, row_end - 1);
         draft[r] = p.by_in_draft.div(row);
         const int in = p.by_in_draft.mod(row, draft[r]), t = p.by_group.div(in), head = head0 * p.group + p.by_group.mod(in, t), s = first + draft[r];
         pos[r] = p.positions[s * p.positions_stride + t];
@@ -213,7 +250,7 @@ __global__ void __launch_bounds__(kAttendThreads, (Shape<T, DP>::waves(RT))) k_a
     }
 #pragma unroll
     for (int r = 0; r < RT; ++r)
-        if (row0 + r * 16 + col >= rows) pos[r] = -1;
+        if (row0 + r * 16 + col >= row_end) pos[r] = -1;
 
     F4 acc[RT][kCols];
     float ref[RT], sum[RT];                                   // sum: over the lane's own keys
@@ -228,7 +265,6 @@ __global__ void __launch_bounds__(kAttendThreads, (Shape<T, DP>::waves(RT))) k_a
     const T *kb = static_cast<const T *>(p.k) + head0 * static_cast<int64_t>(p.k_head_stride);
     const T *vb = static_cast<const T *>(p.v) + head0 * static_cast<int64_t>(p.v_head_stride);
     const int run_k = col >> 2, in_run = col & 3;
-    const int step = WK == 4 && !own ? 4 * kKeys : kKeys;
     constexpr bool kTurned = S::kBf && WK == 1;               // values come out of LDS turned: entry 16 c + col of the lane's run of keys
     // WK = 1: which bytes of a run this lane brings to LDS, [n]: row (n 64 + lane) / kPieces of the run, piece ^ what spreads the banks
     uint32_t fill_k[WK == 1 ? kFills : 1], fill_v[WK == 1 ? kFills : 1];
@@ -242,15 +278,17 @@ __global__ void __launch_bounds__(kAttendThreads, (Shape<T, DP>::waves(RT))) k_a
             fill_v[n] = static_cast<uint32_t>(row % kRun * p.v_token_stride + (ev < p.head_dim ? ev : 0)) * static_cast<uint32_t>(sizeof(T));
         }
     }
-    bool any = own;                                           // something may have been summed
+    bool any = last_part;                                     // something may have been summed
     bool vast = false;                                        // a row of this wave has a reference beyond 2^20
 #pragma unroll 1
-    for (int seg = own && WK == 4 ? wave : 0; seg < (own ? p.drafts : 1); seg += own && WK == 4 ? 4 : 1) {
+    for (int seg = -1; seg < (last_part ? p.drafts : 0); seg = WK == 1 ? seg + 1 : (seg < 0 ? wave : seg + 4)) {
+    const bool own = seg >= 0;                                // -1: what the unit's sequences share
     if (WK == 1 && own) {                                     // drafts without rows in this workgroup
-        const int row = block * 64 * RT, last = min(row + 64 * RT, rows) - 1;
+        const int row = block * p.block_rows, last = min(row + p.block_rows, rows) - 1;
         if (seg < p.by_in_draft.div(row) || seg > p.by_in_draft.div(last)) continue;
     }
-    const int sequence = first + seg;
+    const int step = WK == 4 && !own ? 4 * kKeys : kKeys;
+    const int sequence = first + max(seg, 0);
     int row_low[RT], row_high[RT];
     int lo_all = INT32_MAX, lo_most = -1, hi_all = 0, hi_least = INT32_MAX;
 #pragma unroll
@@ -278,9 +316,9 @@ __global__ void __launch_bounds__(kAttendThreads, (Shape<T, DP>::waves(RT))) k_a
     }
     int start = lo_all >= hi_all ? 0 : lo_all / kKeys * kKeys, end = lo_all >= hi_all ? 0 : hi_all;
     if (PARTS && !own) {
-        // chunks of the planned length, or longer ones where the sequence is longer than was planned for
-        const int span = end - start, least = (span + p.chunks - 1) / p.chunks;
-        const int length = max(p.chunk_keys, (least + kKeys - 1) / kKeys * kKeys);
+        // parts of the planned length, or longer ones where the sequence is longer than was planned for
+        const int span = end - start, least = (span + share.parts - 1) / share.parts;
+        const int length = max(share.length, (least + kKeys - 1) / kKeys * kKeys);
         const int64_t at = start + static_cast<int64_t>(part) * length;
         start = static_cast<int>(min(at, static_cast<int64_t>(end)));
         end = static_cast<int>(min(at + length, static_cast<int64_t>(end)));
@@ -680,11 +718,11 @@ __global__ void __launch_bounds__(kAttendThreads, (Shape<T, DP>::waves(RT))) k_a
     }
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
-        if (row0 + r * 16 + col >= rows) continue;
+        if (row0 + r * 16 + col >= row_end) continue;
         // Partial sums are held in the order in which lanes hold them: in order (kTurned), or vector ((g 4 + i) kVec / 4 + n) 4 + quad of
         // a row are entries (16 g + 4 quad + i) kVec + 4 n + 0..3.  Where nothing was summed they are not written: the sum of weights says so.
         const float inv = sum[r] != 0.0f ? 1.0f / sum[r] : 0.0f;
-        const int64_t at = PARTS ? ((static_cast<int64_t>(unit) * p.kv_heads + head0) * p.parts + part) * rows + row0 + r * 16 + col : 0;
+        const int64_t at = PARTS ? (static_cast<int64_t>(share.at + part) * p.kv_heads + head0) * rows + row0 + r * 16 + col : 0;
         if (PARTS && (WK == 1 || wave == 0) && quad == 0) p.ml[at] = make_float2(ref[r], sum[r]);
         if (PARTS && !any) continue;
         if constexpr (kTurned) {                              // result c of a lane is entries 16 c + 4 quad + 0..3
@@ -738,15 +776,17 @@ __global__ void __launch_bounds__(kAttendThreads) k_attend_join(AttendProblem p)
     const int row = static_cast<int>(at - pair * rows);
     const int unit = static_cast<int>(pair / p.kv_heads), head0 = static_cast<int>(pair - static_cast<int64_t>(unit) * p.kv_heads);
     const int draft = row / in_draft, in = row - draft * in_draft, s = unit * p.drafts + draft, t = in / p.group, h = head0 * p.group + in - t * p.group;
-    const int64_t part0 = pair * p.parts * rows + row;
+    int2 mine_at = p.balanced ? p.places[unit] : make_int2(unit * p.chunks, p.chunks);
+    const int parts = mine_at.y;
+    const int64_t part0 = (static_cast<int64_t>(mine_at.x) * p.kv_heads + head0) * rows + row, between = static_cast<int64_t>(p.kv_heads) * rows;
 
     // the first parts' sums are on their way while the weights of all parts are looked at
     F4 v[kAhead];
 #pragma unroll
     for (int i = 0; i < kAhead; ++i)
-        v[i] = reinterpret_cast<const F4 *>(p.acc + (part0 + static_cast<int64_t>(min(set + i * kSets, p.parts - 1)) * rows) * DP)[vec];
+        v[i] = reinterpret_cast<const F4 *>(p.acc + (part0 + static_cast<int64_t>(min(set + i * kSets, parts - 1)) * between) * DP)[vec];
     float2 ml{-INFINITY, 0.0f};
-    if (tid < p.parts) ml = p.ml[part0 + static_cast<int64_t>(tid) * rows];          // (parts are at most the threads of a row)
+    if (tid < parts) ml = p.ml[part0 + static_cast<int64_t>(tid) * between];          // (parts are at most the threads of a row)
     const int pos = p.positions[s * p.positions_stride + t];
     const bool some = ml.y != 0.0f;                                                   // (a sum that is no number goes on)
     float most = some ? ml.x : -INFINITY;
@@ -767,15 +807,15 @@ __global__ void __launch_bounds__(kAttendThreads) k_attend_join(AttendProblem p)
     }
     const float mine = some ? f : -1.0f;
     F4 acc{0, 0, 0, 0};
-    for (int c0 = set; c0 - set < p.parts; c0 += kAhead * kSets) {                    // the same count for all
+    for (int c0 = set; c0 - set < parts; c0 += kAhead * kSets) {                    // the same count for all
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) {
             const int c = c0 + i * kSets;
-            const float w = c >= p.parts ? -1.0f : (WAVES > 1 ? sh_f[c] : __shfl(mine, c, 64));
+            const float w = c >= parts ? -1.0f : (WAVES > 1 ? sh_f[c] : __shfl(mine, c, 64));
 #pragma unroll
             for (int e = 0; e < 4; ++e) acc[e] += w < 0.0f ? 0.0f : v[i][e] * w;
             const int n = c + kAhead * kSets;
-            if (n < p.parts) v[i] = reinterpret_cast<const F4 *>(p.acc + (part0 + static_cast<int64_t>(n) * rows) * DP)[vec];
+            if (n < parts) v[i] = reinterpret_cast<const F4 *>(p.acc + (part0 + static_cast<int64_t>(n) * between) * DP)[vec];
         }
     }
 #pragma unroll
@@ -798,46 +838,34 @@ __global__ void __launch_bounds__(kAttendThreads) k_attend_join(AttendProblem p)
 template <typename T, int DP, int RT, int WK, bool PARTS>
 hipError_t launch_one(AttendProblem p, hipStream_t stream)
 {
-    const int rows = p.tokens * p.group * p.drafts, per = 16 * RT * (WK == 4 ? 1 : 4);
-    p.row_blocks = (rows + per - 1) / per;
-    p.items = p.sequences / p.drafts * p.kv_heads * (PARTS ? p.parts : 1);
+    p.items = p.all_parts * p.kv_heads;
     p.by_blocks = Divider::of(p.row_blocks);
-    p.by_kv_heads = Divider::of(p.kv_heads);
-    p.by_parts = Divider::of(PARTS ? p.parts : 1);
-    p.by_in_draft = Divider::of(p.tokens * p.group);
-    p.by_group = Divider::of(p.group);
     const int64_t grid = p.row_blocks == 1 ? p.items : static_cast<int64_t>((p.items + 7) / 8 * 8) * p.row_blocks;
     if (grid > INT32_MAX) return hipErrorInvalidConfiguration;
     hipLaunchKernelGGL((k_attend<T, DP, RT, WK, PARTS>), dim3(static_cast<unsigned>(grid)), dim3(kAttendThreads), 0, stream, p);
     return hipGetLastError();
 }
 
-constexpr int kFewRows = 64;                  // up to here the waves of a workgroup share the rows, beyond they share the keys
-
 template <typename T, int DP, bool PARTS>
 hipError_t launch_rows(const AttendProblem &p, hipStream_t stream)
 {
     const int rows = p.tokens * p.group * p.drafts;
     if (rows <= 16) return launch_one<T, DP, 1, 4, PARTS>(p, stream);
-    if constexpr (DP < 256) {
-        if (rows <= kFewRows) return launch_one<T, DP, 2, 4, PARTS>(p, stream);
-        return launch_one<T, DP, 2, 1, PARTS>(p, stream);
-    } else {
-        if (rows <= kFewRows) return launch_one<T, DP, 1, 4, PARTS>(p, stream);
-        return launch_one<T, DP, 1, 1, PARTS>(p, stream);
-    }
+    constexpr int RT = DP < 256 ? 2 : 1;
+    return rows <= kFewRows ? launch_one<T, DP, RT, 4, PARTS>(p, stream) : launch_one<T, DP, RT, 1, PARTS>(p, stream);
 }
 
 template <typename T, int DP>
 hipError_t launch_typed(AttendProblem p, hipStream_t stream)
 {
     p.in_order = Shape<T, DP>::kBf && p.tokens * p.group * p.drafts > kFewRows;
-    if (p.parts == 0) return launch_rows<T, DP, false>(p, stream);
+    if (p.all_parts == p.units && !p.ml) return launch_rows<T, DP, false>(p, stream);
     const hipError_t e = launch_rows<T, DP, true>(p, stream);
     if (e != hipSuccess) return e;
-    // Few parts: a wave per row, so that all rows are on their way at once; many: a workgroup, so that a row's parts are.
+    // Few parts: a wave per row, so that all rows are on their way at once; many (more than lanes of a wave, or than 8 a unit on
+    // average): a workgroup, so that a row's parts are.
     const int64_t rows = static_cast<int64_t>(p.sequences) * p.heads * p.tokens;
-    if (p.parts <= 8) hipLaunchKernelGGL((k_attend_join<T, DP, 1>), dim3(static_cast<unsigned>((rows + 3) / 4)), dim3(kAttendThreads), 0, stream, p);
+    if (p.all_parts <= 8 * p.units && (!p.balanced || p.most_parts <= 64)) hipLaunchKernelGGL((k_attend_join<T, DP, 1>), dim3(static_cast<unsigned>((rows + 3) / 4)), dim3(kAttendThreads), 0, stream, p);
     else hipLaunchKernelGGL((k_attend_join<T, DP, 4>), dim3(static_cast<unsigned>(rows)), dim3(kAttendThreads), 0, stream, p);
     return hipGetLastError();
 }
@@ -857,23 +885,44 @@ AttendPlan plan_attend(int sequences, int drafts, bool shared, int tokens, int h
 {
     AttendPlan a{};
     const int dp = head_dim <= 64 ? 64 : (head_dim <= 128 ? 128 : 256);
-    const int rows = tokens * (heads / kv_heads) * drafts;
+    const int rows = tokens * (heads / kv_heads) * drafts, tall = dp < 256 ? 32 : 16;
+    // rows of a workgroup: a wave's, which all four share, or four waves' own ones, spread evenly over the workgroups
+    if (rows <= kFewRows) a.block_rows = rows <= 16 ? 16 : tall;
+    else {
+        const int blocks = (rows + 4 * tall - 1) / (4 * tall), waves = (rows + tall - 1) / tall;
+        a.block_rows = (waves + blocks - 1) / blocks * tall;
+    }
+    a.row_blocks = (rows + a.block_rows - 1) / a.block_rows;
+    a.units = sequences / drafts;
+    a.all_parts = a.units;
     if (window > 0) longest = longest < static_cast<int64_t>(window) + tokens ? longest : static_cast<int64_t>(window) + tokens;
-    const int per = rows <= 64 ? 32 : 128;
-    const int64_t base = static_cast<int64_t>(sequences / drafts) * kv_heads * ((rows + per - 1) / per);
-    const int least = 256;                                     // keys of a chunk
-    int64_t chunks = (4 * compute_units() + base - 1) / (base < 1 ? 1 : base);
+    const int64_t base = static_cast<int64_t>(a.units) * kv_heads * a.row_blocks;
+    const int least = rows <= kFewRows ? 256 : 128;            // keys of a part
+    const int64_t slots = 2 * compute_units();                 // workgroups on the card at once: registers leave room for two a compute unit
+    int64_t chunks = slots / (base < 1 ? 1 : base);
     const int64_t most = (longest + least - 1) / least;
     if (chunks > most) chunks = most;
-    if (chunks > kMaxParts - 1) chunks = kMaxParts - 1;
+    if (chunks > kMaxParts) chunks = kMaxParts;
     if (chunks < 1) chunks = 1;
     if (chunks == 1 && !shared) return a;                      // one pass, nothing to join
-    a.chunks = static_cast<int>(chunks);
-    a.parts = a.chunks + (shared ? 1 : 0);
-    a.chunk_keys = static_cast<int>(((longest + chunks - 1) / chunks + 127) / 128 * 128);
-    const size_t parts = static_cast<size_t>(sequences / drafts) * kv_heads * a.parts * rows;
+    a.own_keys = shared ? drafts * 32 : 0;
+    a.chunk_keys = least;
+    a.grain = rows <= kFewRows ? 128 : 32;
+    a.balanced = a.units <= 64 && (shared || tokens <= 64);
+    if (a.balanced) {
+        a.most_parts = static_cast<int>(slots / (static_cast<int64_t>(kv_heads) * a.row_blocks));
+        if (a.most_parts < a.units) a.most_parts = a.units;
+        if (a.most_parts > kMaxParts) a.most_parts = kMaxParts;
+        a.all_parts = a.most_parts + a.units;
+    } else {
+        a.chunks = static_cast<int>(chunks);
+        a.all_parts = a.units * a.chunks;
+        a.chunk_keys = static_cast<int>(((longest + chunks - 1) / chunks + 127) / 128 * 128);
+    }
+    const size_t parts = static_cast<size_t>(a.all_parts) * kv_heads * rows;
+    a.places_bytes = (static_cast<size_t>(a.units) * sizeof(int2) + 255) / 256 * 256;
     a.ml_bytes = (parts * sizeof(float2) + 255) / 256 * 256;
-    a.bytes = a.ml_bytes + (parts * dp * sizeof(float) + 255) / 256 * 256;
+    a.bytes = a.places_bytes + a.ml_bytes + (parts * dp * sizeof(float) + 255) / 256 * 256;
     return a;
 }
 

@@ -911,6 +911,21 @@ __device__ __forceinline__ double wave_inclusive_sum(double v) {
     return v;
 }
 
+// Running sum over the wave in lane order, of whole numbers.
+__device__ __forceinline__ uint32_t wave_inclusive_count(uint32_t v)
+{
+#define SPECGBV_COUNT_STEP(CTRL, ROW_MASK) \
+    v += static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(v), CTRL, ROW_MASK, 0xf, false))
+    SPECGBV_COUNT_STEP(0x111, 0xf);
+    SPECGBV_COUNT_STEP(0x112, 0xf);
+    SPECGBV_COUNT_STEP(0x114, 0xf);
+    SPECGBV_COUNT_STEP(0x118, 0xf);
+    SPECGBV_COUNT_STEP(0x142, 0xa);
+    SPECGBV_COUNT_STEP(0x143, 0xc);
+#undef SPECGBV_COUNT_STEP
+    return v;
+}
+
 // Sum over the wave; every lane gets the result.
 __device__ __forceinline__ double wave_sum(double v) {
     const long long b = __double_as_longlong(wave_inclusive_sum(v));

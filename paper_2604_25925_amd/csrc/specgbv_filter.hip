@@ -29,21 +29,6 @@ constexpr uint32_t kNothing = 0x007FFFFFu;    // key of -inf
 // The value of a key that bounds others from above: -0 has a key of its own, which no entry has, and equals the 0 above it.
 __device__ __forceinline__ float bound_of(uint32_t k) { return value_of(k == 0x7FFFFFFFu ? k - 1 : k); }
 
-// Running sum over the wave by moves between lanes, as wave_inclusive_sum.
-__device__ __forceinline__ uint32_t wave_inclusive_count(uint32_t v)
-{
-#define SPECGBV_COUNT_STEP(CTRL, ROW_MASK) \
-    v += static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(v), CTRL, ROW_MASK, 0xf, false))
-    SPECGBV_COUNT_STEP(0x111, 0xf);
-    SPECGBV_COUNT_STEP(0x112, 0xf);
-    SPECGBV_COUNT_STEP(0x114, 0xf);
-    SPECGBV_COUNT_STEP(0x118, 0xf);
-    SPECGBV_COUNT_STEP(0x142, 0xa);
-    SPECGBV_COUNT_STEP(0x143, 0xc);
-#undef SPECGBV_COUNT_STEP
-    return v;
-}
-
 // e^x for x <= 0 in float64: 2^n times the Taylor sum of e^r, |r| <= ln(2) / 2, to r^12 / 12!, whose remainder is 2 10^-16 of it.
 __device__ __forceinline__ double exp_of(double x)
 {

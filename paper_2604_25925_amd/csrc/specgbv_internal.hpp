@@ -174,17 +174,25 @@ struct AttendProblem {
     PageMap map;
     int64_t q_stride[3], out_stride[3], positions_stride;
     int32_t k_page_stride, k_head_stride, k_token_stride, v_page_stride, v_head_stride, v_token_stride;
-    float2 *ml;                    // [units][kv_heads][parts][rows] reference and sum of a part; unit: sequence, or prefix with its drafts
+    float2 *ml;                    // [parts][kv_heads][rows] reference and sum of a part of a unit (a sequence, or a prefix with its drafts);
+                                   // null: one pass without parts
     float *acc;                    // the same, with the sums of values
+    int2 *places;                  // [units] first part and number of parts, where the parts are balanced
     float c;                       // scale * log2(e)
     int sequences, tokens, heads, kv_heads, group, head_dim, drafts, window;
-    int parts, chunks, chunk_keys; // 0 parts: one pass without partial sums; else the chunks and, with drafts, their own keys
+    int units, all_parts;          // all_parts: at most, of all units
+    int balanced, most_parts, own_keys, grain;       // parts by the units' lengths: how many at most, what a unit's own keys count for, granularity
+    int chunks, chunk_keys;        // not balanced: parts of each unit; keys of a part (balanced: at least)
+    int block_rows, row_blocks;    // rows of a workgroup
     int q_wide, out_wide;          // 16-byte loads of q, stores of whole vectors to out
-    int items, row_blocks;         // set by the launches, with what divides block and row numbers
-    int in_order;                  // partial sums are held in the entries' order
-    Divider by_blocks, by_kv_heads, by_parts, by_in_draft, by_group;
+    int in_order;                  // partial sums are held in the entries' order (this and the next are set by the launches)
+    int items;
+    Divider by_blocks, by_kv_heads, by_chunks, by_in_draft, by_group;
 };
-struct AttendPlan { int parts, chunks, chunk_keys; size_t ml_bytes, bytes; };
+struct AttendPlan {
+    int units, all_parts, balanced, most_parts, own_keys, grain, chunks, chunk_keys, block_rows, row_blocks;
+    size_t places_bytes, ml_bytes, bytes;        // bytes: 0 where nothing is to be joined
+};
 AttendPlan plan_attend(int sequences, int drafts, bool shared, int tokens, int heads, int kv_heads, int head_dim, int window,
                        int64_t longest);
 hipError_t launch_attend(const AttendProblem &p, int dtype, hipStream_t stream);

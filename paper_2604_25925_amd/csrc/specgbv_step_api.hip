@@ -186,12 +186,22 @@ specgbv_status specgbv_attend_paged(const specgbv_paged_cache *cache, const spec
     p.k_page_stride = static_cast<int32_t>(c.k_page_stride); p.k_head_stride = static_cast<int32_t>(c.k_head_stride);
     p.k_token_stride = static_cast<int32_t>(c.k_token_stride); p.v_page_stride = static_cast<int32_t>(c.v_page_stride);
     p.v_head_stride = static_cast<int32_t>(c.v_head_stride); p.v_token_stride = static_cast<int32_t>(c.v_token_stride);
-    p.ml = static_cast<float2 *>(workspace);
-    p.acc = reinterpret_cast<float *>(static_cast<char *>(workspace) + plan.ml_bytes);
+    if (plan.bytes > 0) {
+        char *ws = static_cast<char *>(workspace);
+        p.places = reinterpret_cast<int2 *>(ws);
+        p.ml = reinterpret_cast<float2 *>(ws + plan.places_bytes);
+        p.acc = reinterpret_cast<float *>(ws + plan.places_bytes + plan.ml_bytes);
+    }
     p.c = static_cast<float>((a.scale > 0.0f ? static_cast<double>(a.scale) : 1.0 / std::sqrt(static_cast<double>(c.head_dim))) * 1.4426950408889634074);
     p.sequences = c.sequences; p.tokens = a.tokens; p.heads = a.heads; p.kv_heads = c.kv_heads; p.group = a.heads / c.kv_heads;
     p.head_dim = c.head_dim; p.drafts = a.prefixes > 0 ? c.sequences / a.prefixes : 1; p.window = a.window;
-    p.parts = plan.parts; p.chunks = plan.chunks; p.chunk_keys = plan.chunk_keys;
+    p.units = plan.units; p.all_parts = plan.all_parts; p.balanced = plan.balanced; p.most_parts = plan.most_parts;
+    p.own_keys = plan.own_keys; p.grain = plan.grain; p.chunks = plan.chunks; p.chunk_keys = plan.chunk_keys;
+    p.block_rows = plan.block_rows; p.row_blocks = plan.row_blocks;
+    p.by_kv_heads = Divider::of(p.kv_heads);
+    p.by_chunks = Divider::of(plan.chunks > 0 ? plan.chunks : 1);
+    p.by_in_draft = Divider::of(p.tokens * p.group);
+    p.by_group = Divider::of(p.group);
     const int unit = static_cast<int>(16 / esz);
     p.q_wide = allowed_width(unit, a.q, a.q_stride, 3, esz) == unit;
     p.out_wide = allowed_width(unit, a.out, a.out_stride, 3, esz) == unit;
