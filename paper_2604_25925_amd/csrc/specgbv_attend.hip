@@ -479,6 +479,7 @@ __global__ void __launch_bounds__(kAttendThreads, (Shape<T, DP>::waves(RT))) k_a
             bad_pages = __any(bad != 0);
         }
     }
+    bool odd = false;                                         // a value that is not finite was cleared
     for (; tile < end; tile += step) {
         const bool more = tile + step < end;
         const int here = stage;
@@ -537,16 +538,13 @@ __global__ void __launch_bounds__(kAttendThreads, (Shape<T, DP>::waves(RT))) k_a
         // weights
         const bool lost = WK == 4 ? cur_v.page < 0 : lost_here;
         const bool partial = tile < lo_most || tile + kKeys > hi_least || tile + kKeys > end || (WK == 4 ? __any(lost) : bad_pages);
-        uint32_t seen[RT];                                    // bits: which of the lane's keys its row sees
 #pragma unroll
         for (int r = 0; r < RT; ++r) {
-            seen[r] = (1u << kRun) - 1;
             if (partial) {
                 const int base = tile + quad * kRun;
                 const int from = max(row_low[r] - base, 0), to = lost ? 0 : min(max(row_high[r] - base, 0), kRun);
-                seen[r] = from < to ? ((1u << to) - 1) & ~((1u << from) - 1) : 0u;
 #pragma unroll
-                for (int k = 0; k < kRun; ++k) s[r][k / 4][k % 4] = seen[r] >> k & 1 ? s[r][k / 4][k % 4] : -INFINITY;
+                for (int k = 0; k < kRun; ++k) s[r][k / 4][k % 4] = k >= from && k < to ? s[r][k / 4][k % 4] : -INFINITY;
             }
             float top = s[r][0][0];
 #pragma unroll
@@ -579,23 +577,21 @@ __global__ void __launch_bounds__(kAttendThreads, (Shape<T, DP>::waves(RT))) k_a
             for (int k = 0; k < kRun; ++k) sum[r] += s[r][k / 4][k % 4];
         }
 
-        // values that some rows do not see: a weight of 0 does not take out what is not finite.  Keys that no row sees are cleared;
-        // where another value is not finite, it is taken out and put back by products of marks alone, for the rows that see it.
-        bool odd = false;
+        // values that some rows do not see: a weight of 0 does not take out what is not finite.  In such tiles keys that no row sees are
+        // cleared, and so is what is not finite; it is put back behind the loop, for the rows that see it.
         if (partial) {
             const int base = tile + quad * kRun;
             uint32_t bad = 0, keep[kRun];
 #pragma unroll
             for (int k = 0; k < kRun; ++k) keep[k] = lost | (base + k < lo_all) | (base + k >= hi_all) ? 0u : 0xFFFFFFFFu;
+            auto clean = [&](uint32_t &w, uint32_t mask) { w &= mask; bad |= exponents_full<T>(w); };
             if constexpr (kTurned) {
 #pragma unroll
                 for (int c = 0; c < kCols; ++c) {
-                    uint32_t *w = &va[c].x;
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        w[k] &= (keep[2 * k] & 0xFFFFu) | (keep[2 * k + 1] & 0xFFFF0000u);
-                        bad |= exponents_full<T>(w[k]);
-                    }
+                    clean(va[c].x, (keep[0] & 0xFFFFu) | (keep[1] & 0xFFFF0000u));
+                    clean(va[c].y, (keep[2] & 0xFFFFu) | (keep[3] & 0xFFFF0000u));
+                    clean(va[c].z, (keep[4 % kRun] & 0xFFFFu) | (keep[5 % kRun] & 0xFFFF0000u));
+                    clean(va[c].w, (keep[6 % kRun] & 0xFFFFu) | (keep[7 % kRun] & 0xFFFF0000u));
                 }
             } else {
 #pragma unroll
@@ -603,26 +599,75 @@ __global__ void __launch_bounds__(kAttendThreads, (Shape<T, DP>::waves(RT))) k_a
 #pragma unroll
                     for (int g = 0; g < kGroups; ++g)
 #pragma unroll
-                        for (int w = 0; w < kWords; ++w) { vf[k][g][w] &= keep[k]; bad |= exponents_full<T>(vf[k][g][w]); }
+                        for (int w = 0; w < kWords; ++w) clean(vf[k][g][w], keep[k]);
             }
-            odd = __any(bad != 0);
+            if (__any(bad != 0)) {
+                odd = true;
+                if constexpr (kTurned) {
+#pragma unroll
+                    for (int c = 0; c < kCols; ++c) va[c] = U4{without_odd(va[c].x), without_odd(va[c].y), without_odd(va[c].z), without_odd(va[c].w)};
+                } else {
+#pragma unroll
+                    for (int k = 0; k < kRun; ++k)
+#pragma unroll
+                        for (int g = 0; g < kGroups; ++g)
+#pragma unroll
+                            for (int w = 0; w < kWords; ++w) vf[k][g][w] = without_odd(vf[k][g][w]);
+                }
+            }
         }
-        if (odd) {
+
+        // sums of values: entries x rows
+        if constexpr (S::kBf) {
+            B8 w[RT];
+#pragma unroll
+            for (int r = 0; r < RT; ++r)
+#pragma unroll
+                for (int k = 0; k < kRun; ++k) w[r][k] = static_cast<__bf16>(s[r][k / 4][k % 4]);
+#pragma unroll
+            for (int c = 0; c < kCols; ++c) {
+                const U4 a = entry_of(c);
+#pragma unroll
+                for (int r = 0; r < RT; ++r) acc[r][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(B8, a), w[r], acc[r][c], 0, 0, 0);
+            }
+        } else {
+#pragma unroll
+            for (int c = 0; c < kCols; ++c)
+#pragma unroll
+                for (int r = 0; r < RT; ++r)
+#pragma unroll
+                    for (int k = 0; k < kRun; ++k)
+                        acc[r][c] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(vf[k][c / kVec][c % kVec]), s[r][0][k], acc[r][c], 0, 0, 0);
+        }
+        if constexpr (WK == 4) load_values(here_v, more);
+    }
+    // ---- what was not finite in tiles that not all rows see whole: products of marks alone say which rows see such an entry
+    if (odd) {
 #pragma unroll 1
-            for (int kind = 0; kind < 3; ++kind) {
-                const float what = kind == 0 ? NAN : (kind == 1 ? INFINITY : -INFINITY);
+        for (int again = start + (WK == 4 && !own ? wave * kKeys : 0); again < end; again += step) {
+            const Place at = run_of(pages_of(again), again, quad);
+            if (again >= lo_most && again + kKeys <= hi_least && again + kKeys <= end && !(WK == 4 ? __any(at.page < 0) : bad_pages)) continue;
+            const int base = again + quad * kRun;
+            uint32_t seen[RT];
 #pragma unroll
-                for (int c = 0; c < kCols; ++c) {
-                    uint32_t e[kRun];
-                    if constexpr (S::kBf) {
-                        const U4 x = entry_of(c);
-                        const uint32_t *w = &x.x;
+            for (int r = 0; r < RT; ++r) {
+                const int from = max(row_low[r] - base, 0), to = at.page < 0 ? 0 : min(max(row_high[r] - base, 0), kRun);
+                seen[r] = from < to ? ((1u << to) - 1) & ~((1u << from) - 1) : 0u;
+            }
+            const T *src = vb + max(at.page, 0) * static_cast<int64_t>(p.v_page_stride) + at.slot * static_cast<int64_t>(p.v_token_stride);
 #pragma unroll
-                        for (int k = 0; k < kRun; ++k) e[k] = w[k / 2] >> (k % 2 * 16) & 0xFFFFu;
-                    } else {
+            for (int c = 0; c < kCols; ++c) {
+                const int d = kTurned ? 16 * c + col : (c / kVec * 16 + col) * kVec + c % kVec;
+                uint32_t e[kRun];
 #pragma unroll
-                        for (int k = 0; k < kRun; ++k) e[k] = vf[k][c / kVec][c % kVec];
-                    }
+                for (int k = 0; k < kRun; ++k) {
+                    const T x = src[k * static_cast<int64_t>(p.v_token_stride) + (d < p.head_dim ? d : 0)];
+                    if constexpr (S::kBf) e[k] = x;
+                    else e[k] = __float_as_uint(x);
+                }
+#pragma unroll 1
+                for (int kind = 0; kind < 3; ++kind) {
+                    const float what = kind == 0 ? NAN : (kind == 1 ? INFINITY : -INFINITY);
 #pragma unroll
                     for (int r = 0; r < RT; ++r) {
                         F4 n{0, 0, 0, 0};
@@ -646,39 +691,6 @@ __global__ void __launch_bounds__(kAttendThreads, (Shape<T, DP>::waves(RT))) k_a
                 }
             }
         }
-
-        // sums of values: entries x rows
-        if constexpr (S::kBf) {
-            B8 w[RT];
-#pragma unroll
-            for (int r = 0; r < RT; ++r)
-#pragma unroll
-                for (int k = 0; k < kRun; ++k) w[r][k] = static_cast<__bf16>(s[r][k / 4][k % 4]);
-#pragma unroll
-            for (int c = 0; c < kCols; ++c) {
-                U4 a = entry_of(c);
-                if (odd) a = U4{without_odd(a.x), without_odd(a.y), without_odd(a.z), without_odd(a.w)};       // uniform
-#pragma unroll
-                for (int r = 0; r < RT; ++r) acc[r][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(B8, a), w[r], acc[r][c], 0, 0, 0);
-            }
-        } else {
-            if (odd) {
-#pragma unroll
-                for (int k = 0; k < kRun; ++k)
-#pragma unroll
-                    for (int g = 0; g < kGroups; ++g)
-#pragma unroll
-                        for (int w = 0; w < kWords; ++w) vf[k][g][w] = without_odd(vf[k][g][w]);
-            }
-#pragma unroll
-            for (int c = 0; c < kCols; ++c)
-#pragma unroll
-                for (int r = 0; r < RT; ++r)
-#pragma unroll
-                    for (int k = 0; k < kRun; ++k)
-                        acc[r][c] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(vf[k][c / kVec][c % kVec]), s[r][0][k], acc[r][c], 0, 0, 0);
-        }
-        if constexpr (WK == 4) load_values(here_v, more);
     }
     }
 #pragma unroll
@@ -898,7 +910,9 @@ AttendPlan plan_attend(int sequences, int drafts, bool shared, int tokens, int h
     if (window > 0) longest = longest < static_cast<int64_t>(window) + tokens ? longest : static_cast<int64_t>(window) + tokens;
     const int64_t base = static_cast<int64_t>(a.units) * kv_heads * a.row_blocks;
     const int least = rows <= kFewRows ? 256 : 128;            // keys of a part
-    const int64_t slots = 2 * compute_units();                 // workgroups on the card at once: registers leave room for two a compute unit
+    // workgroups on the card at once: registers leave room for two a compute unit; one in sixteen is left free, since a single workgroup
+    // that has to wait for a place doubles the launch
+    const int64_t slots = 2 * compute_units() * 15 / 16;
     int64_t chunks = slots / (base < 1 ? 1 : base);
     const int64_t most = (longest + least - 1) / least;
     if (chunks > most) chunks = most;
