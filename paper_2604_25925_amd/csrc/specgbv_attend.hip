@@ -770,81 +770,134 @@ __global__ void __launch_bounds__(kAttendThreads, (Shape<T, DP>::waves(RT))) k_a
     }
 }
 
-// The parts of a row joined: DP / 4 lanes take a part's vectors, the other lanes the next parts'; WAVES waves per row.
-template <typename T, int DP, int WAVES>
+// The place of a row of the result and of its parts.
+struct JoinRow {
+    int draft, s, t, h, parts;
+    int64_t part0, between;
+
+    __device__ __forceinline__ JoinRow(const AttendProblem &p, int64_t at)
+    {
+        const int rows = p.tokens * p.group * p.drafts;
+        const int64_t pair = at / rows;
+        const int row = static_cast<int>(at - pair * rows), unit = p.by_kv_heads.div(static_cast<int>(pair)), head0 = p.by_kv_heads.mod(static_cast<int>(pair), unit);
+        draft = p.by_in_draft.div(row);
+        const int in = p.by_in_draft.mod(row, draft);
+        s = unit * p.drafts + draft; t = p.by_group.div(in); h = head0 * p.group + p.by_group.mod(in, t);
+        const int2 where = p.balanced ? p.places[unit] : make_int2(unit * p.chunks, p.chunks);
+        parts = where.y;
+        part0 = (static_cast<int64_t>(where.x) * p.kv_heads + head0) * rows + row;
+        between = static_cast<int64_t>(p.kv_heads) * rows;
+    }
+};
+
+// Entry of a row that vector `vec` of its partial sums starts with.
+template <typename T, int DP> __device__ __forceinline__ int entry_at(const AttendProblem &p, int vec)
+{
+    constexpr int kVec = Shape<T, DP>::kVec;
+    const int quad = vec & 3, piece = vec >> 2, n = piece % (kVec / 4), gi = piece / (kVec / 4), i = gi & 3, g = gi >> 2;
+    return p.in_order ? 4 * vec : (16 * g + 4 * quad + i) * kVec + 4 * n;
+}
+
+// The parts of a row joined by DP / 4 lanes, each with a vector of its entries: several rows per wave, so that all are on their way at once.
+template <typename T, int DP>
 __global__ void __launch_bounds__(kAttendThreads) k_attend_join(AttendProblem p)
 {
-    constexpr int kVec = Shape<T, DP>::kVec, kLanes = DP / 4, kThreads = 64 * WAVES, kSets = kThreads / kLanes, kAhead = 4;
-    __shared__ float sh_f[WAVES > 1 ? kMaxParts : 1];
-    __shared__ float sh_most[kWavesPerGroup], sh_total[kWavesPerGroup];
-    __shared__ F4 sh_acc[WAVES > 1 ? kWavesPerGroup * kLanes : 1];
-    const int tid = WAVES > 1 ? threadIdx.x : threadIdx.x & 63, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int vec = tid % kLanes, set = tid / kLanes;
-    const int in_draft = p.tokens * p.group, rows = in_draft * p.drafts;
-    const int64_t all = static_cast<int64_t>(p.sequences) * p.kv_heads * in_draft;
-    const int64_t at = WAVES > 1 ? blockIdx.x : static_cast<int64_t>(blockIdx.x) * 4 + wave;
-    if (at >= all) return;
-    const int64_t pair = at / rows;
-    const int row = static_cast<int>(at - pair * rows);
-    const int unit = static_cast<int>(pair / p.kv_heads), head0 = static_cast<int>(pair - static_cast<int64_t>(unit) * p.kv_heads);
-    const int draft = row / in_draft, in = row - draft * in_draft, s = unit * p.drafts + draft, t = in / p.group, h = head0 * p.group + in - t * p.group;
-    int2 mine_at = p.balanced ? p.places[unit] : make_int2(unit * p.chunks, p.chunks);
-    const int parts = mine_at.y;
-    const int64_t part0 = (static_cast<int64_t>(mine_at.x) * p.kv_heads + head0) * rows + row, between = static_cast<int64_t>(p.kv_heads) * rows;
+    constexpr int kLanes = DP / 4, kAhead = 4;
+    const int vec = threadIdx.x % kLanes;
+    const int64_t at = static_cast<int64_t>(blockIdx.x) * (kAttendThreads / kLanes) + threadIdx.x / kLanes;
+    if (at >= static_cast<int64_t>(p.sequences) * p.heads * p.tokens) return;          // whole groups of lanes
+    const JoinRow row(p, at);
+    const int pos = p.positions[row.s * p.positions_stride + row.t];
+    const F4 *acc_of = reinterpret_cast<const F4 *>(p.acc) + vec;
 
-    // the first parts' sums are on their way while the weights of all parts are looked at
+    // the first parts' sums are on their way while the references of all parts are looked at
     F4 v[kAhead];
 #pragma unroll
-    for (int i = 0; i < kAhead; ++i)
-        v[i] = reinterpret_cast<const F4 *>(p.acc + (part0 + static_cast<int64_t>(min(set + i * kSets, parts - 1)) * between) * DP)[vec];
+    for (int i = 0; i < kAhead; ++i) v[i] = acc_of[(row.part0 + min(i, row.parts - 1) * row.between) * (DP / 4)];
+    float most = -INFINITY;
+    for (int c = vec; c < row.parts; c += kLanes) {
+        const float2 ml = p.ml[row.part0 + c * row.between];
+        if (ml.y != 0.0f) most = fmaxf(most, ml.x);                                    // (a sum that is no number goes on)
+    }
+#pragma unroll
+    for (int m = kLanes / 2; m > 0; m >>= 1) most = fmaxf(most, __shfl_xor(most, m, 64));
+    F4 acc{0, 0, 0, 0};
+    float total = 0.0f;
+    for (int c0 = 0; c0 < row.parts; c0 += kAhead) {
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            const int c = c0 + i;
+            if (c >= row.parts) break;
+            const float2 ml = p.ml[row.part0 + c * row.between];
+            if (ml.y != 0.0f) {                                                        // else there is nothing to read
+                const float f = ml.x == most ? 1.0f : exp2_of(ml.x - most);
+                total += ml.y * f;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[e] += v[i][e] * f;
+            }
+            if (c + kAhead < row.parts) v[i] = acc_of[(row.part0 + (c + kAhead) * row.between) * (DP / 4)];
+        }
+    }
+    const int d = entry_at<T, DP>(p, vec);
+    if (d >= p.head_dim) return;
+    const float inv = pos >= 0 && total != 0.0f ? 1.0f / total : 0.0f;
+    store_entries(static_cast<T *>(p.out) + row.s * p.out_stride[0] + row.t * p.out_stride[1] + row.h * p.out_stride[2] + d, acc, inv, p.out_wide);
+}
+
+// The same by a workgroup per row, for many parts: 4096 / DP of them at once.
+template <typename T, int DP>
+__global__ void __launch_bounds__(kAttendThreads) k_attend_join_many(AttendProblem p)
+{
+    constexpr int kLanes = DP / 4, kSets = kAttendThreads / kLanes, kAhead = 4;
+    __shared__ float sh_f[kMaxParts];
+    __shared__ float sh_most[kWavesPerGroup], sh_total[kWavesPerGroup];
+    __shared__ F4 sh_acc[kWavesPerGroup * kLanes];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, vec = tid % kLanes, set = tid / kLanes;
+    const JoinRow row(p, blockIdx.x);
+    const F4 *acc_of = reinterpret_cast<const F4 *>(p.acc) + vec;
+
+    F4 v[kAhead];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) v[i] = acc_of[(row.part0 + min(set + i * kSets, row.parts - 1) * row.between) * (DP / 4)];
     float2 ml{-INFINITY, 0.0f};
-    if (tid < parts) ml = p.ml[part0 + static_cast<int64_t>(tid) * between];          // (parts are at most the threads of a row)
-    const int pos = p.positions[s * p.positions_stride + t];
-    const bool some = ml.y != 0.0f;                                                   // (a sum that is no number goes on)
+    if (tid < row.parts) ml = p.ml[row.part0 + tid * row.between];                     // (parts are at most the threads)
+    const int pos = p.positions[row.s * p.positions_stride + row.t];
+    const bool some = ml.y != 0.0f;
     float most = some ? ml.x : -INFINITY;
     for (int m = 32; m > 0; m >>= 1) most = fmaxf(most, __shfl_xor(most, m, 64));
-    if (WAVES > 1) {
-        if (lane == 0) sh_most[wave] = most;
-        __syncthreads();
-        most = fmaxf(fmaxf(sh_most[0], sh_most[1]), fmaxf(sh_most[2], sh_most[3]));
-    }
+    if (lane == 0) sh_most[wave] = most;
+    __syncthreads();
+    most = fmaxf(fmaxf(sh_most[0], sh_most[1]), fmaxf(sh_most[2], sh_most[3]));
     const float f = !some ? 0.0f : (ml.x == most ? 1.0f : exp2_of(ml.x - most));
     float total = some ? ml.y * f : 0.0f;
     for (int m = 32; m > 0; m >>= 1) total += __shfl_xor(total, m, 64);
-    if (WAVES > 1) {
-        if (lane == 0) sh_total[wave] = total;
-        if (tid < kMaxParts) sh_f[tid] = some ? f : -1.0f;                            // (-1: there is nothing to read)
-        __syncthreads();
-        total = (sh_total[0] + sh_total[1]) + (sh_total[2] + sh_total[3]);
-    }
-    const float mine = some ? f : -1.0f;
+    if (lane == 0) sh_total[wave] = total;
+    sh_f[tid] = some ? f : -1.0f;                                                      // (-1: there is nothing to read)
+    __syncthreads();
+    total = (sh_total[0] + sh_total[1]) + (sh_total[2] + sh_total[3]);
     F4 acc{0, 0, 0, 0};
-    for (int c0 = set; c0 - set < parts; c0 += kAhead * kSets) {                    // the same count for all
+    for (int c0 = set; c0 - set < row.parts; c0 += kAhead * kSets) {                   // the same count for all
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) {
-            const int c = c0 + i * kSets;
-            const float w = c >= parts ? -1.0f : (WAVES > 1 ? sh_f[c] : __shfl(mine, c, 64));
+            const int c = c0 + i * kSets, n = c + kAhead * kSets;
+            const float w = c >= row.parts ? -1.0f : sh_f[c];
 #pragma unroll
             for (int e = 0; e < 4; ++e) acc[e] += w < 0.0f ? 0.0f : v[i][e] * w;
-            const int n = c + kAhead * kSets;
-            if (n < parts) v[i] = reinterpret_cast<const F4 *>(p.acc + (part0 + static_cast<int64_t>(n) * between) * DP)[vec];
+            if (n < row.parts) v[i] = acc_of[(row.part0 + n * row.between) * (DP / 4)];
         }
     }
 #pragma unroll
     for (int m = 32; m >= kLanes; m >>= 1)
 #pragma unroll
         for (int e = 0; e < 4; ++e) acc[e] += __shfl_xor(acc[e], m, 64);
-    if (WAVES > 1) {
-        if (lane < kLanes) sh_acc[wave * kLanes + vec] = acc;
-        __syncthreads();
-        if (tid >= kLanes) return;
-        acc = (sh_acc[vec] + sh_acc[kLanes + vec]) + (sh_acc[2 * kLanes + vec] + sh_acc[3 * kLanes + vec]);
-    } else if (set != 0) return;
-    const int quad = vec & 3, piece = vec >> 2, n = piece % (kVec / 4), gi = piece / (kVec / 4), i = gi & 3, g = gi >> 2;
-    const int d = p.in_order ? 4 * vec : (16 * g + 4 * quad + i) * kVec + 4 * n;
+    if (lane < kLanes) sh_acc[wave * kLanes + vec] = acc;
+    __syncthreads();
+    if (tid >= kLanes) return;
+    acc = (sh_acc[vec] + sh_acc[kLanes + vec]) + (sh_acc[2 * kLanes + vec] + sh_acc[3 * kLanes + vec]);
+    const int d = entry_at<T, DP>(p, vec);
     if (d >= p.head_dim) return;
     const float inv = pos >= 0 && total != 0.0f ? 1.0f / total : 0.0f;
-    store_entries(static_cast<T *>(p.out) + s * p.out_stride[0] + t * p.out_stride[1] + h * p.out_stride[2] + d, acc, inv, p.out_wide);
+    store_entries(static_cast<T *>(p.out) + row.s * p.out_stride[0] + row.t * p.out_stride[1] + row.h * p.out_stride[2] + d, acc, inv, p.out_wide);
 }
 
 template <typename T, int DP, int RT, int WK, bool PARTS>
@@ -874,11 +927,11 @@ hipError_t launch_typed(AttendProblem p, hipStream_t stream)
     if (p.all_parts == p.units && !p.ml) return launch_rows<T, DP, false>(p, stream);
     const hipError_t e = launch_rows<T, DP, true>(p, stream);
     if (e != hipSuccess) return e;
-    // Few parts: a wave per row, so that all rows are on their way at once; many (more than lanes of a wave, or than 8 a unit on
-    // average): a workgroup, so that a row's parts are.
-    const int64_t rows = static_cast<int64_t>(p.sequences) * p.heads * p.tokens;
-    if (p.all_parts <= 8 * p.units && (!p.balanced || p.most_parts <= 64)) hipLaunchKernelGGL((k_attend_join<T, DP, 1>), dim3(static_cast<unsigned>((rows + 3) / 4)), dim3(kAttendThreads), 0, stream, p);
-    else hipLaunchKernelGGL((k_attend_join<T, DP, 4>), dim3(static_cast<unsigned>(rows)), dim3(kAttendThreads), 0, stream, p);
+    // Few parts (8 a unit on average): several rows per wave, so that all rows are on their way at once; many: a workgroup per row, so that
+    // a row's parts are.
+    const int64_t rows = static_cast<int64_t>(p.sequences) * p.heads * p.tokens, per = kAttendThreads / (DP / 4);
+    if (p.all_parts <= 8 * p.units) hipLaunchKernelGGL((k_attend_join<T, DP>), dim3(static_cast<unsigned>((rows + per - 1) / per)), dim3(kAttendThreads), 0, stream, p);
+    else hipLaunchKernelGGL((k_attend_join_many<T, DP>), dim3(static_cast<unsigned>(rows)), dim3(kAttendThreads), 0, stream, p);
     return hipGetLastError();
 }
 
