@@ -299,3 +299,47 @@ def test_replays_of_a_captured_call():
         torch.cuda.synchronize()
         assert torch.equal(out, eager)
         check_attend(out, q, k, v, table, pos, "bf16")
+
+
+@pytest.mark.parametrize("dtype,S,T,width,window", [("bf16", 70, 1, 260, 0), ("f32", 66, 2, 150, 0), ("bf16", 65, 9, 160, 700)])
+def test_more_sequences_than_lanes(dtype, S, T, width, window):
+    """Units beyond 64 are cut alike, whatever their lengths; some are empty."""
+    import paper_2604_25925_amd as sg
+    rng = np.random.default_rng(S)
+    last = rng.integers(-1, width * 16, (S, 1))
+    last[1], last[2], last[S - 1] = -1, 0, width * 16 - 1
+    positions = np.maximum(last - T + 1 + np.arange(T), -1)
+    _run(S, T, 4, 1, 64, 16, dtype, width, window=window, positions=positions)
+    rng, q, k, v, table = _inputs(S, T, 4, 1, 64, 16, dtype, width)
+    assert sg.specgbv_attend_workspace_bytes(sg.PagedCache(k, v, table), q, window=window) > 0
+
+
+@pytest.mark.parametrize("dtype,B,K,T,H,G", [("bf16", 70, 2, 1, 4, 1), ("f32", 66, 3, 2, 2, 1), ("bf16", 65, 4, 9, 4, 2)])
+def test_more_prefixes_than_lanes(dtype, B, K, T, H, G):
+    import torch
+    import paper_2604_25925_amd as sg
+    rng = np.random.default_rng(B * K)
+    page, width, D = 16, 40, 64
+    length = rng.integers(0, width * page - T - 8, (B, 1))
+    length[0], length[1], length[B - 1] = 0, 5, width * page - T - 8
+    whole, S = length // page, B * K
+    table = rng.permutation(S * width).astype(np.int32).reshape(B, K, width)
+    table = np.where(np.arange(width) < whole[:, :, None], table[:, :1], table).reshape(S, width)
+    k, v, _ = make_cache(rng, S, width, page, G, D, dtype)
+    q = torch.from_numpy(rng.normal(0, 1.5, (S, T, H, D)).astype(np.float32)).cuda().to(torch_dtype(dtype))
+    pos = np.repeat(length, K, axis=0) + np.arange(T) + rng.integers(0, 8, (S, 1))
+    pos, table = torch.from_numpy(pos.astype(np.int32)).cuda(), torch.from_numpy(table).cuda()
+    sl = torch.from_numpy((whole * page).reshape(B).astype(np.int32)).cuda()
+    cache = sg.PagedCache(k, v, table)
+    out, ws = sg.specgbv_attend_paged(cache, q, pos, shared_len=sl)
+    ws.fill_(255)
+    out, _ = sg.specgbv_attend_paged(cache, q, pos, shared_len=sl, workspace=ws)
+    torch.cuda.synchronize()
+    check_attend(out, q, k, v, table, pos, dtype, label="shared")
+
+
+@pytest.mark.parametrize("dtype,D", [("bf16", 64), ("bf16", 128), ("bf16", 256), ("f32", 64), ("f32", 128), ("f32", 200)])
+def test_many_parts_are_joined(dtype, D):
+    """One sequence over the whole card, and one that is empty next to it: dozens of parts a row."""
+    _run(2, 1, 2, 1, D, 16, dtype, 1500, positions=[[23999], [-1]])
+    _run(1, 3, 5, 1, D, 16, dtype, 1100, positions=[[12, 17000, 17599]])
