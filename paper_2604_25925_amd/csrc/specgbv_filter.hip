@@ -527,19 +527,21 @@ __global__ void __launch_bounds__(TH, 4) k_filter(FilterProblem p)
 // (each overflow takes 65535 or 65536 from it), and the row is done by filter_row.
 typedef uint16_t U2x16 __attribute__((ext_vector_type(2)));
 constexpr uint32_t kNegInf2 = 0xFF80FF80u;
-constexpr int kSegments = 1024;               // of 64 values each: 512 of magnitudes from the top down, then 512 below zero from 0 down
 constexpr int kMaxTurns = 8192;               // rows of a workgroup at most
 
-struct CountShared {
-    uint32_t count[1 << 15];
-    double seg_weight[kSegments];             // running sums within blocks of 64 segments
-    uint32_t seg_count[kSegments];
-    double wave_weight[kFilterWaves];
-    uint32_t wave_count[kFilterWaves];
-    uint32_t chunk[kFilterWaves];             // entries of a value
+// TH threads count 32 TH magnitudes: 1024 all of them, 512 those from 2^-63 (which stands for 0) up to 2^65 (the last one stands for -inf).
+// A row with other entries than these (and 0 and -inf) is done by filter_row.
+template <int TH> struct CountShared {
+    uint32_t count[32 * TH];
+    // of the segments of 64 values: TH / 2 of magnitudes from the top down, then TH / 2 below zero from 0 down
+    double seg_weight[TH];                    // running sums within blocks of 64 segments
+    uint32_t seg_count[TH];
+    double wave_weight[TH / 64];
+    uint32_t wave_count[TH / 64];
+    uint32_t chunk[TH / 64];                  // entries of a value
     uint32_t place[2], nth[2];                // the cut's value (nth 0: all its entries stay) and the token's
-    u64 occurs[kFilterWaves], above[kFilterWaves];
-    uint32_t counted, summed;
+    u64 occurs[TH / 64], above[TH / 64];
+    uint32_t counted, summed, outside;
     int index;
 };
 
@@ -555,14 +557,16 @@ __device__ __forceinline__ u64 lane_bits_of(u64 v, int src)
     return static_cast<u64>(hi) << 32 | lo;
 }
 
-template <int NV>
-__global__ void __launch_bounds__(kFilterThreads) k_filter_counts(FilterProblem p)
+template <int NV, int TH>
+__global__ void __launch_bounds__(TH, 4) k_filter_counts(FilterProblem p)
 {
-    __shared__ union { CountShared c; FilterShared f; } shared;
-    __shared__ uint32_t again[kMaxTurns / 32];                     // rows of this workgroup whose counts overflowed
-    CountShared &sh = shared.c;
-    constexpr bool kAhead = NV <= 8;          // the next row is loaded while this one is worked on
-    constexpr bool kMayOverflow = NV > 8;     // shorter rows hold fewer than 2^16 entries
+    constexpr int kWaves = TH / 64;
+    constexpr uint32_t kMagnitudes = 32 * TH, kLowest = TH == 1024 ? 0u : 0x2000u;     // counter c is of magnitude kLowest + c
+    __shared__ union { CountShared<TH> c; FilterShared f; } shared;
+    __shared__ uint32_t again[kMaxTurns / 32];                     // rows of this workgroup that are to be done over
+    CountShared<TH> &sh = shared.c;
+    constexpr bool kAhead = NV == 8 && TH == 1024;                 // the next row is loaded while this one is worked on
+    constexpr bool kMayOverflow = NV * TH > 8 * 1024;              // shorter rows hold fewer than 2^16 entries
     int tid = threadIdx.x;
     const int V = p.V;
     const uint16_t *logits = static_cast<const uint16_t *>(p.logits);
@@ -570,7 +574,7 @@ __global__ void __launch_bounds__(kFilterThreads) k_filter_counts(FilterProblem 
     // vector j of a row: entries 8 j - lead to 8 j - lead + 7, from the 16-byte boundary in front of it on
     auto lead_of = [&](int r) { return static_cast<int>((reinterpret_cast<uintptr_t>(logits + r * p.row_stride) & 15) / 2); };
     // (a wave's vectors are adjacent, so that entries of lower indices are in lower waves)
-    auto per_thread = [&](int lead) { return (lead + V + 8 * kFilterThreads - 1) / (8 * kFilterThreads); };
+    auto per_thread = [&](int lead) { return (lead + V + 8 * TH - 1) / (8 * TH); };
     auto load = [&](int r, U4 (&x)[NV]) {
         const int lead = lead_of(r), last = (lead + V - 1) / 8, j0 = (tid >> 6) * per_thread(lead) * 64 + (tid & 63);
         const U4 *vec = reinterpret_cast<const U4 *>(logits + r * p.row_stride - lead);
@@ -580,7 +584,15 @@ __global__ void __launch_bounds__(kFilterThreads) k_filter_counts(FilterProblem 
     auto clear = [&]() {
         U4 *c = reinterpret_cast<U4 *>(sh.count);
 #pragma unroll
-        for (int i = 0; i < (1 << 13) / kFilterThreads; ++i) c[i * kFilterThreads + tid] = U4{0, 0, 0, 0};
+        for (int i = 0; i < 8; ++i) c[i * TH + tid] = U4{0, 0, 0, 0};
+    };
+    // two entries' counters
+    auto counters = [&](uint32_t w) {
+        w &= 0x7FFF7FFFu;
+        if constexpr (TH == 1024) return w;
+        constexpr uint16_t last = kMagnitudes - 1;
+        const U2x16 x = __builtin_elementwise_sub_sat(__builtin_bit_cast(U2x16, w), U2x16{kLowest, kLowest});
+        return __builtin_bit_cast(uint32_t, __builtin_elementwise_min(x, U2x16{last, last}));
     };
 
     U4 row[NV], next[kAhead ? NV : 1];
@@ -589,7 +601,7 @@ __global__ void __launch_bounds__(kFilterThreads) k_filter_counts(FilterProblem 
     if (tid < kMaxTurns / 32) again[tid] = 0;
     load(r, row);
     clear();
-    if (tid == 0) { sh.counted = 0; sh.summed = 0; }
+    if (tid == 0) { sh.counted = 0; sh.summed = 0; sh.outside = 0; }
     sh.seg_weight[tid] = 0.0;
     sh.seg_count[tid] = 0;
     __syncthreads();
@@ -616,8 +628,9 @@ __global__ void __launch_bounds__(kFilterThreads) k_filter_counts(FilterProblem 
                 const uint32_t *w = &x.x;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    atomicAdd(&sh.count[w[i] & 0x7FFFu], (w[i] << 1 & 0x10000u) + 1u);
-                    atomicAdd(&sh.count[w[i] >> 16 & 0x7FFFu], (w[i] >> 15 & 0x10000u) + 1u);
+                    const uint32_t c = counters(w[i]);
+                    atomicAdd(&sh.count[c & 0xFFFFu], (w[i] << 1 & 0x10000u) + 1u);
+                    atomicAdd(&sh.count[c >> 16], (w[i] >> 15 & 0x10000u) + 1u);
                 }
             }
         }
@@ -628,18 +641,42 @@ __global__ void __launch_bounds__(kFilterThreads) k_filter_counts(FilterProblem 
                 const U4 x = reinterpret_cast<const U4 *>(logits + r * p.row_stride - lead)[lane < 8 ? 0 : vectors - 1];
                 const uint32_t e = logits[r * p.row_stride + i];
                 if (((x.x ^ kNegInf2) | (x.y ^ kNegInf2) | (x.z ^ kNegInf2) | (x.w ^ kNegInf2)) != 0) {
-                    atomicSub(&sh.count[e & 0x7FFFu], (e << 1 & 0x10000u) + 1u);
+                    atomicSub(&sh.count[counters(e) & 0xFFFFu], (e << 1 & 0x10000u) + 1u);
                     atomicSub(&sh.counted, 1u);
                 }
             }
         }
         __syncthreads();
+        if constexpr (TH < 1024) {
+            if ((sh.count[0] | sh.count[kMagnitudes - 1]) != 0) {  // uniform: of the row's entries, are these 0 and -inf?
+                uint32_t found = 0;
+#pragma unroll
+                for (int v = 0; v < NV; ++v) {
+                    __builtin_amdgcn_sched_barrier(0);
+                    if (v >= turns || j0 + 64 * v >= vectors) continue;
+                    const int i0 = 8 * (j0 + 64 * v) - lead;
+                    const uint32_t *w = &row[v].x;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const uint32_t e = w[i / 2] >> (i & 1) * 16 & 0xFFFFu, m = e & 0x7FFFu;
+                        const bool odd = m - kLowest - 1 >= kMagnitudes - 2 && m != 0 && e != 0xFF80u;
+                        found |= odd && i0 + i >= 0 && i0 + i < V ? 1u : 0u;
+                    }
+                }
+                if (__any(found != 0) && lane == 0) sh.outside = 1;
+            }
+        }
 
         // ---- which magnitudes occur: 32 a thread, its eight vectors in an order in which neighbours meet no bank twice
         auto split = [&](int m, uint32_t &pos, uint32_t &neg) {
             const uint32_t d = sh.count[m];
-            neg = m == 0 || m >= 0x7F80 ? 0u : d >> 16;            // (both zeros are one value; -inf and what is no number do not take part)
-            pos = m > 0x7F80 ? 0u : (m == 0x7F80 ? (d & 0xFFFFu) - (d >> 16) : (d & 0xFFFFu) - neg);
+            if constexpr (TH == 1024) {
+                neg = m == 0 || m >= 0x7F80 ? 0u : d >> 16;        // (both zeros are one value; -inf and what is no number do not take part)
+                pos = m > 0x7F80 ? 0u : (m == 0x7F80 ? (d & 0xFFFFu) - (d >> 16) : (d & 0xFFFFu) - neg);
+            } else {
+                neg = m == 0 || m == kMagnitudes - 1 ? 0u : d >> 16;
+                pos = m == kMagnitudes - 1 ? 0u : (d & 0xFFFFu) - neg;
+            }
         };
         {
             uint32_t any = 0, twice_above = 0, both = 0;
@@ -668,11 +705,11 @@ __global__ void __launch_bounds__(kFilterThreads) k_filter_counts(FilterProblem 
             }
         }
         __syncthreads();
-        const u64 occurs = lane < kFilterWaves ? sh.occurs[lane] : 0ull;
-        // the largest value: the highest segment with one above zero, else the first below; 0x8000 + magnitude, or 0x7FFF - magnitude
+        const u64 occurs = lane < kWaves ? sh.occurs[lane] : 0ull;
+        // the largest value: the highest segment with one above zero, else the first below; 0x8000 + counter, or 0x7FFF - counter
         uint32_t top = 0;
         {
-            u64 above = lane < kFilterWaves ? sh.above[lane] : 0ull;
+            u64 above = lane < kWaves ? sh.above[lane] : 0ull;
             if (lane == 0) above |= 1;                             // (zeros below zero alone do not show)
             while (top == 0) {
                 const u64 words = __ballot(above != 0);
@@ -700,7 +737,7 @@ __global__ void __launch_bounds__(kFilterThreads) k_filter_counts(FilterProblem 
                 if (lane == word) left &= ~(1ull << bit);
             }
         }
-        const bool overflow = kMayOverflow && sh.summed != sh.counted;       // uniform
+        const bool overflow = TH < 1024 ? sh.outside != 0 : kMayOverflow && sh.summed != sh.counted;       // uniform
         uint32_t cut_bits = 0xFF7Fu;                               // what is kept: larger values, and this one up to an index
         int cut_index = INT32_MAX, token = -1;
         if (overflow || top == 0) {                                // to be done over at the end, or no entries
@@ -708,30 +745,32 @@ __global__ void __launch_bounds__(kFilterThreads) k_filter_counts(FilterProblem 
             clear();
             if (overflow && tid == 0) again[nth_row / 32] |= 1u << nth_row % 32;
         } else {
-            const float top_z = __uint_as_float((top >= 0x8000u ? top - 0x8000u : 0x8000u | (0x7FFFu - top)) << 16);
+            // bits of the value of a counter
+            auto value_bits = [&](uint32_t c) { return TH == 1024 || c == 0 ? c : kLowest + c; };
+            const float top_z = __uint_as_float((top >= 0x8000u ? value_bits(top - 0x8000u) : 0x8000u | value_bits(0x7FFFu - top)) << 16);
             const double inv_t = 1.0 / static_cast<double>(asked.temperature), min_w = asked.min_p > 0.0f ? static_cast<double>(asked.min_p) : 0.0;
             auto weight = [&](uint32_t bits) {
                 const float z = __uint_as_float(bits << 16);
                 return z == top_z ? 1.0 : exp_of((static_cast<double>(z) - static_cast<double>(top_z)) * inv_t);
             };
-            // ---- counts and weights of the segments that hold something: segment n is wave n % 16's
+            // ---- counts and weights of the segments that hold something: segment n is wave n % kWaves's
 #pragma unroll 1
-            for (int half = 0; half < 2; ++half) {
-                u64 words = __ballot((occurs >> (2 * wave + 32 * half) & 1) != 0);
+            for (int set = 0; set < 32; set += kWaves) {
+                u64 words = __ballot((occurs >> (2 * (wave + set)) & 1) != 0);
 #pragma unroll 1
                 while (words) {
-                    const int word = __ffsll(static_cast<long long>(words)) - 1, at = word * 32 + wave + 16 * half;
+                    const int word = __ffsll(static_cast<long long>(words)) - 1, at = word * 32 + wave + set;
                     words &= words - 1;
                     uint32_t pos, neg;
                     split(at * 64 + lane, pos, neg);
-                    const double wp = weight(at * 64 + lane), wn = weight(0x8000u | (at * 64 + lane));
+                    const double wp = weight(value_bits(at * 64 + lane)), wn = weight(0x8000u | value_bits(at * 64 + lane));
                     if (!(wp >= min_w)) pos = 0;
                     if (!(wn >= min_w)) neg = 0;
                     const uint32_t cp = wave_inclusive_count(pos), cn = wave_inclusive_count(neg);
                     const double sp = wave_inclusive_sum(pos ? pos * wp : 0.0), sn = wave_inclusive_sum(neg ? neg * wn : 0.0);
                     if (lane == 63) {
-                        sh.seg_count[511 - at] = cp; sh.seg_weight[511 - at] = sp;
-                        sh.seg_count[512 + at] = cn; sh.seg_weight[512 + at] = sn;
+                        sh.seg_count[TH / 2 - 1 - at] = cp; sh.seg_weight[TH / 2 - 1 - at] = sp;
+                        sh.seg_count[TH / 2 + at] = cn; sh.seg_weight[TH / 2 + at] = sn;
                     }
                 }
             }
@@ -747,8 +786,8 @@ __global__ void __launch_bounds__(kFilterThreads) k_filter_counts(FilterProblem 
             // ---- places in the order: by count (top_k; or all, where what min_p leaves is asked for), by weight (top_p), and the draw.
             // One wave goes down from blocks to segments to values, 64 at a time; the others would only take its issue slots.
             if (wave == 0) {
-                const double block_w = wave_inclusive_sum(lane < kFilterWaves ? sh.wave_weight[lane & 15] : 0.0);
-                const uint32_t block_c = wave_inclusive_count(lane < kFilterWaves ? sh.wave_count[lane & 15] : 0u);
+                const double block_w = wave_inclusive_sum(lane < kWaves ? sh.wave_weight[lane & (kWaves - 1)] : 0.0);
+                const uint32_t block_c = wave_inclusive_count(lane < kWaves ? sh.wave_count[lane & (kWaves - 1)] : 0u);
                 const uint32_t all = __builtin_amdgcn_readlane(block_c, 63);
                 double total = lane_value(block_w, 63);
 
@@ -759,19 +798,19 @@ __global__ void __launch_bounds__(kFilterThreads) k_filter_counts(FilterProblem 
                         const u64 hit = __ballot(holds && (how == 0 ? c >= goal : (how == 1 ? w >= goal : w > goal))), some = __ballot(holds);
                         return hit ? __ffsll(static_cast<long long>(hit)) - 1 : 63 - __clzll(static_cast<long long>(some | 1));
                     };
-                    const int block = first(block_c, block_w, lane < kFilterWaves && sh.wave_count[lane & 15] != 0);
+                    const int block = first(block_c, block_w, lane < kWaves && sh.wave_count[lane & (kWaves - 1)] != 0);
                     double w0 = block ? lane_value(block_w, block - 1) : 0.0;
                     uint32_t c0 = block ? __builtin_amdgcn_readlane(block_c, block - 1) : 0u;
                     const double seg_w = sh.seg_weight[block * 64 + lane];
                     const uint32_t seg_c = sh.seg_count[block * 64 + lane], seg_before = lane ? sh.seg_count[block * 64 + lane - 1] : 0u;
                     const int seg = first(c0 + seg_c, w0 + seg_w, seg_c != seg_before), o = block * 64 + seg;
                     if (seg) { w0 += lane_value(seg_w, seg - 1); c0 += __builtin_amdgcn_readlane(seg_c, seg - 1); }
-                    const bool minus = o >= 512;
-                    const int at = minus ? o - 512 : 511 - o, m = at * 64 + (minus ? lane : 63 - lane);
+                    const bool minus = o >= TH / 2;
+                    const int at = minus ? o - TH / 2 : TH / 2 - 1 - o, m = at * 64 + (minus ? lane : 63 - lane);
                     uint32_t pos, neg;
                     split(m, pos, neg);
                     uint32_t n = minus ? neg : pos;
-                    const uint32_t bits = (minus ? 0x8000u : 0u) | m;
+                    const uint32_t bits = (minus ? 0x8000u : 0u) | value_bits(m);
                     const double w = weight(bits);
                     if (!(w >= min_w)) n = 0;
                     const double iw = w0 + wave_inclusive_sum(n ? n * w : 0.0);
@@ -863,7 +902,7 @@ __global__ void __launch_bounds__(kFilterThreads) k_filter_counts(FilterProblem 
                 const uint32_t run = wave_inclusive_count(mine);
                 if (lane == 63) sh.chunk[wave] = run;
                 __syncthreads();
-                const uint32_t before = wave_inclusive_count(lane < wave ? sh.chunk[lane & 15] : 0u), here = sh.chunk[wave];
+                const uint32_t before = wave_inclusive_count(lane < wave ? sh.chunk[lane & (kWaves - 1)] : 0u), here = sh.chunk[wave];
                 const uint32_t front = __builtin_amdgcn_readlane(before, 63);
                 if (front < nth && nth <= front + here) {          // one wave
                     uint32_t left = nth - front;
@@ -924,27 +963,27 @@ __global__ void __launch_bounds__(kFilterThreads) k_filter_counts(FilterProblem 
         if (!kAhead || after >= p.rows) break;
         r = after;
         ++nth_row;
-        if (tid == 0) { sh.counted = 0; sh.summed = 0; }
+        if (tid == 0) { sh.counted = 0; sh.summed = 0; sh.outside = 0; }
         if constexpr (kAhead) {
 #pragma unroll
             for (int v = 0; v < NV; ++v) row[v] = next[v];
         }
         __syncthreads();
     }
-    if constexpr (!kMayOverflow) return;
+    if constexpr (!kMayOverflow && TH == 1024) return;
     __syncthreads();
     for (int i = 0; i <= nth_row; ++i)
         if (again[i / 32] >> i % 32 & 1) {                         // uniform
-            filter_row<kFilterThreads, uint16_t>(p, blockIdx.x + i * gridDim.x, shared.f);
+            filter_row<TH, uint16_t>(p, blockIdx.x + i * gridDim.x, shared.f);
             __syncthreads();
         }
 }
 
-template <int NV>
+template <int NV, int TH>
 hipError_t launch_counts(const FilterProblem &p, hipStream_t stream)
 {
-    const int units = NV <= 8 ? compute_units() : p.rows, least = (p.rows + kMaxTurns - 1) / kMaxTurns, most = units > least ? units : least;
-    hipLaunchKernelGGL((k_filter_counts<NV>), dim3(p.rows < most ? p.rows : most), dim3(kFilterThreads), 0, stream, p);
+    const int units = NV == 8 && TH == 1024 ? compute_units() : p.rows, least = (p.rows + kMaxTurns - 1) / kMaxTurns, most = units > least ? units : least;
+    hipLaunchKernelGGL((k_filter_counts<NV, TH>), dim3(p.rows < most ? p.rows : most), dim3(TH), 0, stream, p);
     return hipGetLastError();
 }
 
@@ -953,13 +992,14 @@ hipError_t launch_counts(const FilterProblem &p, hipStream_t stream)
 hipError_t launch_filter(const FilterProblem &p, int dtype, hipStream_t stream)
 {
     const int64_t span = static_cast<int64_t>(p.V) + 7;            // entries with those in front of the row's first vector
-    if (dtype == 1 && span <= 8192) return launch_counts<1>(p, stream);
-    if (dtype == 1 && span <= 4 * 8192) return launch_counts<4>(p, stream);
-    if (dtype == 1 && span <= 8 * 8192) return launch_counts<8>(p, stream);
-    if (dtype == 1 && span <= 16 * 8192) return launch_counts<16>(p, stream);
-    if (dtype == 1 && span <= 20 * 8192) return launch_counts<20>(p, stream);
-    // A row a compute unit: 16 waves each; more: 8, so that two rows share a unit and one's waits are the other's work.
     const bool few = p.rows <= compute_units();
+    if (dtype == 1 && span <= 8 * 4096 && !few) return launch_counts<8, 512>(p, stream);
+    if (dtype == 1 && span <= 8192) return launch_counts<1, 1024>(p, stream);
+    if (dtype == 1 && span <= 4 * 8192) return launch_counts<4, 1024>(p, stream);
+    if (dtype == 1 && span <= 8 * 8192) return launch_counts<8, 1024>(p, stream);
+    if (dtype == 1 && span <= 16 * 8192) return launch_counts<16, 1024>(p, stream);
+    if (dtype == 1 && span <= 20 * 8192) return launch_counts<20, 1024>(p, stream);
+    // A row a compute unit: 16 waves each; more: 8, so that two rows share a unit and one's waits are the other's work.
     const dim3 grid(p.rows);
     if (dtype == 1 && few) hipLaunchKernelGGL((k_filter<1024, uint16_t>), grid, dim3(1024), 0, stream, p);
     else if (dtype == 1) hipLaunchKernelGGL((k_filter<512, uint16_t>), grid, dim3(512), 0, stream, p);

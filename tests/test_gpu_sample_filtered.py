@@ -218,3 +218,30 @@ def test_replays_of_a_captured_call():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(tok, t) and torch.equal(kept, kk)
+
+
+@pytest.mark.parametrize("V", [300, 8191, 32000])
+@pytest.mark.parametrize("kind", ["none", "top_p", "all"])
+def test_more_rows_than_compute_units(V, kind):
+    """Rows of a large batch, among them ones that hold very small and very large magnitudes, zeros of both signs, infinities,
+    numbers that are none, one value alone, and nothing."""
+    rng = np.random.default_rng(V)
+    R = 270
+    z = _rows(rng, R, V, head=50, masked=V // 100)
+    z[::5, 3] = 0.0
+    z[::5, 7] = -0.0
+    z[1, ::2] *= 1e-30
+    z[2, 5] = 2.0 ** -63
+    z[3, :] = 2.0 ** 65 * (1 + rng.random(V))
+    z[4, 9:20] = [2.0 ** 66, -2.0 ** 66, 2.0 ** 64, -2.0 ** 64, 1e38, -1e38, 2.0 ** -62, -2.0 ** -62, 2.0 ** -64, -2.0 ** -64, 1e-38]
+    z[6, 11] = np.inf
+    z[7, ::3] = np.nan
+    z[8, :] = -np.inf
+    z[9, :] = 0.0
+    z[11, :] = -np.inf
+    z[11, V // 2] = -3.0
+    z[12, :] = -rng.random(V) - 1
+    z[13, :] = -3.0e38
+    z[14, 0], z[14, V - 1] = -np.inf, 40.0
+    kw = _some(rng, R, kind)
+    _check(z, "bf16", "%s %d" % (kind, V), **kw)
