@@ -193,7 +193,6 @@ __global__ void __launch_bounds__(kAttendThreads, (Shape<T, DP>::waves(RT))) k_a
         if (share.part == 0 && head0 == 0 && block == 0 && threadIdx.x == 0) p.places[share.unit] = make_int2(share.at, share.parts);
     }
     const int unit = share.unit, part = share.part;
-    const bool last_part = PARTS && p.shared_len && part == share.parts - 1;           // takes the drafts' own keys, behind the shared ones, too
     const int first = unit * p.drafts;                        // its first sequence
     const int in_draft = p.tokens * p.group, rows = in_draft * p.drafts;
     const int row0 = block * p.block_rows + (WK == 4 ? 0 : wave * 16 * RT);
@@ -278,15 +277,16 @@ __global__ void __launch_bounds__(kAttendThreads, (Shape<T, DP>::waves(RT))) k_a
             fill_v[n] = static_cast<uint32_t>(row % kRun * p.v_token_stride + (ev < p.head_dim ? ev : 0)) * static_cast<uint32_t>(sizeof(T));
         }
     }
-    bool any = last_part;                                     // something may have been summed
+    // the drafts' own keys, behind the shared ones: the unit's parts take the drafts in turn, and so do their waves where they share the rows
+    const int last_row = min((block + 1) * p.block_rows, rows) - 1;
+    const int own_from = WK == 4 ? 4 * part : p.by_in_draft.div(block * p.block_rows) + part;
+    const int own_to = !PARTS || !p.shared_len ? 0 : (WK == 4 ? p.drafts : p.by_in_draft.div(last_row) + 1);    // (drafts with rows in this workgroup)
+    const int own_step = WK == 4 ? 4 * share.parts : share.parts;
+    bool any = own_from < own_to;                             // something may have been summed
     bool vast = false;                                        // a row of this wave has a reference beyond 2^20
 #pragma unroll 1
-    for (int seg = -1; seg < (last_part ? p.drafts : 0); seg = WK == 1 ? seg + 1 : (seg < 0 ? wave : seg + 4)) {
+    for (int seg = -1; seg < own_to; seg = seg < 0 ? own_from + (WK == 4 ? wave : 0) : seg + own_step) {
     const bool own = seg >= 0;                                // -1: what the unit's sequences share
-    if (WK == 1 && own) {                                     // drafts without rows in this workgroup
-        const int row = block * p.block_rows, last = min(row + p.block_rows, rows) - 1;
-        if (seg < p.by_in_draft.div(row) || seg > p.by_in_draft.div(last)) continue;
-    }
     const int step = WK == 4 && !own ? 4 * kKeys : kKeys;
     const int sequence = first + max(seg, 0);
     int row_low[RT], row_high[RT];
@@ -316,9 +316,10 @@ __global__ void __launch_bounds__(kAttendThreads, (Shape<T, DP>::waves(RT))) k_a
     }
     int start = lo_all >= hi_all ? 0 : lo_all / kKeys * kKeys, end = lo_all >= hi_all ? 0 : hi_all;
     if (PARTS && !own) {
-        // parts of the planned length, or longer ones where the sequence is longer than was planned for
+        // parts of the planned length, or longer ones where the sequence is longer than was planned for; with drafts' own keys, which come
+        // on top, of one length
         const int span = end - start, least = (span + share.parts - 1) / share.parts;
-        const int length = max(share.length, (least + kKeys - 1) / kKeys * kKeys);
+        const int length = max(p.shared_len ? 0 : share.length, (least + step - 1) / step * step);
         const int64_t at = start + static_cast<int64_t>(part) * length;
         start = static_cast<int>(min(at, static_cast<int64_t>(end)));
         end = static_cast<int>(min(at + length, static_cast<int64_t>(end)));
