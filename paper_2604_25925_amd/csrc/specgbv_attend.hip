@@ -946,10 +946,10 @@ hipError_t launch_dim(const AttendProblem &p, hipStream_t stream)
 
 }  // namespace
 
-AttendPlan plan_attend(int sequences, int drafts, bool shared, int tokens, int heads, int kv_heads, int head_dim, int window,
-                       int64_t longest)
+static AttendPlan plan_for(int sequences, int drafts, bool shared, int tokens, int heads, int kv_heads, int head_dim, int window, int64_t longest)
 {
     AttendPlan a{};
+    a.drafts = drafts; a.shared = shared;
     const int dp = head_dim <= 64 ? 64 : (head_dim <= 128 ? 128 : 256);
     const int rows = tokens * (heads / kv_heads) * drafts, tall = dp < 256 ? 32 : 16;
     // rows of a workgroup: a wave's, which all four share, or four waves' own ones, spread evenly over the workgroups
@@ -992,6 +992,21 @@ AttendPlan plan_attend(int sequences, int drafts, bool shared, int tokens, int h
     a.ml_bytes = (parts * sizeof(float2) + 255) / 256 * 256;
     a.bytes = a.places_bytes + a.ml_bytes + (parts * dp * sizeof(float) + 255) / 256 * 256;
     return a;
+}
+
+// Drafts that share short prefixes are sequences like others: what they have of their own would be most of the work, in units with rows
+// of many drafts, and a read once more comes from the L2 caches.  Shared / alone, us: 32 prefixes of 8 drafts, a token each (32 heads, 8 kv heads
+// of 128, bfloat16) 24 / 18 at 40 tokens, 25 / 23 at 160, 30 / 29 at 320, 27 / 43 at 640; 8 of 8, 9 tokens each, 31 / 26 at 40, 41 / 34 at 640,
+// 46 / 53 at 1280; one of 8, a token each (21 heads, 3 kv heads of 128, float32) 18 / 7 at 40, 26 / 16 at 1280, 26 / 25 at 2560.  The workspace is that of
+// either way, so that it does not hang on max_len.
+AttendPlan plan_attend(int sequences, int drafts, bool shared, int tokens, int heads, int kv_heads, int head_dim, int element_bytes, int window,
+                       int64_t longest)
+{
+    const AttendPlan plan = plan_for(sequences, drafts, shared, tokens, heads, kv_heads, head_dim, window, longest);
+    if (!shared || longest > 1024 || 2 * static_cast<int64_t>(sequences) * longest * kv_heads * head_dim * element_bytes > int64_t{128} << 20) return plan;
+    AttendPlan alone = plan_for(sequences, 1, false, tokens, heads, kv_heads, head_dim, window, longest);
+    if (alone.bytes < plan.bytes) alone.bytes = plan.bytes;
+    return alone;
 }
 
 hipError_t launch_attend(const AttendProblem &p, int dtype, hipStream_t stream)

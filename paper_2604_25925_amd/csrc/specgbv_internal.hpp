@@ -190,10 +190,11 @@ struct AttendProblem {
     Divider by_blocks, by_kv_heads, by_chunks, by_in_draft, by_group;
 };
 struct AttendPlan {
+    int drafts, shared;                          // of a unit; whether its drafts' shared keys are read once
     int units, all_parts, balanced, most_parts, own_keys, grain, chunks, chunk_keys, block_rows, row_blocks;
     size_t places_bytes, ml_bytes, bytes;        // bytes: 0 where nothing is to be joined
 };
-AttendPlan plan_attend(int sequences, int drafts, bool shared, int tokens, int heads, int kv_heads, int head_dim, int window,
+AttendPlan plan_attend(int sequences, int drafts, bool shared, int tokens, int heads, int kv_heads, int head_dim, int element_bytes, int window,
                        int64_t longest);
 hipError_t launch_attend(const AttendProblem &p, int dtype, hipStream_t stream);
 

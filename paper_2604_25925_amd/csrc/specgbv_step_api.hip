@@ -145,7 +145,7 @@ static AttendPlan plan_of(const specgbv_paged_cache &c, const specgbv_attend_arg
 {
     const bool shared = a.prefixes > 0;
     const int64_t held = static_cast<int64_t>(c.table_width) * c.page_size;
-    return plan_attend(c.sequences, shared ? c.sequences / a.prefixes : 1, shared, a.tokens, a.heads, c.kv_heads, c.head_dim, a.window,
+    return plan_attend(c.sequences, shared ? c.sequences / a.prefixes : 1, shared, a.tokens, a.heads, c.kv_heads, c.head_dim, element_bytes(c.dtype), a.window,
                        a.max_len > 0 && a.max_len < held ? a.max_len : held);
 }
 
@@ -179,14 +179,14 @@ specgbv_status specgbv_attend_paged(const specgbv_paged_cache *cache, const spec
     }
     AttendProblem p{};
     p.q = a.q; p.k = c.k; p.v = c.v; p.out = a.out; p.positions = a.positions;
-    p.shared_len = a.prefixes > 0 ? a.shared_len : nullptr;
+    p.shared_len = plan.shared ? a.shared_len : nullptr;
     p.map = page_map(c);
     for (int i = 0; i < 3; ++i) { p.q_stride[i] = a.q_stride[i]; p.out_stride[i] = a.out_stride[i]; }
     p.positions_stride = a.positions_stride;
     p.k_page_stride = static_cast<int32_t>(c.k_page_stride); p.k_head_stride = static_cast<int32_t>(c.k_head_stride);
     p.k_token_stride = static_cast<int32_t>(c.k_token_stride); p.v_page_stride = static_cast<int32_t>(c.v_page_stride);
     p.v_head_stride = static_cast<int32_t>(c.v_head_stride); p.v_token_stride = static_cast<int32_t>(c.v_token_stride);
-    if (plan.bytes > 0) {
+    if (plan.ml_bytes > 0) {
         char *ws = static_cast<char *>(workspace);
         p.places = reinterpret_cast<int2 *>(ws);
         p.ml = reinterpret_cast<float2 *>(ws + plan.places_bytes);
@@ -194,7 +194,7 @@ specgbv_status specgbv_attend_paged(const specgbv_paged_cache *cache, const spec
     }
     p.c = static_cast<float>((a.scale > 0.0f ? static_cast<double>(a.scale) : 1.0 / std::sqrt(static_cast<double>(c.head_dim))) * 1.4426950408889634074);
     p.sequences = c.sequences; p.tokens = a.tokens; p.heads = a.heads; p.kv_heads = c.kv_heads; p.group = a.heads / c.kv_heads;
-    p.head_dim = c.head_dim; p.drafts = a.prefixes > 0 ? c.sequences / a.prefixes : 1; p.window = a.window;
+    p.head_dim = c.head_dim; p.drafts = plan.drafts; p.window = a.window;
     p.units = plan.units; p.all_parts = plan.all_parts; p.balanced = plan.balanced; p.most_parts = plan.most_parts;
     p.own_keys = plan.own_keys; p.grain = plan.grain; p.chunks = plan.chunks; p.chunk_keys = plan.chunk_keys;
     p.block_rows = plan.block_rows; p.row_blocks = plan.row_blocks;

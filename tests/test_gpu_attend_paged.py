@@ -343,3 +343,42 @@ def test_many_parts_are_joined(dtype, D):
     """One sequence over the whole card, and one that is empty next to it: dozens of parts a row."""
     _run(2, 1, 2, 1, D, 16, dtype, 1500, positions=[[23999], [-1]])
     _run(1, 3, 5, 1, D, 16, dtype, 1100, positions=[[12, 17000, 17599]])
+
+
+@pytest.mark.parametrize("dtype,B,K,T,H,G,D,page", [("bf16", 2, 8, 1, 8, 2, 128, 16), ("f32", 2, 4, 1, 4, 1, 64, 32), ("bf16", 2, 2, 9, 8, 2, 128, 16),
+                                                    ("f32", 1, 3, 5, 14, 2, 64, 8), ("bf16", 2, 8, 9, 8, 2, 64, 64), ("f32", 1, 8, 9, 4, 1, 128, 16),
+                                                    ("bf16", 1, 5, 3, 2, 1, 256, 16), ("bf16", 1, 20, 9, 1, 1, 64, 8)])
+@pytest.mark.parametrize("window", [0, 1150])
+def test_drafts_that_share_long_prefixes(dtype, B, K, T, H, G, D, page, window):
+    """Beyond the lengths up to which drafts are taken by themselves: drafts of positions of their own, some without tokens of
+    their own, fewer tokens stated than are shared, pages that are not there."""
+    import torch
+    import paper_2604_25925_amd as sg
+    rng = np.random.default_rng(K * 100 + T)
+    width = 1 + 1400 // page
+    length = np.full((B, 1), width * page - 20 - T)
+    length[1:] = rng.integers(0, width * page - 20 - T, (B - 1, 1))
+    whole, S = length // page, B * K
+    table = rng.permutation(S * width).astype(np.int32).reshape(B, K, width)
+    table = np.where(np.arange(width) < whole[:, :, None], table[:, :1], table).reshape(S, width)
+    k, v, _ = make_cache(rng, S, width, page, G, D, dtype)
+    q = torch.from_numpy(rng.normal(0, 1.5, (S, T, H, D)).astype(np.float32)).cuda().to(torch_dtype(dtype))
+    pos = np.repeat(length, K, axis=0) + np.arange(T) + rng.integers(-3, 8, (S, 1))
+    pos[S - 1, 0], pos[0] = -1, whole[0] * page - T + np.arange(T)                 # (draft 0: nothing of its own)
+    pos, table = torch.from_numpy(pos.astype(np.int32)).cuda(), torch.from_numpy(table).cuda()
+    cache = sg.PagedCache(k, v, table)
+    for shared in (whole * page, whole * 0, np.maximum(whole * page - 5, 0)):
+        sl = torch.from_numpy(shared.reshape(B).astype(np.int32)).cuda()
+        out, ws = sg.specgbv_attend_paged(cache, q, pos, window=window, shared_len=sl)
+        ws.fill_(255)
+        out, _ = sg.specgbv_attend_paged(cache, q, pos, window=window, shared_len=sl, workspace=ws, out=out)
+        torch.cuda.synchronize()
+        check_attend(out, q, k, v, table, pos, dtype, window, label="shared")
+        near, _ = sg.specgbv_attend_paged(cache, q, pos, window=window, shared_len=sl, max_len=900, workspace=ws)      # taken by themselves
+        torch.cuda.synchronize()
+        check_attend(near, q, k, v, table, pos, dtype, window, label="alone")
+    own = int(whole[0, 0])                                   # a page that no draft shares; page 3 is gone for all
+    table[:K, 3], table[0, own], table[K - 1, own] = -1, k.shape[0], -5
+    out, _ = sg.specgbv_attend_paged(cache, q, pos, window=window, shared_len=sl, workspace=ws)
+    torch.cuda.synchronize()
+    check_attend(out, q, k, v, table, pos, dtype, window, label="pages")
