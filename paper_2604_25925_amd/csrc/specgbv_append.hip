@@ -14,7 +14,7 @@ namespace specgbv {
 namespace {
 
 constexpr int kAppendThreads = 256;
-constexpr int kAppendTokens = 4;              // tokens of a workgroup at most
+constexpr int kAppendTokens = 2;              // tokens of a workgroup at most
 constexpr int kAppendMaxPairs = 128;
 
 template <typename T, int W> struct alignas(sizeof(T) * W) Pack { T e[W]; };
@@ -180,7 +180,9 @@ hipError_t launch_append(const AppendProblem &given, int dtype, int width, hipSt
     const int units = p.head_dim / (2 * width);
     p.lane_bits = 0;
     while (p.lane_bits < 6 && (1 << p.lane_bits) < units) ++p.lane_bits;
-    p.block_tokens = p.tokens_all >= 4 * compute_units() ? kAppendTokens : 1;
+    // tokens of a workgroup, 1 / 2 / 4, us (32 heads, 8 kv heads of 128, bfloat16): 5.5 / 6.8 / 10.5 for 256 tokens, 8.2 / 9.0 / 12.2 for 1024,
+    // 13.2 / 12.9 / 16.0 for 2304, 82 / 77 / 79 for 20005
+    p.block_tokens = p.tokens_all >= 8 * compute_units() ? kAppendTokens : 1;
     if (dtype == 1) switch (width) {
         case 8: return launch_width<uint16_t, 8>(p, stream);
         case 4: return launch_width<uint16_t, 4>(p, stream);

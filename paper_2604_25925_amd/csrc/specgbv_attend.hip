@@ -48,7 +48,6 @@ template <typename T, int DP> struct Shape {
 };
 
 constexpr float kRaise = 8.0f;                // a reference is raised where a score is this far above it
-constexpr int kFewRows = 64;                  // up to here the waves of a workgroup share the rows, beyond they share the keys
 constexpr int kMaxParts = 256;                // partial sums of a row at most: a workgroup's threads
 
 template <typename T> __device__ __forceinline__ T rounded(float x);
@@ -918,13 +917,13 @@ hipError_t launch_rows(const AttendProblem &p, hipStream_t stream)
     const int rows = p.tokens * p.group * p.drafts;
     if (rows <= 16) return launch_one<T, DP, 1, 4, PARTS>(p, stream);
     constexpr int RT = DP < 256 ? 2 : 1;
-    return rows <= kFewRows ? launch_one<T, DP, RT, 4, PARTS>(p, stream) : launch_one<T, DP, RT, 1, PARTS>(p, stream);
+    return p.few ? launch_one<T, DP, RT, 4, PARTS>(p, stream) : launch_one<T, DP, RT, 1, PARTS>(p, stream);
 }
 
 template <typename T, int DP>
 hipError_t launch_typed(AttendProblem p, hipStream_t stream)
 {
-    p.in_order = Shape<T, DP>::kBf && p.tokens * p.group * p.drafts > kFewRows;
+    p.in_order = Shape<T, DP>::kBf && !p.few;
     if (p.all_parts == p.units && !p.ml) return launch_rows<T, DP, false>(p, stream);
     const hipError_t e = launch_rows<T, DP, true>(p, stream);
     if (e != hipSuccess) return e;
@@ -953,7 +952,13 @@ static AttendPlan plan_for(int sequences, int drafts, bool shared, int tokens, i
     const int dp = head_dim <= 64 ? 64 : (head_dim <= 128 ? 128 : 256);
     const int rows = tokens * (heads / kv_heads) * drafts, tall = dp < 256 ? 32 : 16;
     // rows of a workgroup: a wave's, which all four share, or four waves' own ones, spread evenly over the workgroups
-    if (rows <= kFewRows) a.block_rows = rows <= 16 ? 16 : tall;
+    // Up to here the waves of a workgroup share its rows and take the keys in turn; beyond they share the keys.  Sharing the rows keeps the keys out of
+    // LDS and needs no barrier, but each 32 rows load them again, and drafts' own keys meet all rows of a workgroup.  Shared rows / shared keys, us, bfloat16,
+    // 2 kv heads of 128: 16 sequences of up to 2048 tokens 24 / 29 at 144 rows, 27 / 40 at 256, 54 / 43 at 544; heads of 256: 42 / 38 at 72 rows, 57 / 47 at 144;
+    // prefixes of 8 drafts (8 kv heads) 46 / 52 at 96 rows, 92 / 74 at 288; of 4 drafts 61 / 52 at 144; float32, 8 sequences of up to 4096, 35 / 43 at 144, 139 / 86 at 544.
+    const int few_rows = dp == 256 ? 64 : (shared ? 128 : 256);
+    a.few = rows <= few_rows;
+    if (a.few) a.block_rows = rows <= 16 ? 16 : tall;
     else {
         const int blocks = (rows + 4 * tall - 1) / (4 * tall), waves = (rows + tall - 1) / tall;
         a.block_rows = (waves + blocks - 1) / blocks * tall;
@@ -963,10 +968,11 @@ static AttendPlan plan_for(int sequences, int drafts, bool shared, int tokens, i
     a.all_parts = a.units;
     if (window > 0) longest = longest < static_cast<int64_t>(window) + tokens ? longest : static_cast<int64_t>(window) + tokens;
     const int64_t base = static_cast<int64_t>(a.units) * kv_heads * a.row_blocks;
-    const int least = rows <= kFewRows ? 256 : 128;            // keys of a part
-    // workgroups on the card at once: registers leave room for two a compute unit; one in sixteen is left free, since a single workgroup
-    // that has to wait for a place doubles the launch
-    const int64_t slots = 2 * compute_units() * 15 / 16;
+    // Keys of a part at least.  One sequence of 1000 tokens, 8 heads on 2 kv heads, 128 / 256 / 512, us: 10.4 / 11.1 / 13.3 with one query; two of 20000
+    // 18.5 / 18.4 / 16.2.  With 36 rows more queries a kv head, 64 / 128 / 256: 12.9 / 14.6 / 18.4, and 20.7 / 19.5 / 21.2 for four of 4096.
+    const int least = a.few ? 256 : 128;
+    // workgroups on the card at once: registers leave room for two a compute unit (one: 8 prefixes of 8 drafts with 9 tokens each 126 us, 69 with two)
+    const int64_t slots = 2 * compute_units();
     int64_t chunks = slots / (base < 1 ? 1 : base);
     const int64_t most = (longest + least - 1) / least;
     if (chunks > most) chunks = most;
@@ -975,7 +981,7 @@ static AttendPlan plan_for(int sequences, int drafts, bool shared, int tokens, i
     if (chunks == 1 && !shared) return a;                      // one pass, nothing to join
     a.own_keys = shared ? drafts * 32 : 0;
     a.chunk_keys = least;
-    a.grain = rows <= kFewRows ? 128 : 32;
+    a.grain = a.few ? 128 : 32;                                // a tile for each wave that takes keys
     a.balanced = a.units <= 64 && (shared || tokens <= 64);
     if (a.balanced) {
         a.most_parts = static_cast<int>(slots / (static_cast<int64_t>(kv_heads) * a.row_blocks));

@@ -34,8 +34,8 @@ __device__ __forceinline__ double exp_of(double x)
 {
     x = fmax(x, -800.0);                                     // (below 2^-1074: 0)
     const double n = rint(x * 1.44269504088896340736);
-    double r = fma(n, -6.93147180369123816490e-01, x);       // the high bits of ln 2, then the rest
-    r = fma(n, -1.90821492927058770002e-10, r);
+    double r = fma(n, -0x1.62e42fefa2000p-1, x);            // ln 2 to 40 bits behind the point, whose products with n are exact, then the rest
+    r = fma(n, -0x1.9ef35793c7673p-41, r);
     double s = 1.0 / 479001600.0;
     s = fma(s, r, 1.0 / 39916800.0);
     s = fma(s, r, 1.0 / 3628800.0);
