@@ -33,6 +33,9 @@ typedef __bf16 B2 __attribute__((ext_vector_type(2)));
 
 constexpr int kAttendThreads = 256, kWavesPerGroup = 4;
 
+// Waves per SIMD, and so workgroups per compute unit, that the registers of a tile, its rows (16 RT) and their sums leave room for.
+constexpr int room_for(int DP, int element_bytes, int RT) { return DP == 256 || (element_bytes == 4 && DP == 128 && RT == 2) ? 1 : 2; }
+
 template <typename T, int DP> struct Shape {
     static constexpr bool kBf = sizeof(T) == 2;
     static constexpr int kKeys = kBf ? 32 : 16;              // of a tile
@@ -43,8 +46,7 @@ template <typename T, int DP> struct Shape {
     static constexpr int kVec = kBf ? (DP >= 128 ? 8 : 4) : 4;   // adjacent entries of a value that a lane takes
     static constexpr int kGroups = DP / (16 * kVec);         // such vectors per key
     static constexpr int kCols = kGroups * kVec;             // result tiles of 16 entries
-    // waves per SIMD that the registers of a tile, its rows and their sums leave room for
-    static constexpr int waves(int RT) { return DP == 256 || (!kBf && DP == 128 && RT == 2) ? 1 : 2; }
+    static constexpr int waves(int RT) { return room_for(DP, sizeof(T), RT); }
 };
 
 constexpr float kRaise = 8.0f;                // a reference is raised where a score is this far above it
@@ -945,7 +947,8 @@ hipError_t launch_dim(const AttendProblem &p, hipStream_t stream)
 
 }  // namespace
 
-static AttendPlan plan_for(int sequences, int drafts, bool shared, int tokens, int heads, int kv_heads, int head_dim, int window, int64_t longest)
+static AttendPlan plan_for(int sequences, int drafts, bool shared, int tokens, int heads, int kv_heads, int head_dim, int element_bytes, int window,
+                           int64_t longest)
 {
     AttendPlan a{};
     a.drafts = drafts; a.shared = shared;
@@ -971,8 +974,9 @@ static AttendPlan plan_for(int sequences, int drafts, bool shared, int tokens, i
     // Keys of a part at least.  One sequence of 1000 tokens, 8 heads on 2 kv heads, 128 / 256 / 512, us: 10.4 / 11.1 / 13.3 with one query; two of 20000
     // 18.5 / 18.4 / 16.2.  With 36 rows more queries a kv head, 64 / 128 / 256: 12.9 / 14.6 / 18.4, and 20.7 / 19.5 / 21.2 for four of 4096.
     const int least = a.few ? 256 : 128;
-    // workgroups on the card at once: registers leave room for two a compute unit (one: 8 prefixes of 8 drafts with 9 tokens each 126 us, 69 with two)
-    const int64_t slots = 2 * compute_units();
+    // Workgroups on the card at once.  One / two a compute unit, us: 8 prefixes of 8 drafts with 9 tokens each, 8 kv heads of 128, bfloat16 (room for two)
+    // 126 / 69; 16 sequences of up to 2048 tokens, 5 queries each of 16 heads on 4 kv heads of 256 (room for one) 33 / 40, and 33 / 43 in float32 of 128.
+    const int64_t slots = static_cast<int64_t>(compute_units()) * room_for(dp, element_bytes, a.block_rows == 16 || dp == 256 ? 1 : 2);
     int64_t chunks = slots / (base < 1 ? 1 : base);
     const int64_t most = (longest + least - 1) / least;
     if (chunks > most) chunks = most;
@@ -981,7 +985,7 @@ static AttendPlan plan_for(int sequences, int drafts, bool shared, int tokens, i
     if (chunks == 1 && !shared) return a;                      // one pass, nothing to join
     a.own_keys = shared ? drafts * 32 : 0;
     a.chunk_keys = least;
-    a.grain = a.few ? 128 : 32;                                // a tile for each wave that takes keys
+    a.grain = !a.few ? 32 : (element_bytes == 2 ? 128 : 64);   // a tile for each wave that takes keys
     a.balanced = a.units <= 64 && (shared || tokens <= 64);
     if (a.balanced) {
         a.most_parts = static_cast<int>(slots / (static_cast<int64_t>(kv_heads) * a.row_blocks));
@@ -1008,9 +1012,9 @@ static AttendPlan plan_for(int sequences, int drafts, bool shared, int tokens, i
 AttendPlan plan_attend(int sequences, int drafts, bool shared, int tokens, int heads, int kv_heads, int head_dim, int element_bytes, int window,
                        int64_t longest)
 {
-    const AttendPlan plan = plan_for(sequences, drafts, shared, tokens, heads, kv_heads, head_dim, window, longest);
+    const AttendPlan plan = plan_for(sequences, drafts, shared, tokens, heads, kv_heads, head_dim, element_bytes, window, longest);
     if (!shared || longest > 1024 || 2 * static_cast<int64_t>(sequences) * longest * kv_heads * head_dim * element_bytes > int64_t{128} << 20) return plan;
-    AttendPlan alone = plan_for(sequences, 1, false, tokens, heads, kv_heads, head_dim, window, longest);
+    AttendPlan alone = plan_for(sequences, 1, false, tokens, heads, kv_heads, head_dim, element_bytes, window, longest);
     if (alone.bytes < plan.bytes) alone.bytes = plan.bytes;
     return alone;
 }
