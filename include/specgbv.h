@@ -427,8 +427,8 @@ specgbv_status specgbv_read_sample_intermediates(
  * The cache.  Token t of sequence s lives in slot t % page_size of page table[s * table_stride + t / page_size]; element
  * (page, head, slot, i) of k is k[page * k_page_stride + head * k_head_stride + slot * k_token_stride + i], so a page may hold its
  * heads one after the other or its tokens; the same for v.  Strides are in elements.  Limits: head_dim a multiple of 8 up to 256,
- * page_size a multiple of 8, k and v 16-byte aligned with strides of whole 16 bytes, at most 2^30 tokens in a sequence
- * (offsets are 64-bit).  A table entry outside [0, pages) stands for a page that is not there: nothing is stored
+ * page_size a multiple of 8, k and v 16-byte aligned with strides of whole 16 bytes, tokens at most 2^26 elements apart, at most 2^30
+ * tokens in a sequence (offsets are 64-bit).  A table entry outside [0, pages) stands for a page that is not there: nothing is stored
  * to it and no query sees its tokens.
  */
 typedef struct {
@@ -476,8 +476,8 @@ specgbv_status specgbv_cache_append(const specgbv_paged_cache *cache, const spec
  *
  * Drafts of one prefix.  With prefixes > 0 the sequences are prefixes x drafts, a prefix's drafts next to each other, and
  * shared_len[b] states how many of its first tokens lie in the same pages for all its drafts (a number of whole pages, say): they
- * are read once for all drafts, through the first one's table row.  The tokens behind them are read per draft, by one workgroup
- * per kv head, so shared_len should leave few.
+ * are read once for all drafts, through the first one's table row (or, where they are short, per draft through its own).  The tokens behind
+ * them are read per draft, so shared_len should leave few.
  *
  * max_len is how far sequences reach at most, for the choice of the split alone (0: the table's width); the result does not
  * depend on it beyond rounding.
@@ -510,7 +510,9 @@ size_t specgbv_attend_workspace_bytes(const specgbv_paged_cache *cache, const sp
  * the token is the first kept entry up to and including which more than u times the kept weight lies (the last kept one where
  * rounding leaves none).  temperature <= 0 keeps the first entry alone.  A row without entries gets token -1 and keeps nothing;
  * where a logit is +inf, the entries at +inf weigh 1 and the others nothing.  NaN counts as -inf; min_p above 1 counts as 1.
- * Weights are float64, or fixed point of 43 fractional bits, in an order that does not change from call to call.
+ * Running weights are float64 sums in an order that does not change from call to call.  What is added up is float64 (bfloat16 rows of
+ * up to 163833 entries: counts times the weight of a value) or, in bins of 1/64 of an octave, integers: weights then are rounded to
+ * 2^-(7 + 64 - 2 c) of themselves, c the bits of V (2^-41 at V = 32003, 2^-35 at 152064).
  *
  *   logits       device, [rows, V], rows row_stride entries apart
  *   temperature, top_p, min_p   device, [rows] float32, or NULL (1, 1, 0);   top_k  device, [rows] int32, or NULL (0)

@@ -9,19 +9,29 @@
 // Rows.  A kv head's queries of one sequence (tokens x heads of its group), or of all drafts of a prefix while the keys lie in pages
 // that the drafts share, are the rows of a matrix product: one read of a key serves them all.  A wave holds 16 RT rows.
 //
-// A tile is 32 keys (bfloat16; 16 in float32) and never leaves registers.  The product is formed as keys x rows: in the
+// A tile is 32 keys (bfloat16; 16 in float32); where the waves of a workgroup share its rows it never leaves registers.  The product is formed as keys x rows: in the
 // result a lane holds scores of ONE row (lane % 16) and, because the product's row m is made key 8 (m / 4) + 4 h + m % 4 of the tile (h: which
 // half), of 8 ADJACENT keys, those of run lane / 16.  That is the layout in which the second product (values^T x weights) takes its
 // right operand, so the weights go from one product to the next without leaving their lane, and a lane loads the values of its own run
 // of keys: whole rows, each used entry by entry (two 16-bit halves put together by one byte permutation).  The order of entries within the
-// contraction over head_dim is free, so lanes take 16-byte pieces of keys.  Neither the keys nor the values pass through LDS,
-// and no barrier stands in the loop.
+// contraction over head_dim is free, so lanes take 16-byte pieces of keys.
 //
-// WK = 4: the waves of a workgroup take the tiles in turn and join at the end through LDS; 1: each wave has rows of its own, and the
-// waves share the tiles, which come into LDS by asynchronous loads two tiles ahead.  Straight into registers each 16-byte piece of a key is
+// WK = 4 (few rows): the waves of a workgroup take the tiles in turn and join at the end through LDS; neither the keys nor the values pass
+// through LDS, and no barrier stands in the loop.  1: each wave has rows of its own, and the
+// waves share the tiles, which come into LDS by asynchronous loads two tiles ahead, and the values are read turned.  Straight into registers each 16-byte piece of a key is
 // a line of its own for the cache (16 neighbouring lanes hold 16 rows), 750 accesses a tile, which bounded it with many rows; through LDS
 // neighbouring lanes load neighbouring pieces, once for four waves.  In LDS piece n of key m lies in slot n ^ m, so that 8 lanes that read one
 // piece of 8 keys meet 8 groups of banks.
+//
+// The split.  A unit (a sequence, or a prefix with its drafts) is cut into parts over its length, so that a launch fills the card once and all
+// workgroups have the same number of keys to read (share_of); k_attend_join brings the parts of a row to the largest reference.
+//
+// What bounds it, with times on one card (kernel, then join).  4 sequences of 131072 tokens, one query each of 32 heads on 8 kv heads of 128,
+// bfloat16: the reads, 2.14 GB in 356 + 5 us, 6.0 TB/s.  32 prefixes of up to 2048 tokens with 8 drafts: 49 + 7 us, 2.2 times the time of its 152 MB; half of it
+// is the start (lengths, positions, table, first tile: loads that wait for each other) and the drafts' own keys.  8 prefixes of up to 4096 tokens,
+// 8 drafts, 9 queries each: 61 + 11 us for 88 MB and 22 GFLOP; matrix instructions are under way for 45 % of the waves' time, the rest are waits for the
+// shared tiles with two waves per SIMD (registers leave no third), and the 48 MB of parts that are written and read.  24 float32 sequences, 5 queries of 14 heads on
+// 2 kv heads of 64, window 1000: 20 + 4 us against 2.7 for its bytes: latency of 4 tiles per wave.  One query: 5.7 us, all latency.
 #include "specgbv_internal.hpp"
 
 namespace specgbv {

@@ -5,6 +5,12 @@
 // that order, by rank or by running weight, and the row needs no sorting: a histogram says in which bin the place lies, and only that
 // bin's entries are put in order.
 //
+// What bounds it.  One row is a chain of passes and searches in one workgroup, and a workgroup's waits are covered only where two share a
+// compute unit.  bfloat16 (k_filter_counts): 256 rows of 128256 entries, tokens, 34.4 us (loads and counts 9, weights of the values that occur 5, places 3,
+// indices 4, launch and the spread of the loads over the card the rest; the bytes alone 13.6); 1152 rows of 32000, truncated rows, 59 us (30.5; 76 with one workgroup
+// a compute unit); one row of 32000 13.4.  float32 (k_filter): 287 rows of 32003, tokens and rows, 52 us (15.2): a row is read from memory for its
+// largest value (7), for the histogram (9, the additions in LDS), for each place that is looked for (4 - 5) and for the output.
+//
 // Weights decide which entry is drawn, and every entry counts, so they are held to more than float32: the histogram's sums are sums of
 // integers, which do not hang on the order of the additions, and running sums are float64 in a fixed order.
 #include "specgbv_internal.hpp"
@@ -993,13 +999,16 @@ hipError_t launch_filter(const FilterProblem &p, int dtype, hipStream_t stream)
 {
     const int64_t span = static_cast<int64_t>(p.V) + 7;            // entries with those in front of the row's first vector
     const bool few = p.rows <= compute_units();
+    // 16 / 8 waves, us, rows of 32000: 200 of them 15.7 / 16.1, 270 28 / 21, 1152 70 / 48.  Longer rows do not fit into the registers of two workgroups.
     if (dtype == 1 && span <= 8 * 4096 && !few) return launch_counts<8, 512>(p, stream);
-    if (dtype == 1 && span <= 8192) return launch_counts<1, 1024>(p, stream);
+    // The fewest vectors a lane that hold the row (more cost registers and turns).  With these / the next ones, 100 rows, us: 32000 entries 15.6 / 17.6, 64000
+    // 20.5 / 21.5 (600 rows, which load ahead, 60 / 63), 128256 28 / 32, 152064 36 / 77 (k_filter).
     if (dtype == 1 && span <= 4 * 8192) return launch_counts<4, 1024>(p, stream);
     if (dtype == 1 && span <= 8 * 8192) return launch_counts<8, 1024>(p, stream);
     if (dtype == 1 && span <= 16 * 8192) return launch_counts<16, 1024>(p, stream);
     if (dtype == 1 && span <= 20 * 8192) return launch_counts<20, 1024>(p, stream);
-    // A row a compute unit: 16 waves each; more: 8, so that two rows share a unit and one's waits are the other's work.
+    // A row a compute unit: 16 waves each; more: 8, so that two rows share a unit and one's waits are the other's work.  16 / 8 waves, us:
+    // float32 rows of 32003 entries, 64 of them 26 / 30, 256 33 / 38, 287 53 / 45, 1200 133 / 122; bfloat16 of 200000, 64 of them 90 / 119, 300 182 / 174.
     const dim3 grid(p.rows);
     if (dtype == 1 && few) hipLaunchKernelGGL((k_filter<1024, uint16_t>), grid, dim3(1024), 0, stream, p);
     else if (dtype == 1) hipLaunchKernelGGL((k_filter<512, uint16_t>), grid, dim3(512), 0, stream, p);
