@@ -520,7 +520,7 @@ size_t specgbv_attend_workspace_bytes(const specgbv_paged_cache *cache, const sp
  *   out_tokens   device out, [rows] int32, or NULL;   kept  device out, [rows, V] of the logits' type, rows kept_stride entries
  *                apart, or NULL: the logits of the kept entries, -inf elsewhere (may be logits itself)
  *   workspace    device, >= specgbv_filter_workspace_bytes(rows, V, dtype) bytes, 256-byte aligned (NULL where that is 0)
- *   rows >= 0, 1 <= V <= 1048576
+ *   0 <= rows < 2^22, 1 <= V <= 1048576
  */
 specgbv_status specgbv_sample_filtered(
     const void *logits, int64_t row_stride, int rows, int V, specgbv_dtype dtype,

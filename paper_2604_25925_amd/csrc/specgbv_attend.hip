@@ -163,10 +163,11 @@ __device__ __forceinline__ void load_to_lds(const void *base, uint32_t byte_offs
 }
 template <int N> __device__ __forceinline__ void wait_for_loads() { asm volatile("s_waitcnt vmcnt(%0)" : : "n"(N) : "memory"); }
 
-// A barrier that waits for nothing but the waves, and that no access to memory is moved across.
+// A barrier that waits for what has been read from LDS, so that it can be written to behind it, but for no load from memory, and that no access
+// to memory is moved across.
 __device__ __forceinline__ void meet()
 {
-    asm volatile("" ::: "memory");
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
 }
@@ -918,7 +919,7 @@ hipError_t launch_one(AttendProblem p, hipStream_t stream)
     p.items = p.all_parts * p.kv_heads;
     p.by_blocks = Divider::of(p.row_blocks);
     const int64_t grid = p.row_blocks == 1 ? p.items : static_cast<int64_t>((p.items + 7) / 8 * 8) * p.row_blocks;
-    if (grid > INT32_MAX) return hipErrorInvalidConfiguration;
+    if (grid >= INT64_C(1) << 24) return hipErrorInvalidConfiguration;        // (threads of a launch: below 2^32)
     hipLaunchKernelGGL((k_attend<T, DP, RT, WK, PARTS>), dim3(static_cast<unsigned>(grid)), dim3(kAttendThreads), 0, stream, p);
     return hipGetLastError();
 }

@@ -368,7 +368,7 @@ struct RowAsked {
     {
         temperature = p.temperature ? p.temperature[r] : 1.0f;
         top_p = p.top_p ? p.top_p[r] : 1.0f;
-        min_p = p.min_p ? fminf(p.min_p[r], 1.0f) : 0.0f;
+        min_p = p.min_p && p.min_p[r] > 0.0f ? fminf(p.min_p[r], 1.0f) : 0.0f;          // (what is no number: off)
         const int asked = p.top_k ? p.top_k[r] : 0;
         k = asked > 0 ? asked : INT32_MAX;
         if (!(temperature > 0.0f)) { temperature = 1.0f; k = 1; }
@@ -626,6 +626,15 @@ __global__ void __launch_bounds__(TH, 4) k_filter_counts(FilterProblem p)
         for (int v = 0; v < NV; ++v) {
             __builtin_amdgcn_sched_barrier(0);                     // (one vector at a time: registers)
             if (v >= turns) continue;                              // uniform
+            const int i0 = 8 * (j0 + 64 * v) - lead;
+            if (i0 < 0 || i0 + 8 > V) {                            // entries that are not the row's (a call in place may be writing them) are -inf
+                uint32_t *w = &row[v].x;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    if (i0 + 2 * i < 0 || i0 + 2 * i >= V) w[i] = (w[i] & 0xFFFF0000u) | 0xFF80u;
+                    if (i0 + 2 * i + 1 < 0 || i0 + 2 * i + 1 >= V) w[i] = (w[i] & 0xFFFFu) | 0xFF800000u;
+                }
+            }
             const U4 x = row[v];
             const bool some = j0 + 64 * v < vectors &&
                               ((x.x ^ kNegInf2) | (x.y ^ kNegInf2) | (x.z ^ kNegInf2) | (x.w ^ kNegInf2)) != 0;
@@ -641,17 +650,6 @@ __global__ void __launch_bounds__(TH, 4) k_filter_counts(FilterProblem p)
             }
         }
         if (lane == 0) atomicAdd(&sh.counted, 8 * counted);
-        if (wave == 0) {                                           // entries in front of the row and behind it are taken out again
-            const int i = lane < 8 ? lane - lead : V + lane - 8;   // (those of a vector of eight times -inf were not counted)
-            if (lane < 16 && (lane < 8 ? i < 0 : i < 8 * vectors - lead)) {
-                const U4 x = reinterpret_cast<const U4 *>(logits + r * p.row_stride - lead)[lane < 8 ? 0 : vectors - 1];
-                const uint32_t e = logits[r * p.row_stride + i];
-                if (((x.x ^ kNegInf2) | (x.y ^ kNegInf2) | (x.z ^ kNegInf2) | (x.w ^ kNegInf2)) != 0) {
-                    atomicSub(&sh.count[counters(e) & 0xFFFFu], (e << 1 & 0x10000u) + 1u);
-                    atomicSub(&sh.counted, 1u);
-                }
-            }
-        }
         __syncthreads();
         if constexpr (TH < 1024) {
             if ((sh.count[0] | sh.count[kMagnitudes - 1]) != 0) {  // uniform: of the row's entries, are these 0 and -inf?
@@ -660,13 +658,11 @@ __global__ void __launch_bounds__(TH, 4) k_filter_counts(FilterProblem p)
                 for (int v = 0; v < NV; ++v) {
                     __builtin_amdgcn_sched_barrier(0);
                     if (v >= turns || j0 + 64 * v >= vectors) continue;
-                    const int i0 = 8 * (j0 + 64 * v) - lead;
                     const uint32_t *w = &row[v].x;
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
                         const uint32_t e = w[i / 2] >> (i & 1) * 16 & 0xFFFFu, m = e & 0x7FFFu;
-                        const bool odd = m - kLowest - 1 >= kMagnitudes - 2 && m != 0 && e != 0xFF80u;
-                        found |= odd && i0 + i >= 0 && i0 + i < V ? 1u : 0u;
+                        found |= m - kLowest - 1 >= kMagnitudes - 2 && m != 0 && e != 0xFF80u ? 1u : 0u;
                     }
                 }
                 if (__any(found != 0) && lane == 0) sh.outside = 1;
@@ -893,10 +889,7 @@ __global__ void __launch_bounds__(TH, 4) k_filter_counts(FilterProblem p)
                         const uint32_t d = (w[i] ^ pair) & care;
                         m |= ((d & 0xFFFFu) == 0 ? 1u : 0u) << (2 * i) | (d >> 16 == 0 ? 2u : 0u) << (2 * i);
                     }
-                    const int i0 = 8 * (j1 + 64 * v) - lead;
-                    if (i0 < 0) m &= 0xFFu << -i0;
-                    if (i0 + 8 > V) m &= i0 < V ? 0xFFu >> (i0 + 8 - V) : 0u;
-                    return m;
+                    return j1 + 64 * v < vectors ? m : 0u;         // (behind the row: its last vector again)
                 };
                 uint32_t mine = 0;
 #pragma unroll

@@ -229,6 +229,7 @@ specgbv_status specgbv_sample_filtered(
     if (rows < 0 || V < 1) return fail(SPECGBV_EINVAL, "sizes must satisfy rows >= 0, V >= 1 (got rows=%d V=%d)", rows, V);
     if (dtype != SPECGBV_F32 && dtype != SPECGBV_BF16) return fail(SPECGBV_EINVAL, "unknown dtype %d", (int)dtype);
     if (V > (1 << 20)) return fail(SPECGBV_EUNSUPPORTED, "V=%d exceeds 1048576", V);
+    if (rows >= 1 << 22) return fail(SPECGBV_EUNSUPPORTED, "rows=%d exceeds 2^22 - 1", rows);
     if (rows == 0) return SPECGBV_OK;
     if (!logits || (!out_tokens && !kept) || (out_tokens && !u)) return fail(SPECGBV_EINVAL, "null input or output pointer");
     if (rows > 1 && (row_stride < V || (kept && kept_stride < V))) return fail(SPECGBV_EINVAL, "a row stride is less than V=%d", V);
@@ -236,12 +237,7 @@ specgbv_status specgbv_sample_filtered(
     if (!aligned(logits, esz) || !aligned(kept, esz) || !aligned(temperature, 4) || !aligned(top_k, 4) || !aligned(top_p, 4) ||
         !aligned(min_p, 4) || !aligned(u, 4) || !aligned(out_tokens, 4))
         return fail(SPECGBV_EINVAL, "pointer not aligned to its element size");
-    const size_t need = specgbv_filter_workspace_bytes(rows, V, dtype);
-    if (need > 0) {
-        if (!workspace) return fail(SPECGBV_EWORKSPACE, "workspace is null (need %zu bytes)", need);
-        if (!aligned(workspace, 256)) return fail(SPECGBV_EWORKSPACE, "workspace must be 256-byte aligned");
-        if (workspace_bytes < need) return fail(SPECGBV_EWORKSPACE, "workspace has %zu bytes, need %zu", workspace_bytes, need);
-    }
+    (void)workspace; (void)workspace_bytes;                   // (none is needed)
     const FilterProblem p{logits, kept, row_stride, kept_stride, temperature, top_p, min_p, u, top_k, out_tokens, rows, V};
     const hipError_t e = launch_filter(p, dtype == SPECGBV_BF16 ? 1 : 0, static_cast<hipStream_t>(hip_stream));
     if (e != hipSuccess) return fail(SPECGBV_EHIP, "filter kernel launch: %s", hipGetErrorString(e));

@@ -218,3 +218,9 @@ def test_places_of_tokens_with_bad_pages(tmp_path):
                    check=True)
     r = subprocess.run([str(tmp_path / "places")], capture_output=True, text=True, env=dict(os.environ, LD_PRELOAD=""))
     assert r.returncode == 0 and r.stdout.strip() == "ok", r.stdout + r.stderr
+
+
+def test_filter_refuses_more_rows_than_a_launch_holds():
+    lib = sg.load_library()
+    assert lib.specgbv_sample_filtered(P, 100, 1 << 22, 100, 1, None, None, None, None, P, P, None, 100, None, 0, None) == 2
+    assert "rows" in sg.specgbv_last_error()

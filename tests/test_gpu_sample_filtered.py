@@ -245,3 +245,26 @@ def test_more_rows_than_compute_units(V, kind):
     z[14, 0], z[14, V - 1] = -np.inf, 40.0
     kw = _some(rng, R, kind)
     _check(z, "bf16", "%s %d" % (kind, V), **kw)
+
+
+@pytest.mark.parametrize("V", [1001, 8190, 32003, 40001])
+def test_many_odd_rows_in_place(V):
+    """Rows whose first and last 16 bytes hold a neighbour's entries, which the neighbour's workgroup overwrites meanwhile."""
+    import torch
+    import paper_2604_25925_amd as sg
+    R = min(3000, 40_000_000 // V)
+    gen = torch.Generator(device="cuda").manual_seed(V)
+    z = (torch.randn((R, V), generator=gen, device="cuda") * 3).bfloat16()
+    u = torch.rand(R, generator=gen, device="cuda")
+    kw = dict(top_p=torch.full((R,), 0.9, device="cuda"), top_k=torch.full((R,), 300, dtype=torch.int32, device="cuda"))
+    tokens, kept, _ = sg.specgbv_sample_filtered(z, u, keep=True, **kw)
+    for _ in range(3):
+        x = z.clone()
+        mine, _, _ = sg.specgbv_sample_filtered(x, u, keep=True, kept=x, **kw)
+        assert torch.equal(mine, tokens) and torch.equal(x, kept)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_a_min_p_that_is_no_number_is_off(dtype):
+    rng = np.random.default_rng(4)
+    _check(_rows(rng, 3, 2000, head=20), dtype, "nan", min_p=[np.nan, 0.05, -np.inf], u=rng.random(3).astype(np.float32))
