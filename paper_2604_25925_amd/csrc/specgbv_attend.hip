@@ -788,11 +788,10 @@ struct JoinRow {
     int draft, s, t, h, parts;
     int64_t part0, between;
 
-    __device__ __forceinline__ JoinRow(const AttendProblem &p, int64_t at)
+    __device__ __forceinline__ JoinRow(const AttendProblem &p, int at)
     {
-        const int rows = p.tokens * p.group * p.drafts;
-        const int64_t pair = at / rows;
-        const int row = static_cast<int>(at - pair * rows), unit = p.by_kv_heads.div(static_cast<int>(pair)), head0 = p.by_kv_heads.mod(static_cast<int>(pair), unit);
+        const int rows = p.tokens * p.group * p.drafts, pair = p.by_rows.div(at), row = p.by_rows.mod(at, pair);
+        const int unit = p.by_kv_heads.div(pair), head0 = p.by_kv_heads.mod(pair, unit);
         draft = p.by_in_draft.div(row);
         const int in = p.by_in_draft.mod(row, draft);
         s = unit * p.drafts + draft; t = p.by_group.div(in); h = head0 * p.group + p.by_group.mod(in, t);
@@ -817,8 +816,8 @@ __global__ void __launch_bounds__(kAttendThreads) k_attend_join(AttendProblem p)
 {
     constexpr int kLanes = DP / 4, kAhead = 4;
     const int vec = threadIdx.x % kLanes;
-    const int64_t at = static_cast<int64_t>(blockIdx.x) * (kAttendThreads / kLanes) + threadIdx.x / kLanes;
-    if (at >= static_cast<int64_t>(p.sequences) * p.heads * p.tokens) return;          // whole groups of lanes
+    const int at = blockIdx.x * (kAttendThreads / kLanes) + threadIdx.x / kLanes;     // (fewer than 2^30 rows)
+    if (at >= p.sequences * p.heads * p.tokens) return;                               // whole groups of lanes
     const JoinRow row(p, at);
     const int pos = p.positions[row.s * p.positions_stride + row.t];
     const F4 *acc_of = reinterpret_cast<const F4 *>(p.acc) + vec;

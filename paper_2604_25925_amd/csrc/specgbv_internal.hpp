@@ -187,7 +187,7 @@ struct AttendProblem {
     int q_wide, out_wide;          // 16-byte loads of q, stores of whole vectors to out
     int few, in_order;             // in_order: partial sums are held in the entries' order (this and the next are set by the launches)
     int items;
-    Divider by_blocks, by_kv_heads, by_chunks, by_in_draft, by_group;
+    Divider by_blocks, by_kv_heads, by_chunks, by_in_draft, by_group, by_rows;
 };
 struct AttendPlan {
     int drafts, shared;                          // of a unit; whether its drafts' shared keys are read once

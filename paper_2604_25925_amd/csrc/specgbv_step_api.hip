@@ -202,6 +202,7 @@ specgbv_status specgbv_attend_paged(const specgbv_paged_cache *cache, const spec
     p.by_chunks = Divider::of(plan.chunks > 0 ? plan.chunks : 1);
     p.by_in_draft = Divider::of(p.tokens * p.group);
     p.by_group = Divider::of(p.group);
+    p.by_rows = Divider::of(p.tokens * p.group * p.drafts);
     const int unit = static_cast<int>(16 / esz);
     p.q_wide = allowed_width(unit, a.q, a.q_stride, 3, esz) == unit;
     p.out_wide = allowed_width(unit, a.out, a.out_stride, 3, esz) == unit;

@@ -53,29 +53,31 @@ class PagedCache:
         self.k, self.v, self.table = k, v, table
         self.pages, self.kv_heads, self.page_size, self.head_dim = k.shape
         self.sequences, self.width = table.shape
-        self.dtype, self.device = k.dtype, k.device
+        self.dtype, self.device, self._index = k.dtype, k.device, k.get_device()
         ks, vs = k.stride(), v.stride()
         self._c = _CACHE.pack(k.data_ptr(), v.data_ptr(), table.data_ptr(), ks[0], ks[1], ks[2], vs[0], vs[1], vs[2],
                               max(table.stride(0), self.width), self.pages, self.kv_heads, self.page_size, self.head_dim,
                               self.sequences, self.width, _DTYPES[k.dtype], 0)
 
     def _heads(self, name, x, heads=None):
-        """Strides of x [sequences, tokens, heads, head_dim]."""
-        if x.dim() != 4 or x.shape[0] != self.sequences or x.shape[3] != self.head_dim or (heads is not None and x.shape[2] != heads):
+        """Tokens, heads and strides of x [sequences, tokens, heads, head_dim]."""
+        shape = x.shape
+        if len(shape) != 4 or shape[0] != self.sequences or shape[3] != self.head_dim or (heads is not None and shape[2] != heads):
             raise ValueError("%s must be [%d, tokens, %s, %d], got %s" %
-                             (name, self.sequences, "heads" if heads is None else heads, self.head_dim, tuple(x.shape)))
+                             (name, self.sequences, "heads" if heads is None else heads, self.head_dim, tuple(shape)))
         if x.dtype is not self.dtype:
             raise TypeError("%s must be %s as the cache is, got %s" % (name, self.dtype, x.dtype))
-        if x.device != self.device:
+        if x.get_device() != self._index:
             raise ValueError("%s must live on the cache's GPU" % name)
         s = x.stride()
         if s[3] != 1:
             raise ValueError("the last dimension of %s must be dense" % name)
-        return s
+        return shape[1], shape[2], s
 
     def _positions(self, positions, tokens):
-        if positions.dim() != 2 or positions.shape[0] != self.sequences or positions.shape[1] != tokens or \
-                positions.dtype is not torch.int32 or positions.device != self.device:
+        shape = positions.shape
+        if len(shape) != 2 or shape[0] != self.sequences or shape[1] != tokens or positions.dtype is not torch.int32 or \
+                positions.get_device() != self._index:
             raise ValueError("positions must be int32 [%d, %d] on the cache's GPU" % (self.sequences, tokens))
         s = positions.stride()
         if tokens > 1 and s[1] != 1:
@@ -89,16 +91,16 @@ def specgbv_cache_append(cache: PagedCache, q, k, v, positions, *, inv_freq=None
     k_weight [D] are given) and rotated by positions [S, T] * inv_freq (float64, [pairs]; entries behind 2 * pairs stay); k and v
     go to the cache.  Positions below 0 are padding.  Returns the rotated queries (`out`; q itself may be given)."""
     lib = load_library()
-    qs = cache._heads("q", q)
-    T, H = q.shape[1], q.shape[2]
-    ks, vs = cache._heads("k", k, cache.kv_heads), cache._heads("v", v, cache.kv_heads)
-    if k.shape[1] != T or v.shape[1] != T:
-        raise ValueError("q, k and v must have the same tokens, got %d, %d and %d" % (T, k.shape[1], v.shape[1]))
+    T, H, qs = cache._heads("q", q)
+    tk, _, ks = cache._heads("k", k, cache.kv_heads)
+    tv, _, vs = cache._heads("v", v, cache.kv_heads)
+    if tk != T or tv != T:
+        raise ValueError("q, k and v must have the same tokens, got %d, %d and %d" % (T, tk, tv))
     ps = cache._positions(positions, T)
     if out is None:
         out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    os = cache._heads("out", out, H)
-    if out.shape[1] != T:
+    to, _, os = cache._heads("out", out, H)
+    if to != T:
         raise ValueError("out must have the shape of q")
     for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
         if w is not None and (w.dim() != 1 or w.shape[0] != cache.head_dim or w.dtype is not cache.dtype or
@@ -117,7 +119,7 @@ def specgbv_cache_append(cache: PagedCache, q, k, v, positions, *, inv_freq=None
     return out
 
 
-def _attend_args(cache, q, qs, out_ptr, os, positions_ptr, ps, window, shared_len, max_len, scale):
+def _attend_args(cache, q, qs, tokens, heads, out_ptr, os, positions_ptr, ps, window, shared_len, max_len, scale):
     prefixes = 0
     if shared_len is not None:
         if shared_len.dim() != 1 or shared_len.dtype is not torch.int32 or shared_len.device != cache.device or \
@@ -127,14 +129,13 @@ def _attend_args(cache, q, qs, out_ptr, os, positions_ptr, ps, window, shared_le
         if prefixes == 0 and cache.sequences:
             raise ValueError("%d sequences are not drafts of 0 prefixes" % cache.sequences)
     return _ATTEND.pack(q.data_ptr(), out_ptr, positions_ptr, shared_len.data_ptr() if prefixes else 0,
-                        qs[0], qs[1], qs[2], os[0], os[1], os[2], ps, q.shape[1], q.shape[2], window, prefixes, max_len or 0, scale or 0.0)
+                        qs[0], qs[1], qs[2], os[0], os[1], os[2], ps, tokens, heads, window, prefixes, max_len or 0, scale or 0.0)
 
 
 def specgbv_attend_workspace_bytes(cache: PagedCache, q, *, window: int = 0, shared_len=None, max_len: Optional[int] = None) -> int:
-    qs = cache._heads("q", q)
-    T = q.shape[1]
+    T, H, qs = cache._heads("q", q)
     return int(load_library().specgbv_attend_workspace_bytes(
-        cache._c, _attend_args(cache, q, qs, 0, (0, 0, 0), 0, T, window, shared_len, max_len, None)))
+        cache._c, _attend_args(cache, q, qs, T, H, 0, (0, 0, 0), 0, T, window, shared_len, max_len, None)))
 
 
 def specgbv_attend_paged(cache: PagedCache, q, positions, *, window: int = 0, shared_len=None, max_len: Optional[int] = None,
@@ -145,15 +146,14 @@ def specgbv_attend_paged(cache: PagedCache, q, positions, *, window: int = 0, sh
     share: those are read once per prefix.  max_len: how far sequences reach at most, for the choice of the split.  Returns
     (out [S, T, heads, D], workspace)."""
     lib = load_library()
-    qs = cache._heads("q", q)
-    T, H = q.shape[1], q.shape[2]
+    T, H, qs = cache._heads("q", q)
     ps = cache._positions(positions, T)
     if out is None:
         out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    os = cache._heads("out", out, H)
-    if out.shape[1] != T:
+    to, _, os = cache._heads("out", out, H)
+    if to != T:
         raise ValueError("out must have the shape of q")
-    args = _attend_args(cache, q, qs, out.data_ptr(), os, positions.data_ptr(), ps, window, shared_len, max_len, scale)
+    args = _attend_args(cache, q, qs, T, H, out.data_ptr(), os, positions.data_ptr(), ps, window, shared_len, max_len, scale)
     if workspace is None:
         need = int(lib.specgbv_attend_workspace_bytes(cache._c, args))
         workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=cache.device)
