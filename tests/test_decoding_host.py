@@ -180,8 +180,8 @@ int main()
             if (q != n / d || v.mod((int)n, q) != n %% d) return bad("quotient", n, d);
         }
     }
-    // tables with pages that are not there: the table is read inside its bounds only (it is as long as it says, so a checker of
-    // addresses sees a read behind it), and a place is inside the cache or none
+    // tables with pages that are not there: the table is read inside its bounds only (it is as long as it says, so a sanitizer
+    // sees a read behind it), and a place is inside the cache or none
     for (int round = 0; round < 300; ++round) {
         const int page = 8 * (1 + std::rand() %% 20), width = 1 + std::rand() %% 9, S = 1 + std::rand() %% 4, pages = 1 + std::rand() %% 12, stride = width + std::rand() %% 3;
         std::vector<int32_t> table((S - 1) * stride + width);
