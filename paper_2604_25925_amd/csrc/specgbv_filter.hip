@@ -6,9 +6,9 @@
 // bin's entries are put in order.
 //
 // What bounds it.  One row is a chain of passes and searches in one workgroup, and a workgroup's waits are covered only where two share a
-// compute unit.  bfloat16 (k_filter_counts): 256 rows of 128256 entries, tokens, 34.4 us (loads and counts 9, weights of the values that occur 5, places 3,
-// indices 4, launch and the spread of the loads over the card the rest; the bytes alone 13.6); 1152 rows of 32000, truncated rows, 59 us (30.5; 76 with one workgroup
-// a compute unit); one row of 32000 13.4.  float32 (k_filter): 287 rows of 32003, tokens and rows, 52 us (15.2): a row is read from memory for its
+// compute unit.  bfloat16 (k_filter_counts): 256 rows of 128256 entries, tokens, 33.6 us (loads and counts 9, weights of the values that occur 5, places 3,
+// indices 4, launch and the spread of the loads over the card the rest; the bytes alone 13.6); 1152 rows of 32000, truncated rows, 57 us (30.5; 76 with one workgroup
+// a compute unit); one row of 32000 13.2.  float32 (k_filter): 287 rows of 32003, tokens and rows, 52 us (15.2): a row is read from memory for its
 // largest value (7), for the histogram (9, the additions in LDS), for each place that is looked for (4 - 5) and for the output.
 //
 // Weights decide which entry is drawn, and every entry counts, so they are held to more than float32: the histogram's sums are sums of
@@ -35,7 +35,7 @@ constexpr uint32_t kNothing = 0x007FFFFFu;    // key of -inf
 // The value of a key that bounds others from above: -0 has a key of its own, which no entry has, and equals the 0 above it.
 __device__ __forceinline__ float bound_of(uint32_t k) { return value_of(k == 0x7FFFFFFFu ? k - 1 : k); }
 
-// e^x for x <= 0 in float64: 2^n times the Taylor sum of e^r, |r| <= ln(2) / 2, to r^12 / 12!, whose remainder is 2 10^-16 of it.
+// e^x for x <= 1 in float64: 2^n times the Taylor sum of e^r, |r| <= ln(2) / 2, to r^12 / 12!, whose remainder is 2 10^-16 of it.
 __device__ __forceinline__ double exp_of(double x)
 {
     x = fmax(x, -800.0);                                     // (below 2^-1074: 0)
@@ -56,6 +56,23 @@ __device__ __forceinline__ double exp_of(double x)
     s = fma(s, r, 1.0);
     s = fma(s, r, 1.0);
     return ldexp(s, static_cast<int>(n));
+}
+
+// The same with 2^(j / 64), j < 64, at hand: the Taylor sum of what is left, at most ln(2) / 128, to r^5 / 5!, whose remainder is 4 10^-17 of it.
+__device__ __forceinline__ double exp_from(const double *of_octave, double x)
+{
+    x = fmax(x, -800.0);
+    const double n = rint(x * 92.33248261689366);
+    double r = fma(n, -0x1.62e42fefa0000p-7, x);            // ln(2) / 64 to 42 bits behind the point, whose products with n are exact, then the rest
+    r = fma(n, -0x1.cf79abc9e3b3ap-46, r);
+    double s = 1.0 / 120.0;
+    s = fma(s, r, 1.0 / 24.0);
+    s = fma(s, r, 1.0 / 6.0);
+    s = fma(s, r, 0.5);
+    s = fma(s, r, 1.0);
+    s = fma(s, r, 1.0);
+    const int k = static_cast<int>(n);
+    return ldexp(of_octave[k & 63] * s, k >> 6);
 }
 
 // How the entries of a row are weighed and binned.  With y = 64 log2(e) (z - top) / T, a weight is 2^(y / 64) = 2^(-bin / 64) (1 + d), bin the
@@ -539,6 +556,7 @@ constexpr int kMaxTurns = 8192;               // rows of a workgroup at most
 // A row with other entries than these (and 0 and -inf) is done by filter_row.
 template <int TH> struct CountShared {
     uint32_t count[32 * TH];
+    double of_octave[64];                     // 2^(j / 64)
     // of the segments of 64 values: TH / 2 of magnitudes from the top down, then TH / 2 below zero from 0 down
     double seg_weight[TH];                    // running sums within blocks of 64 segments
     uint32_t seg_count[TH];
@@ -610,6 +628,7 @@ __global__ void __launch_bounds__(TH, 4) k_filter_counts(FilterProblem p)
     if (tid == 0) { sh.counted = 0; sh.summed = 0; sh.outside = 0; }
     sh.seg_weight[tid] = 0.0;
     sh.seg_count[tid] = 0;
+    if (tid >= TH - 64) sh.of_octave[tid - (TH - 64)] = exp_of((tid - (TH - 64)) * 0.010830424696249145);      // ln(2) / 64
     __syncthreads();
     for (;;) {
         if constexpr (kAhead) asm volatile("" : "+v"(tid));        // (what follows from it is made anew: kept over rows it would cost the registers)
@@ -753,7 +772,7 @@ __global__ void __launch_bounds__(TH, 4) k_filter_counts(FilterProblem p)
             const double inv_t = 1.0 / static_cast<double>(asked.temperature), min_w = asked.min_p > 0.0f ? static_cast<double>(asked.min_p) : 0.0;
             auto weight = [&](uint32_t bits) {
                 const float z = __uint_as_float(bits << 16);
-                return z == top_z ? 1.0 : exp_of((static_cast<double>(z) - static_cast<double>(top_z)) * inv_t);
+                return z == top_z ? 1.0 : exp_from(sh.of_octave, (static_cast<double>(z) - static_cast<double>(top_z)) * inv_t);
             };
             // ---- counts and weights of the segments that hold something: segment n is wave n % kWaves's
 #pragma unroll 1
