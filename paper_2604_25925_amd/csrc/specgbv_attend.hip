@@ -16,7 +16,7 @@
 // of keys: whole rows, each used entry by entry (two 16-bit halves put together by one byte permutation).  The order of entries within the
 // contraction over head_dim is free, so lanes take 16-byte pieces of keys.
 //
-// WK = 4 (few rows): the waves of a workgroup take the tiles in turn and join at the end through LDS; neither the keys nor the values pass
+// WK = 0 (few rows, short): each wave by itself.  4 (few rows): the waves of a workgroup take the tiles in turn and join at the end through LDS; neither the keys nor the values pass
 // through LDS, and no barrier stands in the loop.  1: each wave has rows of its own, and the
 // waves share the tiles, which come into LDS by asynchronous loads two tiles ahead, and the values are read turned.  Straight into registers each 16-byte piece of a key is
 // a line of its own for the cache (16 neighbouring lanes hold 16 rows), 750 accesses a tile, which bounded it with many rows; through LDS
@@ -181,7 +181,7 @@ __global__ void __launch_bounds__(kAttendThreads, (Shape<T, DP>::waves(RT))) k_a
     // WK = 4: sums to be joined, [4 waves][RT][kGroups][4][kVec / 4][64]; 1: the tiles, [3][keys, values][kKeys][DP]
     constexpr int kPieces = DP / S::kPiece, kHalfTile = kKeys * DP * static_cast<int>(sizeof(T)), kStages = 3;
     constexpr int kFills = kKeys * kPieces / kAttendThreads;  // of a wave, for the keys and again for the values
-    __shared__ F4 sh_acc[WK == 4 ? RT * DP * 16 : kStages * 2 * kHalfTile / 16];
+    __shared__ F4 sh_acc[WK == 4 ? RT * DP * 16 : (WK == 1 ? kStages * 2 * kHalfTile / 16 : 1)];
     __shared__ float sh_m[kWavesPerGroup][RT * 16], sh_l[kWavesPerGroup][RT * 16];
     __shared__ int sh_range[8];
 
@@ -190,7 +190,11 @@ __global__ void __launch_bounds__(kAttendThreads, (Shape<T, DP>::waves(RT))) k_a
 
     // ---- which rows, which keys.  Row blocks of one item (they read the same keys) are 8 workgroups apart: on one XCD.
     int item, block;
-    if (p.row_blocks == 1) { item = blockIdx.x; block = 0; }
+    if constexpr (WK == 0) {                                  // no barrier stands in the way of waves that have nothing to do
+        const int at = blockIdx.x * kWavesPerGroup + wave;
+        item = p.by_blocks.div(at); block = p.by_blocks.mod(at, item);
+        if (item >= p.items) return;
+    } else if (p.row_blocks == 1) { item = blockIdx.x; block = 0; }
     else {
         const int set = p.by_blocks.div(blockIdx.x >> 3);
         item = set * 8 + (blockIdx.x & 7); block = p.by_blocks.mod(blockIdx.x >> 3, set);
@@ -207,7 +211,7 @@ __global__ void __launch_bounds__(kAttendThreads, (Shape<T, DP>::waves(RT))) k_a
     const int unit = share.unit, part = share.part;
     const int first = unit * p.drafts;                        // its first sequence
     const int in_draft = p.tokens * p.group, rows = in_draft * p.drafts;
-    const int row0 = block * p.block_rows + (WK == 4 ? 0 : wave * 16 * RT);
+    const int row0 = block * p.block_rows + (WK == 1 ? wave * 16 * RT : 0);
     const int row_end = min(rows, (block + 1) * p.block_rows);
 
     const int shared = p.shared_len ? max(0, min(p.shared_len[unit], held)) : held;
@@ -475,7 +479,7 @@ __global__ void __launch_bounds__(kAttendThreads, (Shape<T, DP>::waves(RT))) k_a
     int next_page = 0;                                        // WK = 1: of this wave's run two tiles on
     bool bad_pages = false;                                   // WK = 1: some page between start and end is not there
     if (tile < end) {
-        if constexpr (WK == 4) {
+        if constexpr (WK != 1) {
             const Pages at = pages_of(tile);
             here_v = run_of(at, tile, quad);
             load_keys(run_of(at, tile, run_k), true);
@@ -540,7 +544,7 @@ __global__ void __launch_bounds__(kAttendThreads, (Shape<T, DP>::waves(RT))) k_a
                     }
                 }
         const Place cur_v = here_v;
-        if constexpr (WK == 4) {
+        if constexpr (WK != 1) {
             __builtin_amdgcn_sched_barrier(0);
             load_keys(run_of(next, tile + step, run_k), more);
             here_v = run_of(next, tile + step, quad);
@@ -549,8 +553,8 @@ __global__ void __launch_bounds__(kAttendThreads, (Shape<T, DP>::waves(RT))) k_a
         } else read_values(here);
 
         // weights
-        const bool lost = WK == 4 ? cur_v.page < 0 : lost_here;
-        const bool partial = tile < lo_most || tile + kKeys > hi_least || tile + kKeys > end || (WK == 4 ? __any(lost) : bad_pages);
+        const bool lost = WK != 1 ? cur_v.page < 0 : lost_here;
+        const bool partial = tile < lo_most || tile + kKeys > hi_least || tile + kKeys > end || (WK != 1 ? __any(lost) : bad_pages);
 #pragma unroll
         for (int r = 0; r < RT; ++r) {
             if (partial) {
@@ -652,14 +656,14 @@ __global__ void __launch_bounds__(kAttendThreads, (Shape<T, DP>::waves(RT))) k_a
                     for (int k = 0; k < kRun; ++k)
                         acc[r][c] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(vf[k][c / kVec][c % kVec]), s[r][0][k], acc[r][c], 0, 0, 0);
         }
-        if constexpr (WK == 4) load_values(here_v, more);
+        if constexpr (WK != 1) load_values(here_v, more);
     }
     // ---- what was not finite in tiles that not all rows see whole: products of marks alone say which rows see such an entry
     if (odd) {
 #pragma unroll 1
         for (int again = start + (WK == 4 && !own ? wave * kKeys : 0); again < end; again += step) {
             const Place at = run_of(pages_of(again), again, quad);
-            if (again >= lo_most && again + kKeys <= hi_least && again + kKeys <= end && !(WK == 4 ? __any(at.page < 0) : bad_pages)) continue;
+            if (again >= lo_most && again + kKeys <= hi_least && again + kKeys <= end && !(WK != 1 ? __any(at.page < 0) : bad_pages)) continue;
             const int base = again + quad * kRun;
             uint32_t seen[RT];
 #pragma unroll
@@ -748,7 +752,7 @@ __global__ void __launch_bounds__(kAttendThreads, (Shape<T, DP>::waves(RT))) k_a
         // a row are entries (16 g + 4 quad + i) kVec + 4 n + 0..3.  Where nothing was summed they are not written: the sum of weights says so.
         const float inv = sum[r] != 0.0f ? 1.0f / sum[r] : 0.0f;
         const int64_t at = PARTS ? (static_cast<int64_t>(share.at + part) * p.kv_heads + head0) * rows + row0 + r * 16 + col : 0;
-        if (PARTS && (WK == 1 || wave == 0) && quad == 0) p.ml[at] = make_float2(ref[r], sum[r]);
+        if (PARTS && (WK != 4 || wave == 0) && quad == 0) p.ml[at] = make_float2(ref[r], sum[r]);
         if (PARTS && !any) continue;
         if constexpr (kTurned) {                              // result c of a lane is entries 16 c + 4 quad + 0..3
 #pragma unroll
@@ -917,7 +921,7 @@ hipError_t launch_one(AttendProblem p, hipStream_t stream)
 {
     p.items = p.all_parts * p.kv_heads;
     p.by_blocks = Divider::of(p.row_blocks);
-    const int64_t grid = p.row_blocks == 1 ? p.items : static_cast<int64_t>((p.items + 7) / 8 * 8) * p.row_blocks;
+    const int64_t grid = WK == 0 ? (static_cast<int64_t>(p.items) * p.row_blocks + kWavesPerGroup - 1) / kWavesPerGroup : p.row_blocks == 1 ? p.items : static_cast<int64_t>((p.items + 7) / 8 * 8) * p.row_blocks;
     if (grid >= INT64_C(1) << 24) return hipErrorInvalidConfiguration;        // (threads of a launch: below 2^32)
     hipLaunchKernelGGL((k_attend<T, DP, RT, WK, PARTS>), dim3(static_cast<unsigned>(grid)), dim3(kAttendThreads), 0, stream, p);
     return hipGetLastError();
@@ -927,8 +931,10 @@ template <typename T, int DP, bool PARTS>
 hipError_t launch_rows(const AttendProblem &p, hipStream_t stream)
 {
     const int rows = p.tokens * p.group * p.drafts;
-    if (rows <= 16) return launch_one<T, DP, 1, 4, PARTS>(p, stream);
     constexpr int RT = DP < 256 ? 2 : 1;
+    if constexpr (!PARTS)
+        if (p.lone) return rows <= 16 ? launch_one<T, DP, 1, 0, false>(p, stream) : launch_one<T, DP, RT, 0, false>(p, stream);
+    if (rows <= 16) return launch_one<T, DP, 1, 4, PARTS>(p, stream);
     return p.few ? launch_one<T, DP, RT, 4, PARTS>(p, stream) : launch_one<T, DP, RT, 1, PARTS>(p, stream);
 }
 
@@ -992,7 +998,13 @@ static AttendPlan plan_for(int sequences, int drafts, bool shared, int tokens, i
     if (chunks > most) chunks = most;
     if (chunks > kMaxParts) chunks = kMaxParts;
     if (chunks < 1) chunks = 1;
-    if (chunks == 1 && !shared) return a;                      // one pass, nothing to join
+    if (chunks == 1 && !shared) {                              // one pass, nothing to join
+        // Few tiles, and more workgroups than the card holds at once: each wave by itself, which saves turns and the join in LDS.  Workgroups / waves, us, one
+        // query of 32 heads on 8 kv heads of 128, bfloat16: 256 sequences of up to 40 tokens 18.4 / 13.3, 100 22.3 / 18.0, 200 33.5 / 32.8; 8 sequences (64
+        // workgroups) 5.8 / 6.8, 6.1 / 8.7, 7.0 / 12.0; heads of 256, 256 sequences 56 / 27, 67 / 39, 84 / 62.
+        a.lone = a.few && longest <= 256 && base > slots;
+        return a;
+    }
     a.own_keys = shared ? drafts * 32 : 0;
     a.chunk_keys = least;
     a.grain = !a.few ? 32 : (element_bytes == 2 ? 128 : 64);   // a tile for each wave that takes keys
@@ -1016,7 +1028,7 @@ static AttendPlan plan_for(int sequences, int drafts, bool shared, int tokens, i
 
 // Drafts that share short prefixes are sequences like others: what they have of their own would be most of the work, in units with rows
 // of many drafts, and a read once more comes from the L2 caches.  Shared / alone, us: 32 prefixes of 8 drafts, a token each (32 heads, 8 kv heads
-// of 128, bfloat16) 24 / 18 at 40 tokens, 25 / 23 at 160, 30 / 29 at 320, 27 / 43 at 640; 8 of 8, 9 tokens each, 31 / 26 at 40, 41 / 34 at 640,
+// of 128, bfloat16) 24 / 12 at 40 tokens, 24 / 21 at 160, 29 / 29 at 320, 27 / 44 at 640; 8 of 8, 9 tokens each, 31 / 17 at 40, 40 / 34 at 640,
 // 46 / 53 at 1280; one of 8, a token each (21 heads, 3 kv heads of 128, float32) 18 / 7 at 40, 26 / 16 at 1280, 26 / 25 at 2560.  The workspace is that of
 // either way, so that it does not hang on max_len.
 AttendPlan plan_attend(int sequences, int drafts, bool shared, int tokens, int heads, int kv_heads, int head_dim, int element_bytes, int window,

@@ -185,13 +185,13 @@ struct AttendProblem {
     int chunks, chunk_keys;        // not balanced: parts of each unit; keys of a part (balanced: at least)
     int block_rows, row_blocks;    // rows of a workgroup
     int q_wide, out_wide;          // 16-byte loads of q, stores of whole vectors to out
-    int few, in_order;             // in_order: partial sums are held in the entries' order (this and the next are set by the launches)
+    int few, lone, in_order;             // in_order: partial sums are held in the entries' order (this and the next are set by the launches)
     int items;
     Divider by_blocks, by_kv_heads, by_chunks, by_in_draft, by_group, by_rows;
 };
 struct AttendPlan {
     int drafts, shared;                          // of a unit; whether its drafts' shared keys are read once
-    int few;                                     // the waves of a workgroup share its rows, else they have rows of their own
+    int few, lone;                               // lone: each wave by itself; few: the waves of a workgroup share its rows, else they have rows of their own
     int units, all_parts, balanced, most_parts, own_keys, grain, chunks, chunk_keys, block_rows, row_blocks;
     size_t places_bytes, ml_bytes, bytes;        // bytes: 0 where nothing is to be joined
 };

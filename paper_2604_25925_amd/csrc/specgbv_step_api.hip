@@ -194,7 +194,7 @@ specgbv_status specgbv_attend_paged(const specgbv_paged_cache *cache, const spec
     }
     p.c = static_cast<float>((a.scale > 0.0f ? static_cast<double>(a.scale) : 1.0 / std::sqrt(static_cast<double>(c.head_dim))) * 1.4426950408889634074);
     p.sequences = c.sequences; p.tokens = a.tokens; p.heads = a.heads; p.kv_heads = c.kv_heads; p.group = a.heads / c.kv_heads;
-    p.head_dim = c.head_dim; p.drafts = plan.drafts; p.few = plan.few; p.window = a.window;
+    p.head_dim = c.head_dim; p.drafts = plan.drafts; p.few = plan.few; p.lone = plan.lone; p.window = a.window;
     p.units = plan.units; p.all_parts = plan.all_parts; p.balanced = plan.balanced; p.most_parts = plan.most_parts;
     p.own_keys = plan.own_keys; p.grain = plan.grain; p.chunks = plan.chunks; p.chunk_keys = plan.chunk_keys;
     p.block_rows = plan.block_rows; p.row_blocks = plan.row_blocks;

@@ -382,3 +382,32 @@ def test_drafts_that_share_long_prefixes(dtype, B, K, T, H, G, D, page, window):
     out, _ = sg.specgbv_attend_paged(cache, q, pos, window=window, shared_len=sl, workspace=ws)
     torch.cuda.synchronize()
     check_attend(out, q, k, v, table, pos, dtype, window, label="pages")
+
+
+@pytest.mark.parametrize("dtype,S,T,H,G,D,page,window", [("bf16", 300, 1, 4, 2, 128, 16, 0), ("f32", 300, 1, 4, 2, 64, 8, 0), ("bf16", 150, 3, 12, 4, 64, 16, 0),
+                                                         ("f32", 130, 2, 16, 4, 128, 32, 20), ("bf16", 260, 1, 3, 1, 256, 16, 30), ("f32", 260, 1, 2, 1, 200, 8, 0),
+                                                         ("bf16", 90, 9, 24, 6, 80, 16, 0), ("f32", 65, 4, 64, 8, 72, 24, 0)])
+def test_many_short_sequences(dtype, S, T, H, G, D, page, window):
+    """More units than the card holds at once, of 0 to 200 tokens: each wave by itself.  Queries see nothing, a part of a tile, tiles with
+    pages that are not there and numbers that are none behind their positions."""
+    import torch
+    import paper_2604_25925_amd as sg
+    width = -(-200 // page)
+    rng, q, k, v, table = _inputs(S, T, H, G, D, page, dtype, width)
+    last = rng.integers(-1, width * page, (S, 1))
+    last[0], last[1], last[S - 1] = width * page - 1, -1, 0
+    pos = np.maximum(last - T + 1 + np.arange(T), -1).astype(np.int32)
+    table[5, 1], table[6, 0], table[7] = -1, k.shape[0], -3
+    p = torch.from_numpy(pos).cuda()
+    cache = sg.PagedCache(k, v, table)
+    out, _ = sg.specgbv_attend_paged(cache, q, p, window=window)
+    torch.cuda.synchronize()
+    check_attend(out, q, k, v, table, p, dtype, window)
+    k1, v1 = k.clone(), v.clone()
+    for s in range(8, 40):                                   # slots behind the last position
+        for a in range(int(pos[s].max()) + 1, width * page):
+            k1[table[s, a // page], :, a % page] = float("nan")
+            v1[table[s, a // page], :, a % page] = float("inf")
+    got, _ = sg.specgbv_attend_paged(sg.PagedCache(k1, v1, table), q, p, window=window)
+    torch.cuda.synchronize()
+    assert torch.equal(got, out)
