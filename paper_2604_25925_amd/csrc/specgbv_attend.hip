@@ -1001,8 +1001,9 @@ static AttendPlan plan_for(int sequences, int drafts, bool shared, int tokens, i
     if (chunks == 1 && !shared) {                              // one pass, nothing to join
         // Few tiles, and more workgroups than the card holds at once: each wave by itself, which saves turns and the join in LDS.  Workgroups / waves, us, one
         // query of 32 heads on 8 kv heads of 128, bfloat16: 256 sequences of up to 40 tokens 18.4 / 13.3, 100 22.3 / 18.0, 200 33.5 / 32.8; 8 sequences (64
-        // workgroups) 5.8 / 6.8, 6.1 / 8.7, 7.0 / 12.0; heads of 256, 256 sequences 56 / 27, 67 / 39, 84 / 62.
-        a.lone = a.few && longest <= 256 && base > slots;
+        // workgroups) 5.8 / 6.8, 6.1 / 8.7, 7.0 / 12.0.  With many registers a wave, which leave few waves to cover a workgroup's end, up to longer: 9 queries each
+        // of 64 sequences 25 / 18 at 40, 36 / 29 at 440, 41 / 38 at 640, in float32 93 / 83 and 108 / 113; one query at heads of 256, 256 sequences 56 / 27, 125 / 120, 156 / 159.
+        a.lone = a.few && longest <= (dp == 256 || (dp == 128 && a.block_rows > 16) ? 448 : 208) && base > slots;
         return a;
     }
     a.own_keys = shared ? drafts * 32 : 0;
