@@ -411,3 +411,42 @@ def test_many_short_sequences(dtype, S, T, H, G, D, page, window):
     got, _ = sg.specgbv_attend_paged(sg.PagedCache(k1, v1, table), q, p, window=window)
     torch.cuda.synchronize()
     assert torch.equal(got, out)
+
+
+@pytest.mark.parametrize("dtype,D", [("bf16", 40), ("bf16", 64), ("bf16", 128), ("bf16", 256), ("f32", 64), ("f32", 96), ("f32", 128), ("f32", 256)])
+@pytest.mark.parametrize("T,H,G,width,window", [(33, 8, 1, 12, 0), (70, 4, 1, 13, 50), (150, 4, 2, 40, 0), (40, 7, 1, 150, 0)])
+def test_more_rows_than_waves_share(dtype, D, T, H, G, width, window):
+    """Queries times heads of a group beyond 256: in one pass and in parts, with and without a window, a ragged last workgroup."""
+    _run(2, T, H, G, D, 16, dtype, width, window=window, token_major=D == 64)
+
+
+@pytest.mark.parametrize("dtype,D", [("bf16", 64), ("bf16", 128), ("f32", 64), ("bf16", 256)])
+@pytest.mark.parametrize("value", [float("nan"), float("inf"), float("-inf")])
+def test_many_rows_and_what_they_do_not_see(dtype, D, value):
+    """As for few rows: later queries' tokens, what lies in front of the window and behind the last position hold numbers that are
+    none; queries that see such a value get it in its entries alone.  Pages that are not there."""
+    import torch
+    import paper_2604_25925_amd as sg
+    S, T, H, G, page, width = 2, 72, 4, 1, 16, 16
+    rng, q, k, v, table = _inputs(S, T, H, G, D, page, dtype, width)
+    table[1, 2] = -1
+    pos = np.stack([100 + np.arange(T), 20 + np.arange(T)]).astype(np.int32)
+    p = torch.from_numpy(pos).cuda()
+    for window in (0, 90):
+        k1, v1 = k.clone(), v.clone()
+        for s in range(S):
+            for a in range(width * page):
+                if (a > pos[s, T // 2] or (window and a <= pos[s, 0] - window)) and table[s, a // page] >= 0:
+                    k1[table[s, a // page], :, a % page] = value
+                    v1[table[s, a // page], :, a % page, ::3] = value
+        ref, _ = sg.specgbv_attend_paged(sg.PagedCache(k, v, table), q, p, window=window)
+        out, _ = sg.specgbv_attend_paged(sg.PagedCache(k1, v1, table), q, p, window=window)
+        torch.cuda.synchronize()
+        check_attend(ref, q, k, v, table, p, dtype, window)
+        n = T // 2 + 1
+        assert torch.equal(out[:, :n], ref[:, :n])
+        if not window:
+            out, _ = sg.specgbv_attend_paged(sg.PagedCache(k, v1, table), q, p)
+            got = host(out)
+            assert np.isfinite(got[:, :n]).all() and np.isfinite(got[:, n:, :, 1::3]).all() and np.isfinite(got[:, n:, :, 2::3]).all()
+            assert not np.isfinite(got[:, n:, :, ::3]).any()

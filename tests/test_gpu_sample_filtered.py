@@ -268,3 +268,13 @@ def test_many_odd_rows_in_place(V):
 def test_a_min_p_that_is_no_number_is_off(dtype):
     rng = np.random.default_rng(4)
     _check(_rows(rng, 3, 2000, head=20), dtype, "nan", min_p=[np.nan, 0.05, -np.inf], u=rng.random(3).astype(np.float32))
+
+
+@pytest.mark.parametrize("dtype,R,V", [("bf16", 530, 33001), ("bf16", 300, 100003), ("f32", 300, 9001)])
+def test_batches_of_longer_rows(dtype, R, V):
+    """More rows than compute units, of lengths that other forms of the kernel take: the next row loaded ahead, rows at odd addresses."""
+    rng = np.random.default_rng(V)
+    z = _rows(rng, R, V, head=50, masked=V // 100)
+    z[3, :] = -np.inf
+    z[R - 1, ::2] = np.nan
+    _check(z, dtype, "%d" % V, **_some(rng, R, "all"))
