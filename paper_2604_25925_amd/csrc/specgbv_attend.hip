@@ -486,14 +486,14 @@ __global__ void __launch_bounds__(kAttendThreads, (Shape<T, DP>::waves(RT))) k_a
             load_values(here_v, true);
             next = pages_of(tile + step);                     // (behind the end: the last run's page)
         } else {
-            const int second = own_page(tile + step);
-            fill(own_page(tile), tile, 0);
-            if (tile + step < end) fill(second, tile + step, 1);
+            const int first_page = own_page(tile), second = own_page(tile + step);
             next_page = own_page(tile + 2 * step);
-            uint32_t bad = 0;
+            uint32_t bad = 0;                                 // (in front of the fills, which a wait for these loads would wait for too)
             for (int n = p.map.page.div(start) + lane, last = p.map.page.div(end - 1); n <= last; n += 64)
                 bad |= static_cast<uint32_t>(p.map.table[sequence * p.map.table_stride + n]) < static_cast<uint32_t>(p.map.pages) ? 0u : 1u;
             bad_pages = __any(bad != 0);
+            fill(first_page, tile, 0);
+            if (tile + step < end) fill(second, tile + step, 1);
         }
     }
     bool odd = false;                                         // a value that is not finite was cleared
