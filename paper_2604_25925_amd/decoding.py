@@ -32,11 +32,17 @@ def _stream(device, stream: Optional[int]) -> int:
     return _raw_stream(device.index) if _raw_stream is not None else torch.cuda.current_stream(device).cuda_stream
 
 
+def _between(stride: int, rows: int, length: int) -> int:
+    """Entries between rows of `length`: the tensor's own, which the library looks at, but of one row, whose stride is of no matter."""
+    return stride if rows > 1 else max(stride, length)
+
+
 class PagedCache:
     """Keys and values in pages: k and v [pages, kv_heads, page_size, head_dim] (bfloat16 or float32, the last dimension
     dense; a page may hold its tokens before its heads: pass the transposed view) and table [sequences, width] int32: token t of sequence
-    s lies in slot t % page_size of page table[s, t // page_size].  The tensors stay the caller's: what is written to them, the
-    table included, is what the next call sees.  A table entry outside [0, pages) is a page that is not there."""
+    s lies in slot t % page_size of page table[s, t // page_size] (rows of the table, and of positions, may lie apart, but not overlap).
+    The tensors stay the caller's: what is written to them, the table included, is what the next call sees.  A table entry outside
+    [0, pages) is a page that is not there."""
 
     def __init__(self, k, v, table):
         if k.dim() != 4 or k.shape != v.shape or k.dtype != v.dtype:
@@ -56,7 +62,7 @@ class PagedCache:
         self.dtype, self.device, self._index = k.dtype, k.device, k.get_device()
         ks, vs = k.stride(), v.stride()
         self._c = _CACHE.pack(k.data_ptr(), v.data_ptr(), table.data_ptr(), ks[0], ks[1], ks[2], vs[0], vs[1], vs[2],
-                              max(table.stride(0), self.width), self.pages, self.kv_heads, self.page_size, self.head_dim,
+                              _between(table.stride(0), self.sequences, self.width), self.pages, self.kv_heads, self.page_size, self.head_dim,
                               self.sequences, self.width, _DTYPES[k.dtype], 0)
 
     def _heads(self, name, x, heads=None):
@@ -82,7 +88,7 @@ class PagedCache:
         s = positions.stride()
         if tokens > 1 and s[1] != 1:
             raise ValueError("the last dimension of positions must be dense")
-        return max(s[0], tokens)
+        return _between(s[0], shape[0], tokens)
 
 
 def specgbv_cache_append(cache: PagedCache, q, k, v, positions, *, inv_freq=None, interleaved: bool = False, q_weight=None,

@@ -1,0 +1,60 @@
+"""What the binding of the decoding step's operators makes of tensors, without a GPU: CPU tensors that say they live on one take the public
+functions up to the C checks, which refuse the call before anything is launched."""
+import pytest
+import torch
+
+import paper_2604_25925_amd as sg
+
+pytestmark = pytest.mark.skipif(torch.cuda.is_available(), reason="addresses here are no GPU's: nothing may come to a launch")
+
+
+class _Said(torch.Tensor):
+    """A CPU tensor that says it lives on a GPU."""
+    is_cuda = True
+
+
+def _said(x):
+    return x.as_subclass(_Said)
+
+
+def _cache(S, width=4, pages=8, G=2, page=8, D=64, table=None, dtype=torch.bfloat16):
+    k, v = (_said(torch.zeros((pages, G, page, D), dtype=dtype)) for _ in range(2))
+    return sg.PagedCache(k, v, _said(torch.zeros((S, width), dtype=torch.int32) if table is None else table))
+
+
+def _append(cache, positions, heads=4):
+    S, T, D = cache.sequences, positions.shape[1], cache.head_dim
+    q, k = (_said(torch.zeros((S, T, h, D), dtype=cache.dtype)) for h in (heads, cache.kv_heads))
+    return sg.specgbv_cache_append(cache, q, k, k, positions, stream=0)
+
+
+def _attend(cache, positions, heads=4, **kw):
+    q = _said(torch.zeros((cache.sequences, positions.shape[1], heads, cache.head_dim), dtype=cache.dtype))
+    return sg.specgbv_attend_paged(cache, q, positions, stream=0, **kw)
+
+
+def _overlapping(S, n):
+    """int32 [S, n] views whose rows lie closer together than they are long."""
+    return [_said(torch.zeros((1, n), dtype=torch.int32).expand(S, n)), _said(torch.zeros(S + n - 1, dtype=torch.int32).unfold(0, n, 1))]
+
+
+@pytest.mark.parametrize("call", [_append, _attend])
+def test_rows_that_are_closer_than_they_are_long_are_refused(call):
+    for positions in _overlapping(3, 5):
+        assert positions.shape == (3, 5) and positions.stride(0) < 5
+        with pytest.raises(sg.SpecGBVError) as e:
+            call(_cache(3), positions)
+        assert e.value.status == 1 and "positions_stride" in str(e.value)
+    for table in _overlapping(3, 4):
+        with pytest.raises(sg.SpecGBVError) as e:
+            call(_cache(3, table=table), _said(torch.zeros((3, 2), dtype=torch.int32)))
+        assert e.value.status == 1 and "table_stride" in str(e.value)
+
+
+@pytest.mark.parametrize("stride", [0, 1, 7, 50])
+def test_the_stride_of_a_single_row_is_of_no_matter(stride):
+    one = _said(torch.zeros(60, dtype=torch.int32).as_strided((1, 5), (stride, 1)))
+    assert _cache(1)._positions(one, 5) >= 5
+    assert _cache(1, table=one).sequences == 1
+    rows = _said(torch.zeros(60, dtype=torch.int32).as_strided((3, 5), (11, 1)))
+    assert _cache(3)._positions(rows, 5) == 11
