@@ -139,6 +139,13 @@ def _check(status: int):
         raise SpecGBVError(status, specgbv_last_error())
 
 
+def _scratch(workspace, dev):
+    """The caller's workspace, whose address and size go to the kernels as they are."""
+    if not workspace.is_cuda or workspace.device != dev or not workspace.is_contiguous():
+        raise ValueError("workspace must be a dense tensor on the call's GPU")
+    return workspace
+
+
 def _dtype_code(t) -> int:
     import torch
     if t.dtype == torch.float32:
@@ -198,6 +205,8 @@ def specgbv_verify_ex(target_logits, draft_logits, draft_tokens, temperature: fl
     need = specgbv_workspace_bytes(B, K, L, V, dt)
     if workspace is None:
         workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=dev)
+    else:
+        _scratch(workspace, dev)
     if out is None:
         out = (torch.empty(B, dtype=torch.int32, device=dev), torch.empty(B, dtype=torch.int32, device=dev),
                torch.empty((B, L + 1), dtype=torch.int32, device=dev))
@@ -257,6 +266,8 @@ def specgbv_verify(target_logits, draft_logits, draft_tokens, temperature: float
     dev = target_logits.device
     if workspace is None:
         workspace = torch.empty(max(specgbv_workspace_bytes(B, K, L, V, dt), 256), dtype=torch.uint8, device=dev)
+    else:
+        _scratch(workspace, dev)
     if out is None:
         out = (torch.empty(B, dtype=torch.int32, device=dev), torch.empty(B, dtype=torch.int32, device=dev),
                torch.empty((B, L + 1), dtype=torch.int32, device=dev))
@@ -283,6 +294,8 @@ def specgbv_verify_kseq(target_logits, draft_logits, draft_tokens, temperature: 
     dev = target_logits.device
     if workspace is None:
         workspace = torch.empty(max(specgbv_workspace_bytes(B, K, L, V, dt), 256), dtype=torch.uint8, device=dev)
+    else:
+        _scratch(workspace, dev)
     if out is None:
         out = (torch.empty(B, dtype=torch.int32, device=dev), torch.empty(B, dtype=torch.int32, device=dev),
                torch.empty((B, L + 1), dtype=torch.int32, device=dev))
@@ -426,6 +439,8 @@ def specgbv_modify_target(target_logits, draft_logits, draft_tokens, temperature
         workspace = res.get("workspace")
     if workspace is None:
         workspace = torch.empty(max(specgbv_modify_workspace_bytes(B, K, M, bonus), 256), dtype=torch.uint8, device=dev)
+    else:
+        _scratch(workspace, dev)
     res["workspace"] = workspace
     if stream is None:
         stream = torch.cuda.current_stream(dev).cuda_stream
@@ -457,6 +472,8 @@ def specgbv_sample_tokens(logits, temperature: float, rng_seed: int, rng_offset:
         out = torch.empty(rows, dtype=torch.int32, device=dev)
     if workspace is None:
         workspace = torch.empty(max(specgbv_sample_workspace_bytes(rows, V), 256), dtype=torch.uint8, device=dev)
+    else:
+        _scratch(workspace, dev)
     if stream is None:
         stream = torch.cuda.current_stream(dev).cuda_stream
     st = lib.specgbv_sample_tokens(logits.data_ptr(), rows, V, _dtype_code(logits), c_float(temperature), rng_seed,
@@ -505,6 +522,8 @@ def specgbv_carry_advance(rows_q, rows_p, draft_tokens, accepted_len, accepted_d
         raise ValueError("rows must be contiguous GPU tensors")
     if workspace is None:
         workspace = torch.empty(max(specgbv_carry_workspace_bytes(B, M), 256), dtype=torch.uint8, device=rows_q.device)
+    else:
+        _scratch(workspace, rows_q.device)
     if stream is None:
         stream = torch.cuda.current_stream(rows_q.device).cuda_stream
     st = lib.specgbv_carry_advance(rows_q.data_ptr(), rows_p.data_ptr(), draft_tokens.data_ptr(), accepted_len.data_ptr(),

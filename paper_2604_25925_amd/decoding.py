@@ -12,7 +12,7 @@ from typing import Optional
 
 import torch
 
-from .binding import BF16, F32, _check, load_library
+from .binding import BF16, F32, _check, _scratch, load_library
 
 # specgbv_paged_cache, specgbv_append_args and specgbv_attend_args of the C header, field by field
 _CACHE = struct.Struct("@PPP7q8i")
@@ -163,6 +163,8 @@ def specgbv_attend_paged(cache: PagedCache, q, positions, *, window: int = 0, sh
     if workspace is None:
         need = int(lib.specgbv_attend_workspace_bytes(cache._c, args))
         workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=cache.device)
+    else:
+        _scratch(workspace, cache.device)
     _check(lib.specgbv_attend_paged(cache._c, args, workspace.data_ptr(), workspace.numel() * workspace.element_size(),
                                     _stream(cache.device, stream)))
     return out, workspace
@@ -235,6 +237,8 @@ def specgbv_sample_filtered(logits, u=None, *, temperature=None, top_k=None, top
     dt = _DTYPES[logits.dtype]
     if workspace is None:
         workspace = torch.empty(max(int(lib.specgbv_filter_workspace_bytes(rows, V, dt)), 256), dtype=torch.uint8, device=dev)
+    else:
+        _scratch(workspace, dev)
     _check(lib.specgbv_sample_filtered(logits.data_ptr(), row_stride, rows, V, dt, ptr[0], ptr[1], ptr[2], ptr[3], ptr[4],
                                        out.data_ptr() if draw else None, kept.data_ptr() if keep else None, kept_stride,
                                        workspace.data_ptr(), workspace.numel() * workspace.element_size(), _stream(dev, stream)))

@@ -58,3 +58,34 @@ def test_the_stride_of_a_single_row_is_of_no_matter(stride):
     assert _cache(1, table=one).sequences == 1
     rows = _said(torch.zeros(60, dtype=torch.int32).as_strided((3, 5), (11, 1)))
     assert _cache(3)._positions(rows, 5) == 11
+
+
+def _filtered(**kw):
+    z = _said(torch.zeros((3, 40)))
+    return sg.specgbv_sample_filtered(z, _said(torch.zeros(3)), stream=0, **kw)
+
+
+def _verification(name, **kw):
+    B, K, L, V = 1, 2, 3, 64
+    target, draft, tokens = _said(torch.zeros((B, K, L + 1, V))), _said(torch.zeros((B, K, L, V))), _said(torch.zeros((B, K, L), dtype=torch.int32))
+    one, nu = _said(torch.zeros(B, dtype=torch.int32)), _said(torch.zeros(B, dtype=torch.float64))
+    if name in ("specgbv_verify", "specgbv_verify_ex", "specgbv_verify_kseq"):
+        return getattr(sg, name)(target, draft, tokens, 1.0, 0, 0, stream=0, **kw)
+    if name == "specgbv_modify_target":
+        return sg.specgbv_modify_target(target, draft, tokens, 1.0, nu, one, stream=0, **kw)
+    if name == "specgbv_sample_tokens":
+        return sg.specgbv_sample_tokens(target, 1.0, 0, 0, 0, stream=0, **kw)
+    return sg.specgbv_carry_advance(target, draft, tokens, one, one, _said(torch.zeros((B, L + 1), dtype=torch.int32)), 1.0, nu, one, stream=0, **kw)
+
+
+@pytest.mark.parametrize("call", [lambda **kw: _attend(_cache(3), _said(torch.zeros((3, 2), dtype=torch.int32)), **kw), _filtered] +
+                         [lambda name=name, **kw: _verification(name, **kw) for name in
+                          ("specgbv_verify", "specgbv_verify_ex", "specgbv_verify_kseq", "specgbv_modify_target", "specgbv_sample_tokens", "specgbv_carry_advance")])
+def test_a_workspace_is_dense_and_lives_on_the_calls_gpu(call):
+    n = 1 << 24
+    for workspace in (torch.zeros(n, dtype=torch.uint8),                                      # on the host
+                      _said(torch.zeros(1, dtype=torch.uint8).expand(n)),                     # less memory than entries
+                      _said(torch.zeros(4 * n, dtype=torch.uint8))[::4],
+                      _said(torch.zeros(n, dtype=torch.uint8, device="meta"))):               # on another device
+        with pytest.raises(ValueError, match="workspace"):
+            call(workspace=workspace)
