@@ -16,22 +16,24 @@ import torch
 sys.path.insert(0, os.path.join(os.path.dirname(os.path.abspath(__file__)), ".."))
 import paper_2604_25925_amd as sg  # noqa: E402
 
+DEVICE = "cuda"
+
 
 class Model:
     """A decoder: per layer attention of `heads` heads in groups that share a key and value head, and a gated product."""
 
     def __init__(self, seed, V=2048, E=256, layers=2, heads=8, kv_heads=2, D=64, dtype=torch.bfloat16, like=None, noise=0.0):
-        gen = torch.Generator(device="cuda").manual_seed(seed)
+        gen = torch.Generator(device=DEVICE).manual_seed(seed)
 
         def weight(*shape):
-            return (torch.randn(shape, generator=gen, device="cuda") / math.sqrt(shape[0])).to(dtype)
+            return (torch.randn(shape, generator=gen, device=DEVICE) / math.sqrt(shape[0])).to(dtype)
 
         self.V, self.heads, self.kv_heads, self.D, self.dtype = V, heads, kv_heads, D, dtype
-        self.inv_freq = 10000.0 ** (-torch.arange(D // 2, device="cuda", dtype=torch.float64) / (D // 2))
-        self.embed = torch.randn((V, E), generator=gen, device="cuda").to(dtype)
+        self.inv_freq = 10000.0 ** (-torch.arange(D // 2, device=DEVICE, dtype=torch.float64) / (D // 2))
+        self.embed = torch.randn((V, E), generator=gen, device=DEVICE).to(dtype)
         self.layers = [{"qkv": weight(E, (heads + 2 * kv_heads) * D), "o": weight(heads * D, E), "up": weight(E, 2 * E), "gate": weight(E, 2 * E),
-                        "down": weight(2 * E, E), "q_norm": torch.ones(D, dtype=dtype, device="cuda"),
-                        "k_norm": torch.ones(D, dtype=dtype, device="cuda")} for _ in range(layers)]
+                        "down": weight(2 * E, E), "q_norm": torch.ones(D, dtype=dtype, device=DEVICE),
+                        "k_norm": torch.ones(D, dtype=dtype, device=DEVICE)} for _ in range(layers)]
         self.head = weight(E, V) * 3
         if like is not None:                                  # a model near to another one: what a draft model is to its target
             self.embed, self.layers = like.embed, like.layers[:layers]
@@ -39,7 +41,7 @@ class Model:
 
     def cache(self, pages, page):
         shape = (len(self.layers), 2, pages, self.kv_heads, page, self.D)
-        return torch.zeros(shape, dtype=self.dtype, device="cuda")
+        return torch.zeros(shape, dtype=self.dtype, device=DEVICE)
 
     def forward(self, tokens, positions, caches, shared_len=None, rows=None):
         """Logits [S, rows, V] of the last `rows` tokens; tokens and positions [S, T] (position below 0: padding); caches: a PagedCache
@@ -65,11 +67,12 @@ class Model:
 def right_aligned(rows):
     """int32 [n, longest] of lists, padded in front with -1."""
     T = max(1, max(len(r) for r in rows))
-    return torch.tensor([[-1] * (T - len(r)) + list(r) for r in rows], dtype=torch.int32, device="cuda")
+    return torch.tensor([[-1] * (T - len(r)) + list(r) for r in rows], dtype=torch.int32, device=DEVICE)
 
 
 def decode(target, draft, prompts, drafts=4, length=8, new=64, page=16, temperature=0.8, top_k=0, top_p=0.95, min_p=0.0, seed=1):
-    """Texts (lists of tokens, the prompts included) and the number of iterations.
+    """Texts (lists of tokens, the prompts included) and the number of iterations.  A prompt that has `new` tokens is finished: it is padding in
+    the iterations that others still need.
 
     Every draft has pages of its own; those of a page index that the prefix fills are the accepted draft's for all drafts of the prefix
     (the table says so, and shared_len).  The tokens behind the last whole page are fed again to every draft, so no page is ever copied."""
@@ -79,19 +82,19 @@ def decode(target, draft, prompts, drafts=4, length=8, new=64, page=16, temperat
     width = (max(len(p) for p in prompts) + new + 2 * L + 2 * page) // page
     own = torch.arange(S * width, dtype=torch.int32).view(B, K, width)
     table = own.clone()
-    dev_table = table.view(S, width).cuda()
+    dev_table = table.view(S, width).to(DEVICE)
     models = (target, draft)
     memory = [m.cache(S * width, page) for m in models]
     step = [[sg.PagedCache(c[0], c[1], dev_table) for c in mem] for mem in memory]
 
-    gen = torch.Generator(device="cuda").manual_seed(seed)
+    gen = torch.Generator(device=DEVICE).manual_seed(seed)
 
     def filters(n):
-        return {name: torch.full((n,), value, dtype=torch.int32 if name == "top_k" else torch.float32, device="cuda")
+        return {name: torch.full((n,), value, dtype=torch.int32 if name == "top_k" else torch.float32, device=DEVICE)
                 for name, value in (("temperature", temperature), ("top_k", top_k), ("top_p", top_p), ("min_p", min_p))}
 
     each, block = filters(S), filters(S * (L + 1))
-    state = torch.zeros(sg.specgbv_pending_state_bytes(B), dtype=torch.uint8, device="cuda")
+    state = torch.zeros(sg.specgbv_pending_state_bytes(B), dtype=torch.uint8, device=DEVICE)
 
     # the prompts' whole pages, by draft 0 of each
     whole = [(len(t) - 1) // page for t in text]
@@ -106,23 +109,28 @@ def decode(target, draft, prompts, drafts=4, length=8, new=64, page=16, temperat
             m.forward(tokens.clamp(min=0), at, [sg.PagedCache(c[0], c[1], first) for c in mem], rows=1)
 
     iterations = 0
-    while min(len(t) - len(p) for t, p in zip(text, prompts)) < new:
-        shared = torch.tensor([w * page for w in whole], dtype=torch.int32, device="cuda")
-        tail = right_aligned([t[w * page:] for t, w in zip(text, whole)]).repeat_interleave(K, dim=0).clamp(min=0)
-        tail_at = right_aligned([range(w * page, len(t)) for t, w in zip(text, whole)]).repeat_interleave(K, dim=0)
-        end = tail_at[:, -1:].clone()
+    while True:
+        going = [len(t) - len(p) < new for t, p in zip(text, prompts)]
+        if not any(going):
+            return text, iterations
+        # (a block reaches to its prompt's length + new + L - 2 at most, which the table holds)
+        shared = torch.tensor([w * page if g else 0 for w, g in zip(whole, going)], dtype=torch.int32, device=DEVICE)
+        tail = right_aligned([t[w * page:] if g else [] for t, w, g in zip(text, whole, going)]).repeat_interleave(K, dim=0).clamp(min=0)
+        tail_at = right_aligned([range(w * page, len(t)) if g else [] for t, w, g in zip(text, whole, going)]).repeat_interleave(K, dim=0)
+        end = tail_at[:, -1:].clone()                         # -1: finished
+        drafted_at = torch.where(end < 0, end, end + 1 + torch.arange(L, dtype=torch.int32, device=DEVICE))
 
         # ---- the drafts: one token a step
-        drafted = torch.empty((S, L), dtype=torch.int32, device="cuda")
-        draft_rows = torch.empty((S, L, V), dtype=draft.dtype, device="cuda")
+        drafted = torch.empty((S, L), dtype=torch.int32, device=DEVICE)
+        draft_rows = torch.empty((S, L, V), dtype=draft.dtype, device=DEVICE)
         for i in range(L):
-            tokens, at = (tail, tail_at) if i == 0 else (drafted[:, i - 1:i], end + i)
+            tokens, at = (tail, tail_at) if i == 0 else (drafted[:, i - 1:i], drafted_at[:, i - 1:i])
             z = draft.forward(tokens, at.contiguous(), step[1], shared, rows=1)
-            u = torch.rand(S, generator=gen, device="cuda")
+            u = torch.rand(S, generator=gen, device=DEVICE)
             drafted[:, i] = sg.specgbv_sample_filtered(z[:, 0], u, keep=True, kept=draft_rows[:, i], **each)[0]
 
         # ---- the target scores all blocks at once, and its rows are truncated as the drafts' were
-        at = torch.cat((tail_at, end + 1 + torch.arange(L, dtype=torch.int32, device="cuda")), dim=1)
+        at = torch.cat((tail_at, drafted_at), dim=1)
         z = target.forward(torch.cat((tail, drafted), dim=1), at.contiguous(), step[0], shared, rows=L + 1)
         sg.specgbv_sample_filtered(z, draw=False, keep=True, kept=z, **block)
 
@@ -132,12 +140,13 @@ def decode(target, draft, prompts, drafts=4, length=8, new=64, page=16, temperat
         iterations += 1
         taken, by, out = taken.tolist(), by.tolist(), out.tolist()
         for b in range(B):
+            if not going[b]:
+                continue
             held = (len(text[b]) + taken[b]) // page           # whole pages of tokens whose keys and values are there
             text[b] += out[b][:taken[b] + 1]
             table[b, :, whole[b]:held] = own[b, max(by[b], 0), whole[b]:held]
             whole[b] = held
         dev_table.copy_(table.view(S, width))
-    return text, iterations
 
 
 def main():
@@ -155,7 +164,7 @@ def main():
     prompts = [torch.randint(target.V, (20 + 31 * i,), generator=gen).tolist() for i in range(a.prompts)]
     text, iterations = decode(target, draft, prompts, a.drafts, a.length, a.tokens)
     made = sum(len(t) - len(p) for t, p in zip(text, prompts))
-    print("%d tokens for %d prompts in %d iterations: %.2f a prompt and iteration" % (made, a.prompts, iterations, made / iterations / a.prompts))
+    print("%d tokens for %d prompts in %d iterations" % (made, a.prompts, iterations))
 
 
 if __name__ == "__main__":
