@@ -142,7 +142,8 @@ def decode(target, draft, prompts, drafts=4, length=8, new=64, page=16, temperat
         for b in range(B):
             if not going[b]:
                 continue
-            held = (len(text[b]) + taken[b]) // page           # whole pages of tokens whose keys and values are there
+            # whole pages of tokens whose keys and values both models have: the draft model was not fed the last drafted token
+            held = (len(text[b]) + min(taken[b], L - 1)) // page
             text[b] += out[b][:taken[b] + 1]
             table[b, :, whole[b]:held] = own[b, max(by[b], 0), whole[b]:held]
             whole[b] = held

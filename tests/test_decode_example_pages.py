@@ -87,3 +87,39 @@ def _decode(example, monkeypatch, accepted, lengths, drafts, length, new, page, 
 def test_a_prompt_that_is_ahead_of_the_slowest_one(example, monkeypatch, fast, slow, drafts, length, page, new):
     """One prompt takes all but one token a block, the other none: the first is done long before and must not outgrow its table."""
     _decode(example, monkeypatch, lambda b, i: length - 1 if b == fast else 0, [41, 37] if fast == 0 else [5, 60], drafts, length, new, page)
+
+
+@pytest.mark.parametrize("drafts,length,page,prompt", [(2, 4, 8, 4), (3, 8, 8, 16), (1, 5, 16, 11), (4, 7, 8, 1), (2, 1, 8, 7)])
+def test_blocks_that_are_taken_whole_and_end_on_a_page(example, monkeypatch, drafts, length, page, prompt):
+    """The draft model has not seen a block's last drafted token when the block is verified: a page that ends with it is not yet whole."""
+    assert any((prompt + i * (length + 1) + length) % page == 0 for i in range(page))
+    _decode(example, monkeypatch, lambda b, i: length, [prompt, prompt + 3], drafts, length, 8 * page, page)
+
+
+def test_blocks_that_are_taken_in_part(example, monkeypatch):
+    rng = np.random.default_rng(3)
+    for length in (1, 3, 8):
+        _decode(example, monkeypatch, lambda b, i: int(rng.integers(0, length + 1)), [1, 9, 30, 64], 3, length, 50, 8, seed=length)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("drafts,length,page", [(2, 4, 8), (1, 8, 8), (3, 7, 16)])
+def test_a_draft_model_that_is_the_target_is_always_right(drafts, length, page):
+    """top_k 1 and one model for both: every drafted token is taken for as long as the draft model's cache holds what the text says.  Rows of one
+    token and of a block round differently: where the logits of the two likeliest tokens are within 1e-3, far beyond float32's errors over two
+    layers, a block may be cut short."""
+    from test_gpu_decode_example import _plain_logits
+    path = pathlib.Path(__file__).resolve().parents[1] / "examples" / "speculative_decode.py"
+    spec = importlib.util.spec_from_file_location("speculative_decode_same", path)
+    module = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(module)
+    target = module.Model(1, V=500, E=128, D=64, dtype=torch.float32)
+    draft = module.Model(2, dtype=torch.float32, V=500, E=128, D=64, like=target, noise=0.0)
+    prompts = [np.random.default_rng(n).integers(0, 500, n).tolist() for n in (3, 8, 17)]
+    new = 6 * (length + 1)
+    text, iterations = module.decode(target, draft, prompts, drafts, length, new=new, page=page, top_k=1, top_p=1.0)
+    near = 0
+    for p, t in zip(prompts, text):
+        best = np.sort(_plain_logits(target, t)[len(p) - 1:-1], axis=-1)[:, -2:]
+        near += int((best[:, 1] - best[:, 0] < 1e-3).sum())
+    assert near <= 1 and 6 <= iterations <= 6 + near
