@@ -176,6 +176,8 @@ def specgbv_filter_workspace_bytes(rows: int, V: int, dtype: int) -> int:
 
 def _rows_of(name, x, V=None):
     """(rows, stride between rows) of x [..., V] whose leading dimensions step evenly."""
+    if 0 in x.shape[:-1]:
+        return 0, x.shape[-1]
     if x.dim() == 2:
         rows, stride = x.shape[0], x.stride(0)
     else:

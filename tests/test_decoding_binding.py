@@ -89,3 +89,11 @@ def test_a_workspace_is_dense_and_lives_on_the_calls_gpu(call):
                       _said(torch.zeros(n, dtype=torch.uint8, device="meta"))):               # on another device
         with pytest.raises(ValueError, match="workspace"):
             call(workspace=workspace)
+
+
+@pytest.mark.parametrize("shape", [(0, 40), (2, 0, 40), (0, 2, 40), (3, 0, 2, 40), (1, 0, 40)])
+def test_logits_without_rows(shape):
+    for z in (torch.zeros(shape), torch.zeros([n + 3 for n in shape[:-1]] + [50])[tuple(slice(0, n) for n in shape)]):
+        assert z.shape == shape
+        tokens, kept, _ = sg.specgbv_sample_filtered(_said(z), _said(torch.zeros(0)), keep=True, stream=0)
+        assert tokens.shape == (0,) and kept.shape == shape
