@@ -433,7 +433,7 @@ specgbv_status specgbv_read_sample_intermediates(
  */
 typedef struct {
     void *k, *v;               /* device, bfloat16 or float32 as dtype says                        */
-    const int32_t *table;      /* device, [sequences, table_width], rows table_stride entries apart */
+    const int32_t *table;      /* device, [sequences, table_width], rows table_stride entries apart; may be NULL where sequences = 0 */
     int64_t k_page_stride, k_head_stride, k_token_stride;
     int64_t v_page_stride, v_head_stride, v_token_stride;
     int64_t table_stride;

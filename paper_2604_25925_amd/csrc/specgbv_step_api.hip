@@ -33,7 +33,7 @@ static specgbv_status check_cache(const specgbv_paged_cache *c, bool pointers)
     if (c->k_token_stride > (1 << 26) || c->v_token_stride > (1 << 26))
         return fail(SPECGBV_EUNSUPPORTED, "tokens of the cache lie more than 2^26 entries apart");
     if (pointers) {
-        if (!c->k || !c->v || !c->table) return fail(SPECGBV_EINVAL, "null pointer in the cache");
+        if (!c->k || !c->v || (!c->table && c->sequences > 0)) return fail(SPECGBV_EINVAL, "null pointer in the cache");
         if (!aligned(c->k, 16) || !aligned(c->v, 16)) return fail(SPECGBV_EUNSUPPORTED, "the cache is not 16-byte aligned");
         if (!aligned(c->table, 4)) return fail(SPECGBV_EINVAL, "pointer not aligned to its element size");
     }

@@ -97,3 +97,11 @@ def test_logits_without_rows(shape):
         assert z.shape == shape
         tokens, kept, _ = sg.specgbv_sample_filtered(_said(z), _said(torch.zeros(0)), keep=True, stream=0)
         assert tokens.shape == (0,) and kept.shape == shape
+
+
+def test_caches_without_sequences_and_calls_without_tokens():
+    for S, T in ((0, 1), (0, 0), (3, 0)):
+        positions = _said(torch.zeros((S, T), dtype=torch.int32))
+        assert _append(_cache(S), positions).shape == (S, T, 4, 64)
+        assert _attend(_cache(S), positions)[0].shape == (S, T, 4, 64)
+        assert _attend(_cache(S), positions, shared_len=_said(torch.zeros(S, dtype=torch.int32)))[0].shape == (S, T, 4, 64)
