@@ -496,8 +496,9 @@ typedef struct {
 specgbv_status specgbv_attend_paged(const specgbv_paged_cache *cache, const specgbv_attend_args *args,
                                     void *workspace, size_t workspace_bytes, void *hip_stream);
 
-/* Bytes of device workspace (256-byte aligned, contents of no matter) specgbv_attend_paged needs for these arguments, whose
- * pointers are not looked at; 0 if they are invalid, or if none is needed. */
+/* Bytes of device workspace (256-byte aligned, contents of no matter) specgbv_attend_paged needs for these arguments with any
+ * max_len, so that one workspace serves a text that grows (a call itself asks for no more than it needs); pointers are not looked at; 0
+ * if the arguments are invalid, or if none is needed. */
 size_t specgbv_attend_workspace_bytes(const specgbv_paged_cache *cache, const specgbv_attend_args *args);
 
 /*

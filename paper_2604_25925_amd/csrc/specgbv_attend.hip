@@ -1030,16 +1030,34 @@ static AttendPlan plan_for(int sequences, int drafts, bool shared, int tokens, i
 // Drafts that share short prefixes are sequences like others: what they have of their own would be most of the work, in units with rows
 // of many drafts, and a read once more comes from the L2 caches.  Shared / alone, us: 32 prefixes of 8 drafts, a token each (32 heads, 8 kv heads
 // of 128, bfloat16) 24 / 12 at 40 tokens, 24 / 21 at 160, 29 / 29 at 320, 27 / 44 at 640; 8 of 8, 9 tokens each, 31 / 17 at 40, 40 / 34 at 640,
-// 46 / 53 at 1280; one of 8, a token each (21 heads, 3 kv heads of 128, float32) 18 / 7 at 40, 26 / 16 at 1280, 26 / 25 at 2560.  The workspace is that of
-// either way, so that it does not hang on max_len.
+// 46 / 53 at 1280; one of 8, a token each (21 heads, 3 kv heads of 128, float32) 18 / 7 at 40, 26 / 16 at 1280, 26 / 25 at 2560.
+// Up to which length they are taken by themselves:
+static int64_t alone_up_to(int sequences, int kv_heads, int head_dim, int element_bytes)
+{
+    const int64_t reads = (int64_t{128} << 20) / (2 * static_cast<int64_t>(sequences) * kv_heads * head_dim * element_bytes);
+    return reads < 1024 ? reads : 1024;
+}
+
+// (a call asks for the workspace of either way)
 AttendPlan plan_attend(int sequences, int drafts, bool shared, int tokens, int heads, int kv_heads, int head_dim, int element_bytes, int window,
                        int64_t longest)
 {
     const AttendPlan plan = plan_for(sequences, drafts, shared, tokens, heads, kv_heads, head_dim, element_bytes, window, longest);
-    if (!shared || longest > 1024 || 2 * static_cast<int64_t>(sequences) * longest * kv_heads * head_dim * element_bytes > int64_t{128} << 20) return plan;
+    if (!shared || longest > alone_up_to(sequences, kv_heads, head_dim, element_bytes)) return plan;
     AttendPlan alone = plan_for(sequences, 1, false, tokens, heads, kv_heads, head_dim, element_bytes, window, longest);
     if (alone.bytes < plan.bytes) alone.bytes = plan.bytes;
     return alone;
+}
+
+// The parts of a plan, and so its bytes, do not get fewer with the length: the longest one of each way asks for most.
+size_t attend_bytes(int sequences, int drafts, bool shared, int tokens, int heads, int kv_heads, int head_dim, int element_bytes, int window,
+                    int64_t held)
+{
+    const size_t whole = plan_for(sequences, drafts, shared, tokens, heads, kv_heads, head_dim, element_bytes, window, held).bytes;
+    const int64_t near = shared ? alone_up_to(sequences, kv_heads, head_dim, element_bytes) : 0;
+    if (near < 1) return whole;
+    const size_t alone = plan_for(sequences, 1, false, tokens, heads, kv_heads, head_dim, element_bytes, window, near < held ? near : held).bytes;
+    return alone > whole ? alone : whole;
 }
 
 hipError_t launch_attend(const AttendProblem &p, int dtype, hipStream_t stream)

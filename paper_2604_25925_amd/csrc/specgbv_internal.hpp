@@ -197,6 +197,9 @@ struct AttendPlan {
 };
 AttendPlan plan_attend(int sequences, int drafts, bool shared, int tokens, int heads, int kv_heads, int head_dim, int element_bytes, int window,
                        int64_t longest);
+// Most that plan_attend asks for with any `longest` up to `held`.
+size_t attend_bytes(int sequences, int drafts, bool shared, int tokens, int heads, int kv_heads, int head_dim, int element_bytes, int window,
+                    int64_t held);
 hipError_t launch_attend(const AttendProblem &p, int dtype, hipStream_t stream);
 
 // Truncated distributions and draws from them (see specgbv_sample_filtered).

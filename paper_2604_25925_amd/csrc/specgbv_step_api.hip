@@ -156,7 +156,10 @@ extern "C" {
 size_t specgbv_attend_workspace_bytes(const specgbv_paged_cache *cache, const specgbv_attend_args *args)
 {
     if (check_attend(cache, args, false) != SPECGBV_OK || cache->sequences == 0 || args->tokens == 0) return 0;
-    return plan_of(*cache, *args).bytes;
+    const specgbv_paged_cache &c = *cache;
+    const specgbv_attend_args &a = *args;
+    return attend_bytes(c.sequences, a.prefixes > 0 ? c.sequences / a.prefixes : 1, a.prefixes > 0, a.tokens, a.heads, c.kv_heads, c.head_dim,
+                        element_bytes(c.dtype), a.window, static_cast<int64_t>(c.table_width) * c.page_size);
 }
 
 specgbv_status specgbv_attend_paged(const specgbv_paged_cache *cache, const specgbv_attend_args *args,

@@ -150,7 +150,7 @@ def specgbv_attend_paged(cache: PagedCache, q, positions, *, window: int = 0, sh
     cache: the query at position p sees tokens p - window < j <= p of its sequence (window 0: all up to p).  shared_len [prefixes]
     int32 states that the S sequences are the drafts of as many prefixes and how many first tokens lie in pages that a prefix's drafts
     share: those are read once per prefix.  max_len: how far sequences reach at most, for the choice of the split.  Returns
-    (out [S, T, heads, D], workspace)."""
+    (out [S, T, heads, D], workspace); the workspace serves calls of these shapes with any max_len."""
     lib = load_library()
     T, H, qs = cache._heads("q", q)
     ps = cache._positions(positions, T)

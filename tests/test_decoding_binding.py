@@ -105,3 +105,43 @@ def test_caches_without_sequences_and_calls_without_tokens():
         assert _append(_cache(S), positions).shape == (S, T, 4, 64)
         assert _attend(_cache(S), positions)[0].shape == (S, T, 4, 64)
         assert _attend(_cache(S), positions, shared_len=_said(torch.zeros(S, dtype=torch.int32)))[0].shape == (S, T, 4, 64)
+
+
+HINTS = [0, 1, 40, 200, 256, 257, 513, 900, 1024, 1025, 2048, 4000, 5000, 1 << 20]
+
+
+@pytest.mark.parametrize("prefixes,drafts", [(1, 1), (1, 3), (3, 1), (4, 8), (32, 8), (70, 1), (70, 2), (300, 1)])
+@pytest.mark.parametrize("window", [0, 700])
+def test_a_workspace_serves_every_max_len(prefixes, drafts, window):
+    """A loop that keeps its workspace while its text, and with it max_len, grows or starts anew."""
+    for G, D, T, heads, dtype in ((8, 128, 8, 32, torch.bfloat16), (8, 128, 1, 32, torch.bfloat16), (1, 64, 1, 5, torch.float32), (2, 256, 9, 8, torch.bfloat16)):
+        S = prefixes * drafts
+        for shared in ([None, _said(torch.zeros(prefixes, dtype=torch.int32))] if drafts > 1 else [None]):
+            cache = _cache(S, width=600, pages=1, G=G, D=D, dtype=dtype)
+            q = _said(torch.zeros((1, 1, 1, 1), dtype=dtype).expand(S, T, heads, D).contiguous())
+            need = {n: sg.specgbv_attend_workspace_bytes(cache, q, window=window, shared_len=shared, max_len=n) for n in HINTS}
+            assert len(set(need.values())) == 1, (G, D, T, shared is None, need)
+            positions = _said(torch.zeros((S, T), dtype=torch.int32))
+            _, kept = _tried(cache, q, positions, window=window, shared_len=shared, max_len=200)      # what the binding makes for a short text
+            for n in HINTS:
+                status, _ = _tried(cache, q, positions, window=window, shared_len=shared, max_len=n, workspace=kept)
+                assert status == 4, (G, D, T, shared is None, n)                                      # (no GPU: it came to the launch)
+
+
+def _tried(cache, q, positions, workspace=None, **kw):
+    """(status, workspace) of a call that comes as far as its launch."""
+    made = []
+    empty = torch.empty
+
+    def keep(n, **kwargs):                                    # on a border of 256 bytes, as on a GPU
+        room = empty(n + 256, **kwargs)
+        at = -room.data_ptr() % 256
+        made.append(_said(room[at:at + n]))
+        return made[-1]
+    torch.empty = keep
+    try:
+        sg.specgbv_attend_paged(cache, q, positions, stream=0, out=q, workspace=workspace, **kw)
+    except sg.SpecGBVError as e:
+        return e.status, workspace if workspace is not None else made[0]
+    finally:
+        torch.empty = empty
