@@ -170,7 +170,7 @@ __global__ void __launch_bounds__(kAppendThreads) k_append(AppendProblem p)
 template <typename T, int W>
 hipError_t launch_width(const AppendProblem &p, hipStream_t stream)
 {
-    const int grid = (p.tokens_all + p.block_tokens - 1) / p.block_tokens;
+    const int grid = (p.tokens_all + p.block_tokens - 1) / p.block_tokens;      // (fewer than 2^30 tokens)
     hipLaunchKernelGGL((k_append<T, W, W == 1 ? 2 : 1>), dim3(grid), dim3(kAppendThreads), 0, stream, p);
     return hipGetLastError();
 }
@@ -186,6 +186,7 @@ hipError_t launch_append(const AppendProblem &given, int dtype, int width, hipSt
     // tokens of a workgroup, 1 / 2 / 4, us (32 heads, 8 kv heads of 128, bfloat16): 5.5 / 6.8 / 10.5 for 256 tokens, 8.2 / 9.0 / 12.2 for 1024,
     // 13.2 / 12.9 / 16.0 for 2304, 82 / 77 / 79 for 20005
     p.block_tokens = p.tokens_all >= 8 * compute_units() ? kAppendTokens : 1;
+    if ((static_cast<int64_t>(p.tokens_all) + p.block_tokens - 1) / p.block_tokens >= kLaunchGroups) return hipErrorInvalidConfiguration;
     if (dtype == 1) switch (width) {
         case 8: return launch_width<uint16_t, 8>(p, stream);
         case 4: return launch_width<uint16_t, 4>(p, stream);

@@ -147,6 +147,9 @@ hipError_t launch_carry_advance(const void *rows_q, const void *rows_p, const in
 // The message of this thread's last failing call; returns `st`.
 specgbv_status fail(specgbv_status st, const char *fmt, ...);
 
+// A launch has fewer than 2^32 threads: workgroups of 256.  Launches of the decoding step with more return hipErrorInvalidConfiguration.
+constexpr int64_t kLaunchGroups = int64_t{1} << 24;
+
 // Appending to a paged cache (see specgbv_append_args); strides in elements, of the caches: page, head, slot.
 struct AppendProblem {
     const void *q, *k, *v;

@@ -85,6 +85,7 @@ specgbv_status specgbv_cache_append(const specgbv_paged_cache *cache, const spec
     if (!(a.eps >= 0.0) || !std::isfinite(a.eps)) return fail(SPECGBV_EINVAL, "eps must be finite and >= 0 (got %g)", a.eps);
     for (int i = 0; i < 3; ++i)
         if (a.q_stride[i] < 0 || a.k_stride[i] < 0 || a.v_stride[i] < 0 || a.q_out_stride[i] < 0) return fail(SPECGBV_EINVAL, "negative stride");
+    if (a.heads + 2 * static_cast<int64_t>(c.kv_heads) > (1 << 29)) return fail(SPECGBV_EUNSUPPORTED, "a token has more than 2^29 heads");
     if (c.sequences == 0 || a.tokens == 0) return SPECGBV_OK;
     if (!a.q || !a.k || !a.v || !a.q_out || !a.positions || (a.pairs > 0 && !a.inv_freq)) return fail(SPECGBV_EINVAL, "null input or output pointer");
     const size_t esz = element_bytes(c.dtype);
@@ -116,6 +117,7 @@ specgbv_status specgbv_cache_append(const specgbv_paged_cache *cache, const spec
     p.eps = static_cast<float>(a.eps); p.inv_dim = 1.0f / c.head_dim;
     p.heads = a.heads; p.kv_heads = c.kv_heads; p.head_dim = c.head_dim; p.pairs = a.pairs; p.interleaved = a.interleaved != 0;
     const hipError_t e = launch_append(p, c.dtype == SPECGBV_BF16 ? 1 : 0, width, static_cast<hipStream_t>(hip_stream));
+    if (e == hipErrorInvalidConfiguration) return fail(SPECGBV_EUNSUPPORTED, "too many tokens for one launch (%d)", p.tokens_all);
     if (e != hipSuccess) return fail(SPECGBV_EHIP, "append kernel launch: %s", hipGetErrorString(e));
     return SPECGBV_OK;
 }

@@ -4,6 +4,7 @@ import pytest
 import torch
 
 import paper_2604_25925_amd as sg
+import paper_2604_25925_amd.decoding  # noqa: F401
 
 pytestmark = pytest.mark.skipif(torch.cuda.is_available(), reason="addresses here are no GPU's: nothing may come to a launch")
 
@@ -145,3 +146,20 @@ def _tried(cache, q, positions, workspace=None, **kw):
         return e.status, workspace if workspace is not None else made[0]
     finally:
         torch.empty = empty
+
+
+def _sizes(S, T, H, G, D=64, page=16, width=600, prefixes=0):
+    """(cache, append's arguments, attention's arguments) of sizes that no tensors here have."""
+    P = 1 << 20
+    cache = sg.decoding._CACHE.pack(P, P, P, page * G * D, page * D, D, page * G * D, page * D, D, width, 9, G, page, D, S, width, 1, 0)
+    q, kv = (T * H * D, H * D, D), (T * G * D, G * D, D)
+    append = sg.decoding._APPEND.pack(P, P, P, P, P, 0, 0, 0, *q, *kv, *kv, *q, T, 1e-6, T, H, 0, 0)
+    attend = sg.decoding._ATTEND.pack(P, P, P, P if prefixes else 0, *q, *q, T, T, H, 0, prefixes, 0, 0.0)
+    return cache, append, attend
+
+
+@pytest.mark.parametrize("S,T,H,G,fits", [(1, 2 ** 25 - 2, 8, 2, True), (1, 2 ** 25 - 1, 8, 2, False), (5 * 10 ** 7, 1, 4, 1, False), (2 ** 24, 2, 1, 1, False),
+                                          (1, 1, 2 ** 29 - 2, 1, True), (1, 1, 2 ** 29, 1, False), (1, 1, 10 ** 9, 10 ** 9, False)])
+def test_appends_that_no_launch_holds(S, T, H, G, fits):
+    cache, append, _ = _sizes(S, T, H, G, D=8)
+    assert sg.load_library().specgbv_cache_append(cache, append, None) == (4 if fits else 2), sg.specgbv_last_error()
