@@ -922,7 +922,7 @@ hipError_t launch_one(AttendProblem p, hipStream_t stream)
     p.items = p.all_parts * p.kv_heads;
     p.by_blocks = Divider::of(p.row_blocks);
     const int64_t grid = WK == 0 ? (static_cast<int64_t>(p.items) * p.row_blocks + kWavesPerGroup - 1) / kWavesPerGroup : p.row_blocks == 1 ? p.items : static_cast<int64_t>((p.items + 7) / 8 * 8) * p.row_blocks;
-    if (grid >= INT64_C(1) << 24) return hipErrorInvalidConfiguration;        // (threads of a launch: below 2^32)
+    if (grid >= kLaunchGroups) return hipErrorInvalidConfiguration;
     hipLaunchKernelGGL((k_attend<T, DP, RT, WK, PARTS>), dim3(static_cast<unsigned>(grid)), dim3(kAttendThreads), 0, stream, p);
     return hipGetLastError();
 }
@@ -943,13 +943,15 @@ hipError_t launch_typed(AttendProblem p, hipStream_t stream)
 {
     p.in_order = Shape<T, DP>::kBf && !p.few;
     if (p.all_parts == p.units && !p.ml) return launch_rows<T, DP, false>(p, stream);
-    const hipError_t e = launch_rows<T, DP, true>(p, stream);
-    if (e != hipSuccess) return e;
     // Few parts (8 a unit on average): several rows per wave, so that all rows are on their way at once; many: a workgroup per row, so that
     // a row's parts are.
-    const int64_t rows = static_cast<int64_t>(p.sequences) * p.heads * p.tokens, per = kAttendThreads / (DP / 4);
-    if (p.all_parts <= 8 * p.units) hipLaunchKernelGGL((k_attend_join<T, DP>), dim3(static_cast<unsigned>((rows + per - 1) / per)), dim3(kAttendThreads), 0, stream, p);
-    else hipLaunchKernelGGL((k_attend_join_many<T, DP>), dim3(static_cast<unsigned>(rows)), dim3(kAttendThreads), 0, stream, p);
+    const bool few = p.all_parts <= 8 * p.units;
+    const int64_t rows = static_cast<int64_t>(p.sequences) * p.heads * p.tokens, per = few ? kAttendThreads / (DP / 4) : 1, grid = (rows + per - 1) / per;
+    if (grid >= kLaunchGroups) return hipErrorInvalidConfiguration;
+    const hipError_t e = launch_rows<T, DP, true>(p, stream);
+    if (e != hipSuccess) return e;
+    if (few) hipLaunchKernelGGL((k_attend_join<T, DP>), dim3(static_cast<unsigned>(grid)), dim3(kAttendThreads), 0, stream, p);
+    else hipLaunchKernelGGL((k_attend_join_many<T, DP>), dim3(static_cast<unsigned>(grid)), dim3(kAttendThreads), 0, stream, p);
     return hipGetLastError();
 }
 

@@ -212,6 +212,7 @@ specgbv_status specgbv_attend_paged(const specgbv_paged_cache *cache, const spec
     p.q_wide = allowed_width(unit, a.q, a.q_stride, 3, esz) == unit;
     p.out_wide = allowed_width(unit, a.out, a.out_stride, 3, esz) == unit;
     const hipError_t e = launch_attend(p, c.dtype == SPECGBV_BF16 ? 1 : 0, static_cast<hipStream_t>(hip_stream));
+    if (e == hipErrorInvalidConfiguration) return fail(SPECGBV_EUNSUPPORTED, "too many queries for one launch");
     if (e != hipSuccess) return fail(SPECGBV_EHIP, "attention kernel launch: %s", hipGetErrorString(e));
     return SPECGBV_OK;
 }

@@ -163,3 +163,11 @@ def _sizes(S, T, H, G, D=64, page=16, width=600, prefixes=0):
 def test_appends_that_no_launch_holds(S, T, H, G, fits):
     cache, append, _ = _sizes(S, T, H, G, D=8)
     assert sg.load_library().specgbv_cache_append(cache, append, None) == (4 if fits else 2), sg.specgbv_last_error()
+
+
+@pytest.mark.parametrize("S,T,H,G,prefixes,fits", [(2 ** 21 - 1, 1, 8, 8, 0, True), (2 ** 21, 1, 8, 8, 0, False), (2, 2 ** 20 - 1, 128, 128, 1, True),
+                                                   (2, 2 ** 20, 128, 128, 1, False)])
+def test_attention_that_no_launch_holds(S, T, H, G, prefixes, fits):
+    """By its own grid, and by that of the join behind it, before either is launched."""
+    cache, _, attend = _sizes(S, T, H, G, prefixes=prefixes)
+    assert sg.load_library().specgbv_attend_paged(cache, attend, 1 << 20, 1 << 50, None) == (4 if fits else 2), sg.specgbv_last_error()
