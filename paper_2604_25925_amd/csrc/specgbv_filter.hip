@@ -540,7 +540,7 @@ __global__ void __launch_bounds__(TH, 4) k_filter(FilterProblem p)
     filter_row<TH, T>(p, blockIdx.x, sh);
 }
 
-// bfloat16 rows of up to NV 8192 - 8 entries.
+// bfloat16 rows of up to NV 8 TH - 7 entries, and 65521 where the halves of the counters are not looked after.
 //
 // A bfloat16 has 2^15 magnitudes: the row is counted into one 32-bit counter each, entries in the low half and those below zero in the high
 // half, and everything about the order follows from the counts.  So an entry costs one addition in LDS, an exponential in
@@ -590,7 +590,7 @@ __global__ void __launch_bounds__(TH, 4) k_filter_counts(FilterProblem p)
     __shared__ uint32_t again[kMaxTurns / 32];                     // rows of this workgroup that are to be done over
     CountShared<TH> &sh = shared.c;
     constexpr bool kAhead = NV == 8 && TH == 1024;                 // the next row is loaded while this one is worked on
-    constexpr bool kMayOverflow = NV * TH > 8 * 1024;              // shorter rows hold fewer than 2^16 entries
+    constexpr bool kMayOverflow = NV * TH > 8 * 1024;              // fewer vectors than 2^13 hold fewer than 2^16 entries
     int tid = threadIdx.x;
     const int V = p.V;
     const uint16_t *logits = static_cast<const uint16_t *>(p.logits);
@@ -1016,7 +1016,7 @@ hipError_t launch_filter(const FilterProblem &p, int dtype, hipStream_t stream)
     // The fewest vectors a lane that hold the row (more cost registers and turns).  With these / the next ones, 100 rows, us: 32000 entries 15.6 / 17.6, 64000
     // 20.5 / 21.5 (600 rows, which load ahead, 60 / 63), 128256 28 / 32, 152064 36 / 77 (k_filter).
     if (dtype == 1 && span <= 4 * 8192) return launch_counts<4, 1024>(p, stream);
-    if (dtype == 1 && span <= 8 * 8192) return launch_counts<8, 1024>(p, stream);
+    if (dtype == 1 && span <= 8 * 8191) return launch_counts<8, 1024>(p, stream);          // (one vector less: its counters must not overflow)
     if (dtype == 1 && span <= 16 * 8192) return launch_counts<16, 1024>(p, stream);
     if (dtype == 1 && span <= 20 * 8192) return launch_counts<20, 1024>(p, stream);
     // A row a compute unit: 16 waves each; more: 8, so that two rows share a unit and one's waits are the other's work.  16 / 8 waves, us:
