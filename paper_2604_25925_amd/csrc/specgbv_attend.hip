@@ -92,11 +92,6 @@ template <typename T> __device__ __forceinline__ uint32_t exponents_full(uint32_
 
 // A sequence's row of the table through scalar loads: it is read by whole waves, and nothing in the kernel writes it.
 typedef const int32_t __attribute__((address_space(4))) *ConstTable;
-__device__ __forceinline__ Place place_in(const PageMap &m, ConstTable table, int32_t pos)
-{
-    const int32_t n = m.page.div(pos), page = table[n];         // pos lies in front of the table's end
-    return {static_cast<uint32_t>(page) < static_cast<uint32_t>(m.pages) ? page : -1, m.page.mod(pos, n)};
-}
 
 // One entry's bits against a kind of value that is not finite: 0 not a number, 1 +inf, 2 -inf.
 template <typename T> __device__ __forceinline__ bool is_kind(uint32_t e, int kind)
