@@ -510,7 +510,8 @@ size_t specgbv_attend_workspace_bytes(const specgbv_paged_cache *cache, const sp
  *   top_p < 1      keeps of these the entries in front of which less than top_p of their weight lies (never fewer than one);
  * the token is the first kept entry up to and including which more than u times the kept weight lies (the last kept one where
  * rounding leaves none).  temperature <= 0 keeps the first entry alone.  A row without entries gets token -1 and keeps nothing;
- * where a logit is +inf, the entries at +inf weigh 1 and the others nothing.  NaN counts as -inf; min_p above 1 counts as 1.
+ * where a logit is +inf, the entries at +inf weigh 1 and the others nothing.  NaN counts as -inf; min_p above 1 counts as 1, which keeps
+ * the entries that equal the largest.
  * Running weights are float64 sums in an order that does not change from call to call.  What is added up is float64 (bfloat16 rows of
  * up to 163833 entries: counts times the weight of a value) or, in bins of 1/64 of an octave, integers: weights then are rounded to
  * 2^-(7 + 64 - 2 c) of themselves, c the bits of V (2^-41 at V = 32003, 2^-35 at 152064).

@@ -390,6 +390,12 @@ struct RowAsked {
         k = asked > 0 ? asked : INT32_MAX;
         if (!(temperature > 0.0f)) { temperature = 1.0f; k = 1; }
     }
+    // 1 / temperature.  min_p = 1 leaves the entries that equal the largest, and of these no temperature changes the weight: a factor that
+    // takes every other weight to 0 keeps out those that would round to 1.
+    __device__ __forceinline__ double per_temperature() const
+    {
+        return min_p == 1.0f && temperature < INFINITY ? 1e300 : 1.0 / static_cast<double>(temperature);
+    }
 };
 
 // A row of any length and type, read from memory in every step.
@@ -420,7 +426,7 @@ __device__ __forceinline__ void filter_row(const FilterProblem &p, int r, Filter
     if (most != kNothing) {                                 // uniform
         RowRule rule;
         rule.top = value_of(most);
-        rule.inv_t = 1.0 / static_cast<double>(temperature);
+        rule.inv_t = asked.per_temperature();
         rule.per = rule.inv_t * (64.0 * 1.44269504088896340736);
         const int length = 32 - __clz(V);                   // bits of V
         rule.shift = 64 - length;
@@ -769,7 +775,7 @@ __global__ void __launch_bounds__(TH, 4) k_filter_counts(FilterProblem p)
             // bits of the value of a counter
             auto value_bits = [&](uint32_t c) { return TH == 1024 || c == 0 ? c : kLowest + c; };
             const float top_z = __uint_as_float((top >= 0x8000u ? value_bits(top - 0x8000u) : 0x8000u | value_bits(0x7FFFu - top)) << 16);
-            const double inv_t = 1.0 / static_cast<double>(asked.temperature), min_w = asked.min_p > 0.0f ? static_cast<double>(asked.min_p) : 0.0;
+            const double inv_t = asked.per_temperature(), min_w = asked.min_p > 0.0f ? static_cast<double>(asked.min_p) : 0.0;
             auto weight = [&](uint32_t bits) {
                 const float z = __uint_as_float(bits << 16);
                 return z == top_z ? 1.0 : exp_from(sh.of_octave, (static_cast<double>(z) - static_cast<double>(top_z)) * inv_t);
