@@ -514,7 +514,10 @@ size_t specgbv_attend_workspace_bytes(const specgbv_paged_cache *cache, const sp
  * the entries that equal the largest.
  * Running weights are float64 sums in an order that does not change from call to call.  What is added up is float64 (bfloat16 rows of
  * up to 163833 entries: counts times the weight of a value) or, in bins of 1/64 of an octave, integers: weights then are rounded to
- * 2^-(7 + 64 - 2 c) of themselves, c the bits of V (2^-41 at V = 32003, 2^-35 at 152064).
+ * 2^-(7 + 64 - 2 c) of themselves, c the bits of V (2^-41 at V = 32003, 2^-35 at 152064, 2^-29 at 1048576), and those below 2^-64 of
+ * the largest (2^-63.98) count as 0.  The latter holds for float32 rows, longer bfloat16 rows, bfloat16 rows that hold one magnitude 65536
+ * times or more and, in calls of more rows than the GPU has compute units with V <= 32761, bfloat16 rows that hold a magnitude of 2^-63 and
+ * below other than 0, of nearly 2^65 and above other than -inf, or NaN.
  *
  *   logits       device, [rows, V], rows row_stride entries apart
  *   temperature, top_p, min_p   device, [rows] float32, or NULL (1, 1, 0);   top_k  device, [rows] int32, or NULL (0)

@@ -9,7 +9,7 @@
 // so the rotation stays within a lane, and a head is a power of two of lanes, so its norm is a few exchanges in a wave.  W is 16
 // bytes where pairs, strides and addresses allow it.
 //
-// 5 prompts of up to 4001 tokens, 32 heads and 8 kv heads of 128, bfloat16: 330 MB in 73 us, 4.5 TB/s (a copy 4.8).  256 tokens with norms: 6.1 us;
+// 5 prompts of up to 4001 tokens, 32 heads and 8 kv heads of 128, bfloat16: 330 MB in 73 us, 4.5 TB/s (a copy 4.8).  256 tokens with norms: 6.0 us;
 // one token: 2.9; both the latency of position, table, input and store in a row.
 #include "specgbv_internal.hpp"
 

@@ -27,11 +27,11 @@
 // workgroups have the same number of keys to read (share_of); k_attend_join brings the parts of a row to the largest reference.
 //
 // What bounds it, with times on one card (kernel, then join).  4 sequences of 131072 tokens, one query each of 32 heads on 8 kv heads of 128,
-// bfloat16: the reads, 2.14 GB in 356 + 5 us, 6.0 TB/s.  32 prefixes of up to 2048 tokens with 8 drafts: 49 + 7 us, 2.2 times the time of its 152 MB; half of it
+// bfloat16: the reads, 2.14 GB in 355 + 5 us, 6.0 TB/s.  32 prefixes of up to 2048 tokens with 8 drafts: 49 + 6 us, 2.2 times the time of its 152 MB; half of it
 // is the start (lengths, positions, table, first tile: loads that wait for each other) and the drafts' own keys.  8 prefixes of up to 4096 tokens,
-// 8 drafts, 9 queries each: 61 + 11 us for 88 MB and 22 GFLOP; matrix instructions are under way for 17 % of the time, the rest are waits for the
+// 8 drafts, 9 queries each: 59 + 10 us for 88 MB and 22 GFLOP; matrix instructions are under way for 17 % of the time, the rest are waits for the
 // shared tiles and each other with two waves per SIMD (registers leave no third), and the 48 MB of parts that are written and read.  24 float32 sequences, 5 queries of 14 heads on
-// 2 kv heads of 64, window 1000: 20 + 4 us against 2.7 for its bytes: latency of 4 tiles per wave.  One query: 5.7 us, all latency.
+// 2 kv heads of 64, window 1000: 20 + 4 us against 2.7 for its bytes: latency of 4 tiles per wave.  One query: 5.9 us, all latency.
 #include "specgbv_internal.hpp"
 
 namespace specgbv {
@@ -629,7 +629,9 @@ __global__ void __launch_bounds__(kAttendThreads, (Shape<T, DP>::waves(RT))) k_a
             }
         }
 
-        // sums of values: entries x rows
+        // sums of values: entries x rows.  bfloat16 values meet weights rounded to bfloat16, the one pair the matrix instructions take (a product in float32
+        // has an eighth of their rate): results are off by 0.0018 to 0.0024 of themselves against 64 bits where their own rounding makes 0.0017 (root mean
+        // square, 40 to 16384 keys).  The sum of weights has them unrounded; the rounded ones there change this in the third digit only.
         if constexpr (S::kBf) {
             B8 w[RT];
 #pragma unroll

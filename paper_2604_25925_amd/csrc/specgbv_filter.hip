@@ -6,9 +6,9 @@
 // bin's entries are put in order.
 //
 // What bounds it.  One row is a chain of passes and searches in one workgroup, and a workgroup's waits are covered only where two share a
-// compute unit.  bfloat16 (k_filter_counts): 256 rows of 128256 entries, tokens, 33.6 us (loads and counts 9, weights of the values that occur 5, places 3,
-// indices 4, launch and the spread of the loads over the card the rest; the bytes alone 13.6); 1152 rows of 32000, truncated rows, 57 us (30.5; 76 with one workgroup
-// a compute unit); one row of 32000 13.2.  float32 (k_filter): 287 rows of 32003, tokens and rows, 52 us (15.2): a row is read from memory for its
+// compute unit.  bfloat16 (k_filter_counts): 256 rows of 128256 entries, tokens, 33.3 us (loads and counts 9, weights of the values that occur 5, places 3,
+// indices 4, launch and the spread of the loads over the card the rest; the bytes alone 13.6); 1152 rows of 32000, truncated rows, 56 us (30.5; 76 with one workgroup
+// a compute unit); one row of 32000 13.3.  float32 (k_filter): 287 rows of 32003, tokens and rows, 53 us (15.2): a row is read from memory for its
 // largest value (7), for the histogram (9, the additions in LDS), for each place that is looked for (4 - 5) and for the output.
 //
 // Weights decide which entry is drawn, and every entry counts, so they are held to more than float32: the histogram's sums are sums of
