@@ -308,7 +308,7 @@ def _handle(s):
     """The handle of the cache is kept between the steps of a decoding loop."""
     import paper_2604_25925_amd as sg
     if "handle" not in s:
-        s["handle"] = sg.PagedCache4(s["k"], s["v"], s["k_scale"], s["v_scale"], s["table"], DTYPES[s["case"]["dtype"]])
+        s["handle"] = sg.PackedCache(s["k"], s["v"], s["k_scale"], s["v_scale"], s["table"], DTYPES[s["case"]["dtype"]])
         s["out"] = torch.empty(s["q"].shape, dtype=s["q"].dtype, device=DEVICE)
         s["workspace"] = None
     return sg, s["handle"]
@@ -317,7 +317,7 @@ def _handle(s):
 def _own_attend(s):
     """The workspace and the output are kept as well."""
     sg, cache = _handle(s)
-    s["out"], s["workspace"] = sg.specgbv_attend4_paged(cache, s["q"], s["positions"], window=s["case"]["window"], shared_len=s["shared_len"],
+    s["out"], s["workspace"] = sg.specgbv_packed_attend(cache, s["q"], s["positions"], window=s["case"]["window"], shared_len=s["shared_len"],
                                                         max_len=s["max_len"], out=s["out"], workspace=s["workspace"])
     return {"out": s["out"]}
 
@@ -327,9 +327,9 @@ def _own_append(s):
     sg, cache = _handle(s)
     if "seen" not in s:
         s["seen"] = [torch.empty(s["new_k"].shape, dtype=s["new_k"].dtype, device=DEVICE) for _ in range(2)]
-    sg.specgbv_cache4_append(cache, s["q"], s["new_k"], s["new_v"], s["positions"], inv_freq=s["inv_freq"],
+    sg.specgbv_packed_append(cache, s["q"], s["new_k"], s["new_v"], s["positions"], inv_freq=s["inv_freq"],
                              interleaved=s["case"]["interleaved"], q_weight=s["q_weight"], k_weight=s["k_weight"], eps=s["eps"], out=s["out"])
-    k, v = sg.specgbv_cache4_read(cache, s["positions"], k=s["seen"][0], v=s["seen"][1])
+    k, v = sg.specgbv_packed_read(cache, s["positions"], k=s["seen"][0], v=s["seen"][1])
     return {"q": s["out"], "k": k, "v": v}
 
 
