@@ -502,6 +502,127 @@ specgbv_status specgbv_attend_paged(const specgbv_paged_cache *cache, const spec
 size_t specgbv_attend_workspace_bytes(const specgbv_paged_cache *cache, const specgbv_attend_args *args);
 
 /*
+ * A cache held in 4 bits.  An entry is a 4-bit code (bit 3 the sign, bits 2 and 1 an exponent, bit 0 a mantissa bit: 0, 1/2, 1, 3/2, 2, 3, 4, 6)
+ * times a power of two that 32 adjacent entries of a head share.  Entry i of token t of (page, head, slot) is the low (i even) or high half of
+ * the byte k[page * k_page_stride + head * k_head_stride + slot * k_token_stride + i / 2], and its power 2^(b - 127) with the byte
+ * b = k_scale[page * k_scale_page_stride + head * k_scale_head_stride + (i / 32) * k_scale_block_stride + slot]: the scales of a block's tokens
+ * lie next to each other.  The same for v; strides are in bytes.  b = 255 marks a block that is no number; 253 and 254 are not used (a query
+ * that sees such entries may get what is not finite).
+ *
+ * Table, pages and limits are those of specgbv_paged_cache, and head_dim is a multiple of 32; k_scale and v_scale are 8-byte aligned with
+ * strides of whole 8 bytes, blocks at most 2^26 bytes apart.
+ */
+typedef struct {
+    void *k, *v;               /* device, uint8 */
+    void *k_scale, *v_scale;   /* device, uint8 */
+    const int32_t *table;      /* device, [sequences, table_width], rows table_stride entries apart; may be NULL where sequences = 0 */
+    int64_t k_page_stride, k_head_stride, k_token_stride;
+    int64_t v_page_stride, v_head_stride, v_token_stride;
+    int64_t k_scale_page_stride, k_scale_head_stride, k_scale_block_stride;
+    int64_t v_scale_page_stride, v_scale_head_stride, v_scale_block_stride;
+    int64_t table_stride;      /* in entries */
+    int32_t pages, kv_heads, page_size, head_dim, sequences, table_width;
+    int32_t dtype;             /* specgbv_dtype of every q, k, v, out and weight used with the cache */
+    int32_t reserved;          /* 0 */
+} specgbv_packed_cache;
+
+/*
+ * specgbv_packed_append: as specgbv_cache_append, with keys and values stored in 4 bits.  Of a block of 32 entries y, with A = max |y|, the power is the
+ * least 2^e with A <= 7 * 2^e, e in [-120, 125], and an entry becomes the nearest of the values above times 2^e, of two as near the one of even code,
+ * +-6 * 2^e beyond 5 * 2^e; a block that holds an entry that is not finite is marked by the byte 255.  Keys are normalised, rotated and
+ * rounded in float64, so a code differs from the definition's only where the entry lies within 2^-50 of itself of a border; queries as in
+ * specgbv_cache_append.
+ */
+specgbv_status specgbv_packed_append(const specgbv_packed_cache *cache, const specgbv_append_args *args, void *hip_stream);
+
+/*
+ * specgbv_packed_read: keys and values of tokens as the cache holds them, k[s, t] and v[s, t] of the token at positions[s, t] of sequence s; 0 where the
+ * position lies below 0 or behind the table's width or its page is not there.
+ */
+typedef struct {
+    void *k, *v;               /* device out, [sequences, tokens, kv_heads, head_dim] of the cache's dtype, entries of a head adjacent */
+    const int32_t *positions;  /* device, [sequences, tokens], rows positions_stride entries apart */
+    int64_t k_stride[3], v_stride[3];   /* sequence, token, head; in elements */
+    int64_t positions_stride;
+    int32_t tokens, reserved;
+} specgbv_read_args;
+
+specgbv_status specgbv_packed_read(const specgbv_packed_cache *cache, const specgbv_read_args *args, void *hip_stream);
+
+/*
+ * specgbv_packed_attend: specgbv_attend_paged over a cache held in 4 bits; drafts of a prefix, windows, padding and max_len as there.  The cache's entries enter
+ * as they are; with bfloat16 the weights are rounded to bfloat16 for the product that sums the values, with float32 queries and weights keep
+ * their 24 bits.
+ */
+specgbv_status specgbv_packed_attend(const specgbv_packed_cache *cache, const specgbv_attend_args *args,
+                                     void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/* As specgbv_attend_workspace_bytes: one size for any max_len. */
+size_t specgbv_packed_attend_workspace_bytes(const specgbv_packed_cache *cache, const specgbv_attend_args *args);
+
+/*
+ * Pages dealt out to requests on the device.  A request is a prefix with `drafts` sequences (1: a sequence by itself); sequence b * drafts + k is a row of the
+ * table.  held[b] = (w, h) says that entries [0, w) of the request's rows are pages that its drafts share and entries [w, h) pages of each draft's own; the
+ * others are -1.  Free pages are ring[(head + i) % pages], i < count, with ends = (head, count).  At the start table is -1, held 0, ring any order of the pages
+ * that may be dealt out, ends = (0, their number).  No page may be in the ring twice, or there and in the table.
+ */
+typedef struct {
+    int32_t *table;            /* device, [prefixes * drafts, table_width], rows table_stride entries apart */
+    int32_t *ring;             /* device, [pages]                                             */
+    int32_t *ends;             /* device, [2]: head, count                                    */
+    int32_t *held;             /* device, [prefixes, 2]                                       */
+    int64_t table_stride;
+    int32_t pages, page_size, prefixes, drafts, table_width;
+    int32_t reserved;          /* 0 */
+} specgbv_page_pool;
+
+/*
+ * specgbv_pages_advance: brings every request's pages to its length, between two steps of a decoding loop.  With length[b] tokens that stay (0 and below: the
+ * request has ended) and `room` more that the next step may write, the request wants h' = ceil((length + room) / page_size) pages, w' = length / page_size of them
+ * shared (0 and 0 where it has ended).  The draft chosen[b] (NULL: 0; taken into [0, drafts - 1]) wrote the tokens since the last call: its pages [w, w') become those of
+ * all drafts; what a draft has and no longer wants is given back, what it wants and has not is taken.  So pages that the drafts share are
+ * dealt out once, and a new request has them at once.
+ *   served[b]      1: as above;  0: more pages were needed than there are;  -1: h' exceeds table_width.  A request that is not served keeps what it has.
+ *   shared_len[b]  tokens in pages that the drafts share now: w * page_size (for specgbv_attend_paged)
+ * Order.  Requests that take no more than they give are all served.  The others are served in their order while pages suffice, counting every page
+ * given back in this call; from the first that does not fit on none is.  Pages given back go behind the ring's last, and pages are taken from
+ * its head, both by request, in it the chosen draft first and then the others, in a row by entry: the same state gives the same tables.
+ * The device only looks at numbers that it can trust: w and h beyond the width, ends beyond the pages are taken into their range.
+ * Limits: pages < 2^30, rows times table_width at most 2^30, table_width * page_size at most 2^30.
+ */
+typedef struct {
+    const int32_t *length;     /* device, [prefixes] */
+    const int32_t *chosen;     /* device, [prefixes], or NULL */
+    int32_t *shared_len;       /* device out, [prefixes] */
+    int32_t *served;           /* device out, [prefixes] */
+    int32_t room, reserved;
+} specgbv_advance_args;
+
+specgbv_status specgbv_pages_advance(const specgbv_page_pool *pool, const specgbv_advance_args *args, void *workspace, size_t workspace_bytes,
+                                     void *hip_stream);
+
+/* Bytes of device workspace (256-byte aligned, contents of no matter) specgbv_pages_advance needs; 0 if it needs none or the pool is invalid. */
+size_t specgbv_pages_workspace_bytes(const specgbv_page_pool *pool);
+
+/*
+ * specgbv_slot_map: where new tokens lie.  Sequence s = b * drafts + k has count[b] tokens (taken into [0, tokens]) at positions start[b], start[b] + 1, ...; they stand in the
+ * first places of its row, or with right != 0 in the last ones, and the others are padding.
+ *   positions[s, t]  the token's position, -1: padding (also where it lies below 0 or beyond 2^31 - 1)
+ *   slots[s, t]      page * page_size + slot of its place in a cache, -1: padding, behind the table's width, or no page
+ */
+typedef struct {
+    const int32_t *table;      /* device, [sequences, table_width], rows table_stride entries apart; may be NULL where slots is */
+    const int32_t *start, *count;   /* device, [sequences / drafts] */
+    int32_t *positions;        /* device out, [sequences, tokens], rows positions_stride entries apart */
+    int64_t *slots;            /* device out, [sequences, tokens], rows slots_stride entries apart, or NULL */
+    int64_t table_stride, positions_stride, slots_stride;
+    int32_t sequences, drafts, table_width, page_size, pages, tokens, right;
+    int32_t reserved;          /* 0 */
+} specgbv_slot_args;
+
+specgbv_status specgbv_slot_map(const specgbv_slot_args *args, void *hip_stream);
+
+/*
  * specgbv_sample_filtered: truncated distributions and draws from them, by given uniforms.  The entries of a row that are not
  * -inf are ordered by logit, the largest first, ties by the lowest index first, and weigh w = exp((z - max z) / temperature).  In
  * this order

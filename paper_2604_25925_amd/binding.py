@@ -23,7 +23,9 @@ _ALGO = {"auto": ALGO_AUTO, "split": ALGO_SPLIT, "chain": ALGO_CHAIN}
 EXPORTS = ("specgbv_workspace_bytes", "specgbv_verify", "specgbv_verify_static", "specgbv_verify_ex", "specgbv_verify_kseq", "specgbv_read_kseq_intermediates", "specgbv_read_intermediates",
            "specgbv_workspace_carry", "specgbv_modify_target", "specgbv_modify_workspace_bytes", "specgbv_sample_tokens", "specgbv_sample_workspace_bytes",
            "specgbv_read_sample_intermediates", "specgbv_carry_advance", "specgbv_carry_workspace_bytes", "specgbv_pending_state_bytes", "specgbv_cache_append", "specgbv_attend_paged",
-           "specgbv_attend_workspace_bytes", "specgbv_sample_filtered", "specgbv_filter_workspace_bytes", "specgbv_last_error", "specgbv_version")
+           "specgbv_attend_workspace_bytes", "specgbv_sample_filtered", "specgbv_filter_workspace_bytes", "specgbv_packed_append", "specgbv_packed_read",
+           "specgbv_packed_attend", "specgbv_packed_attend_workspace_bytes", "specgbv_pages_advance", "specgbv_pages_workspace_bytes", "specgbv_slot_map",
+           "specgbv_last_error", "specgbv_version")
 
 
 class SpecGBVError(RuntimeError):
@@ -113,6 +115,20 @@ def load_library() -> ctypes.CDLL:
     L.specgbv_attend_paged.restype = c_int
     L.specgbv_attend_workspace_bytes.argtypes = [c_void_p, c_void_p]
     L.specgbv_attend_workspace_bytes.restype = c_size_t
+    L.specgbv_packed_append.argtypes = [c_void_p, c_void_p, c_void_p]
+    L.specgbv_packed_append.restype = c_int
+    L.specgbv_packed_read.argtypes = [c_void_p, c_void_p, c_void_p]
+    L.specgbv_packed_read.restype = c_int
+    L.specgbv_packed_attend.argtypes = [c_void_p, c_void_p, c_void_p, c_size_t, c_void_p]
+    L.specgbv_packed_attend.restype = c_int
+    L.specgbv_packed_attend_workspace_bytes.argtypes = [c_void_p, c_void_p]
+    L.specgbv_packed_attend_workspace_bytes.restype = c_size_t
+    L.specgbv_pages_advance.argtypes = [c_void_p, c_void_p, c_void_p, c_size_t, c_void_p]
+    L.specgbv_pages_advance.restype = c_int
+    L.specgbv_pages_workspace_bytes.argtypes = [c_void_p]
+    L.specgbv_pages_workspace_bytes.restype = c_size_t
+    L.specgbv_slot_map.argtypes = [c_void_p, c_void_p]
+    L.specgbv_slot_map.restype = c_int
     L.specgbv_sample_filtered.argtypes = [c_void_p, ctypes.c_int64, c_int, c_int, c_int, c_void_p, c_void_p, c_void_p, c_void_p,
                                           c_void_p, c_void_p, c_void_p, ctypes.c_int64, c_void_p, c_size_t, c_void_p]
     L.specgbv_sample_filtered.restype = c_int

@@ -10,8 +10,9 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libspecgbv.so")
 SOURCES = ["specgbv_api.hip", "specgbv_split.hip", "specgbv_rows.hip", "specgbv_chain.hip", "specgbv_decide.hip", "specgbv_modify.hip", "specgbv_sample.hip", "specgbv_kseq.hip",
-           "specgbv_append.hip", "specgbv_attend.hip", "specgbv_filter.hip", "specgbv_step_api.hip"]
-HEADERS = ["specgbv_device.hpp", "specgbv_internal.hpp", "specgbv_paged.hpp", os.path.join("..", "..", "include", "specgbv.h")]
+           "specgbv_append.hip", "specgbv_attend.hip", "specgbv_filter.hip", "specgbv_packed.hip", "specgbv_packed_attend.hip", "specgbv_pages.hip",
+           "specgbv_step_api.hip"]
+HEADERS = ["specgbv_device.hpp", "specgbv_internal.hpp", "specgbv_paged.hpp", "specgbv_attend.hpp", os.path.join("..", "..", "include", "specgbv.h")]
 FLAGS = ["-O3", "--offload-arch=gfx950", "-fPIC", "-std=c++17", "-Wall", "-Wno-unused-function",
          # packed-FP32 instructions are not to be generated on the test machines
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]

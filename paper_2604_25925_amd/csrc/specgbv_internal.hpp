@@ -205,6 +205,77 @@ size_t attend_bytes(int sequences, int drafts, bool shared, int tokens, int head
                     int64_t held);
 hipError_t launch_attend(const AttendProblem &p, int dtype, hipStream_t stream);
 
+// Attention over a paged cache of 4-bit entries: the same with strides of k and v in bytes, and the blocks' powers of two.
+struct PackedProblem {
+    AttendProblem a;
+    const uint8_t *k_scale, *v_scale;
+    int32_t k_scale_page_stride, k_scale_head_stride, k_scale_block_stride, v_scale_page_stride, v_scale_head_stride, v_scale_block_stride;
+    int near;                      // every byte of a head lies less than 2^32 bytes behind its first one, in each of the four arrays
+    Divider by_strip;              // workgroups next to each other on an XCD (set by the launch)
+};
+AttendPlan plan_packed_attend(int sequences, int drafts, bool shared, int tokens, int heads, int kv_heads, int head_dim, int element_bytes, int window,
+                              int64_t longest);
+// Most that plan_packed_attend asks for with any `longest` up to `held`.
+size_t packed_attend_bytes(int sequences, int drafts, bool shared, int tokens, int heads, int kv_heads, int head_dim, int element_bytes, int window,
+                           int64_t held);
+hipError_t launch_packed_attend(const PackedProblem &p, int dtype, hipStream_t stream);
+
+// Appending to a paged cache of 4-bit entries (see specgbv_packed_append); strides of q, k, v in elements, of the cache in bytes.
+struct PackedAppendProblem {
+    const void *q, *k, *v;
+    void *q_out;
+    uint8_t *k_cache, *v_cache, *k_scale, *v_scale;
+    const void *q_weight, *k_weight;
+    const int32_t *positions;
+    const double *inv_freq;
+    PageMap map;
+    Divider by_tokens, by_heads;   // tokens of a sequence; heads of q, k and v together
+    int64_t q_stride[3], k_stride[3], v_stride[3], q_out_stride[3];
+    int64_t k_cache_stride[3], v_cache_stride[3], k_scale_stride[3], v_scale_stride[3];      // page, head, slot; of the scales page, head, block
+    int64_t positions_stride;
+    double eps;
+    int tokens_all, heads, kv_heads, head_dim, pairs, interleaved;
+    int lane_bits, block_tokens;   // set by launch_packed_append
+};
+// wide: strides and addresses allow 16-byte loads, and a vector's partners in the rotation are a vector.
+hipError_t launch_packed_append(const PackedAppendProblem &p, int dtype, bool wide, hipStream_t stream);
+
+struct PackedReadProblem {
+    const uint8_t *k_cache, *v_cache, *k_scale, *v_scale;
+    void *k, *v;
+    const int32_t *positions;
+    PageMap map;
+    Divider by_tokens, by_heads;   // tokens of a sequence; kv heads, twice
+    int64_t k_cache_stride[3], v_cache_stride[3], k_scale_stride[3], v_scale_stride[3], k_stride[3], v_stride[3], positions_stride;
+    int tokens_all, kv_heads, head_dim;
+    int lane_bits;                 // set by launch_packed_read
+};
+hipError_t launch_packed_read(const PackedReadProblem &p, int dtype, bool wide, hipStream_t stream);
+
+// Pages of requests (see specgbv_pages_advance).
+struct PagesProblem {
+    int32_t *table, *ring, *ends, *held;
+    const int32_t *length, *chosen;
+    int32_t *shared_len, *served;
+    void *plan;                    // in the workspace
+    int64_t table_stride;
+    Divider by_page;
+    int pages, prefixes, drafts, width, room;
+};
+size_t pages_bytes(int prefixes, int drafts, int width);
+hipError_t launch_pages(const PagesProblem &p, hipStream_t stream);
+
+struct SlotsProblem {
+    PageMap map;
+    const int32_t *start, *count;
+    int32_t *positions;
+    int64_t *slots;
+    int64_t positions_stride, slots_stride;
+    Divider by_tokens, by_drafts;
+    int sequences, tokens, right;
+};
+hipError_t launch_slots(const SlotsProblem &p, hipStream_t stream);
+
 // Truncated distributions and draws from them (see specgbv_sample_filtered).
 struct FilterProblem {
     const void *logits;

@@ -1,5 +1,7 @@
-"""Binding of the decoding step around the verification: a paged cache of keys and values, attention over it and draws
+"""Binding of the decoding step around the verification: a paged cache of keys and values, attention over it, block tables, and draws
 from truncated distributions.  Argument marshalling only, as in ``binding``.
+
+A cache may also hold its entries in 4 bits (``PackedCache``), and pages can be dealt out to requests on the GPU (``PagePool``).
 
 The arguments of a call travel in one C structure (``specgbv_append_args``, ``specgbv_attend_args``), packed by the standard
 library's ``struct`` with the C compiler's own alignment: for calls of a few microseconds of GPU time the two dozen conversions of a
@@ -14,10 +16,15 @@ import torch
 
 from .binding import BF16, F32, _check, _scratch, load_library
 
-# specgbv_paged_cache, specgbv_append_args and specgbv_attend_args of the C header, field by field
+# specgbv_paged_cache, specgbv_append_args, specgbv_attend_args and so on of the C header, field by field
 _CACHE = struct.Struct("@PPP7q8i")
 _APPEND = struct.Struct("@PPPPPPPP12qqd4i")
 _ATTEND = struct.Struct("@PPPP6qq5if")
+_PACKED = struct.Struct("@PPPPP13q8i")
+_READ = struct.Struct("@PPP6qq2i")
+_POOL = struct.Struct("@PPPPq6i")
+_ADVANCE = struct.Struct("@PPPP2i")
+_SLOTS = struct.Struct("@PPPPP3q8i")
 
 _DTYPES = {torch.float32: F32, torch.bfloat16: BF16}
 
@@ -37,33 +44,16 @@ def _between(stride: int, rows: int, length: int) -> int:
     return stride if rows > 1 else max(stride, length)
 
 
-class PagedCache:
-    """Keys and values in pages: k and v [pages, kv_heads, page_size, head_dim] (bfloat16 or float32, the last dimension
-    dense; a page may hold its tokens before its heads: pass the transposed view) and table [sequences, width] int32: token t of sequence
-    s lies in slot t % page_size of page table[s, t // page_size] (rows of the table, and of positions, may lie apart, but not overlap).
-    The tensors stay the caller's: what is written to them, the table included, is what the next call sees.  A table entry outside
-    [0, pages) is a page that is not there."""
+def _on(index: int, call, *args):
+    """The call with the GPU `index` as the current one, which a launch on its streams needs."""
+    if index < 0 or index == torch.cuda.current_device():
+        return call(*args)
+    with torch.cuda.device(index):
+        return call(*args)
 
-    def __init__(self, k, v, table):
-        if k.dim() != 4 or k.shape != v.shape or k.dtype != v.dtype:
-            raise ValueError("k and v must be [pages, kv_heads, page_size, head_dim] of one dtype, got %s and %s" %
-                             (tuple(k.shape), tuple(v.shape)))
-        if k.dtype not in _DTYPES:
-            raise TypeError("a cache holds float32 or bfloat16, got %s" % k.dtype)
-        if table.dim() != 2 or table.dtype != torch.int32:
-            raise ValueError("table must be int32 [sequences, width]")
-        if not (k.is_cuda and v.device == k.device and table.device == k.device):
-            raise ValueError("k, v and table must live on one GPU")
-        if k.stride(3) != 1 or v.stride(3) != 1 or (table.shape[1] > 1 and table.stride(1) != 1):
-            raise ValueError("the last dimension of k, v and table must be dense")
-        self.k, self.v, self.table = k, v, table
-        self.pages, self.kv_heads, self.page_size, self.head_dim = k.shape
-        self.sequences, self.width = table.shape
-        self.dtype, self.device, self._index = k.dtype, k.device, k.get_device()
-        ks, vs = k.stride(), v.stride()
-        self._c = _CACHE.pack(k.data_ptr(), v.data_ptr(), table.data_ptr(), ks[0], ks[1], ks[2], vs[0], vs[1], vs[2],
-                              _between(table.stride(0), self.sequences, self.width), self.pages, self.kv_heads, self.page_size, self.head_dim,
-                              self.sequences, self.width, _DTYPES[k.dtype], 0)
+
+class _Cache:
+    """What calls look at whatever a cache's entries are: sequences, head_dim, dtype and device."""
 
     def _heads(self, name, x, heads=None):
         """Tokens, heads and strides of x [sequences, tokens, heads, head_dim]."""
@@ -91,12 +81,36 @@ class PagedCache:
         return _between(s[0], shape[0], tokens)
 
 
-def specgbv_cache_append(cache: PagedCache, q, k, v, positions, *, inv_freq=None, interleaved: bool = False, q_weight=None,
-                         k_weight=None, eps: float = 1e-6, out=None, stream: Optional[int] = None):
-    """Enqueue the append of new tokens: heads of q [S, T, heads, D] and k [S, T, kv_heads, D] are normalised (where q_weight /
-    k_weight [D] are given) and rotated by positions [S, T] * inv_freq (float64, [pairs]; entries behind 2 * pairs stay); k and v
-    go to the cache.  Positions below 0 are padding.  Returns the rotated queries (`out`; q itself may be given)."""
-    lib = load_library()
+class PagedCache(_Cache):
+    """Keys and values in pages: k and v [pages, kv_heads, page_size, head_dim] (bfloat16 or float32, the last dimension
+    dense; a page may hold its tokens before its heads: pass the transposed view) and table [sequences, width] int32: token t of sequence
+    s lies in slot t % page_size of page table[s, t // page_size] (rows of the table, and of positions, may lie apart, but not overlap).
+    The tensors stay the caller's: what is written to them, the table included, is what the next call sees.  A table entry outside
+    [0, pages) is a page that is not there."""
+
+    def __init__(self, k, v, table):
+        if k.dim() != 4 or k.shape != v.shape or k.dtype != v.dtype:
+            raise ValueError("k and v must be [pages, kv_heads, page_size, head_dim] of one dtype, got %s and %s" %
+                             (tuple(k.shape), tuple(v.shape)))
+        if k.dtype not in _DTYPES:
+            raise TypeError("a cache holds float32 or bfloat16, got %s" % k.dtype)
+        if table.dim() != 2 or table.dtype != torch.int32:
+            raise ValueError("table must be int32 [sequences, width]")
+        if not (k.is_cuda and v.device == k.device and table.device == k.device):
+            raise ValueError("k, v and table must live on one GPU")
+        if k.stride(3) != 1 or v.stride(3) != 1 or (table.shape[1] > 1 and table.stride(1) != 1):
+            raise ValueError("the last dimension of k, v and table must be dense")
+        self.k, self.v, self.table = k, v, table
+        self.pages, self.kv_heads, self.page_size, self.head_dim = k.shape
+        self.sequences, self.width = table.shape
+        self.dtype, self.device, self._index = k.dtype, k.device, k.get_device()
+        ks, vs = k.stride(), v.stride()
+        self._c = _CACHE.pack(k.data_ptr(), v.data_ptr(), table.data_ptr(), ks[0], ks[1], ks[2], vs[0], vs[1], vs[2],
+                              _between(table.stride(0), self.sequences, self.width), self.pages, self.kv_heads, self.page_size, self.head_dim,
+                              self.sequences, self.width, _DTYPES[k.dtype], 0)
+
+
+def _append_args(cache, q, k, v, positions, inv_freq, interleaved, q_weight, k_weight, eps, out):
     T, H, qs = cache._heads("q", q)
     tk, _, ks = cache._heads("k", k, cache.kv_heads)
     tv, _, vs = cache._heads("v", v, cache.kv_heads)
@@ -117,10 +131,19 @@ def specgbv_cache_append(cache: PagedCache, q, k, v, positions, *, inv_freq=None
         if inv_freq.dim() != 1 or inv_freq.dtype is not torch.float64 or inv_freq.device != cache.device or not inv_freq.is_contiguous():
             raise ValueError("inv_freq must be dense float64 [pairs] on the cache's GPU")
         pairs = inv_freq.shape[0]
-    args = _APPEND.pack(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), positions.data_ptr(),
-                        inv_freq.data_ptr() if pairs else 0, q_weight.data_ptr() if q_weight is not None else 0,
-                        k_weight.data_ptr() if k_weight is not None else 0, qs[0], qs[1], qs[2], ks[0], ks[1], ks[2],
-                        vs[0], vs[1], vs[2], os[0], os[1], os[2], ps, eps, T, H, pairs, 1 if interleaved else 0)
+    return out, _APPEND.pack(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), positions.data_ptr(),
+                             inv_freq.data_ptr() if pairs else 0, q_weight.data_ptr() if q_weight is not None else 0,
+                             k_weight.data_ptr() if k_weight is not None else 0, qs[0], qs[1], qs[2], ks[0], ks[1], ks[2],
+                             vs[0], vs[1], vs[2], os[0], os[1], os[2], ps, eps, T, H, pairs, 1 if interleaved else 0)
+
+
+def specgbv_cache_append(cache: PagedCache, q, k, v, positions, *, inv_freq=None, interleaved: bool = False, q_weight=None,
+                         k_weight=None, eps: float = 1e-6, out=None, stream: Optional[int] = None):
+    """Enqueue the append of new tokens: heads of q [S, T, heads, D] and k [S, T, kv_heads, D] are normalised (where q_weight /
+    k_weight [D] are given) and rotated by positions [S, T] * inv_freq (float64, [pairs]; entries behind 2 * pairs stay); k and v
+    go to the cache.  Positions below 0 are padding.  Returns the rotated queries (`out`; q itself may be given)."""
+    lib = load_library()
+    out, args = _append_args(cache, q, k, v, positions, inv_freq, interleaved, q_weight, k_weight, eps, out)
     _check(lib.specgbv_cache_append(cache._c, args, _stream(cache.device, stream)))
     return out
 
@@ -138,6 +161,23 @@ def _attend_args(cache, q, qs, tokens, heads, out_ptr, os, positions_ptr, ps, wi
                         qs[0], qs[1], qs[2], os[0], os[1], os[2], ps, tokens, heads, window, prefixes, max_len or 0, scale or 0.0)
 
 
+def _attend_call(cache, q, positions, window, shared_len, max_len, scale, out):
+    T, H, qs = cache._heads("q", q)
+    ps = cache._positions(positions, T)
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    to, _, os = cache._heads("out", out, H)
+    if to != T:
+        raise ValueError("out must have the shape of q")
+    return out, _attend_args(cache, q, qs, T, H, out.data_ptr(), os, positions.data_ptr(), ps, window, shared_len, max_len, scale)
+
+
+def _attend_workspace(cache, args, workspace, need):
+    if workspace is None:
+        return torch.empty(max(int(need(cache._c, args)), 256), dtype=torch.uint8, device=cache.device)
+    return _scratch(workspace, cache.device)
+
+
 def specgbv_attend_workspace_bytes(cache: PagedCache, q, *, window: int = 0, shared_len=None, max_len: Optional[int] = None) -> int:
     T, H, qs = cache._heads("q", q)
     return int(load_library().specgbv_attend_workspace_bytes(
@@ -152,22 +192,213 @@ def specgbv_attend_paged(cache: PagedCache, q, positions, *, window: int = 0, sh
     share: those are read once per prefix.  max_len: how far sequences reach at most, for the choice of the split.  Returns
     (out [S, T, heads, D], workspace); the workspace serves calls of these shapes with any max_len."""
     lib = load_library()
-    T, H, qs = cache._heads("q", q)
-    ps = cache._positions(positions, T)
-    if out is None:
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    to, _, os = cache._heads("out", out, H)
-    if to != T:
-        raise ValueError("out must have the shape of q")
-    args = _attend_args(cache, q, qs, T, H, out.data_ptr(), os, positions.data_ptr(), ps, window, shared_len, max_len, scale)
-    if workspace is None:
-        need = int(lib.specgbv_attend_workspace_bytes(cache._c, args))
-        workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=cache.device)
-    else:
-        _scratch(workspace, cache.device)
+    out, args = _attend_call(cache, q, positions, window, shared_len, max_len, scale, out)
+    workspace = _attend_workspace(cache, args, workspace, lib.specgbv_attend_workspace_bytes)
     _check(lib.specgbv_attend_paged(cache._c, args, workspace.data_ptr(), workspace.numel() * workspace.element_size(),
                                     _stream(cache.device, stream)))
     return out, workspace
+
+
+class PackedCache(_Cache):
+    """Keys and values in pages, each entry held in 4 bits: k and v uint8 [pages, kv_heads, page_size, head_dim / 2] (the last dimension dense; a page
+    may hold its tokens before its heads) and the powers of two of 32 adjacent entries, k_scale and v_scale uint8 [pages, kv_heads,
+    head_dim / 32, page_size] (the last dimension dense); head_dim is a multiple of 32.  table as in PagedCache.  dtype: that of the queries,
+    keys, values and results of the calls (bfloat16 or float32)."""
+
+    def __init__(self, k, v, k_scale, v_scale, table, dtype=torch.bfloat16):
+        if k.dim() != 4 or k.shape != v.shape:
+            raise ValueError("k and v must be [pages, kv_heads, page_size, head_dim / 2], got %s and %s" % (tuple(k.shape), tuple(v.shape)))
+        for x in (k, v, k_scale, v_scale):
+            if x.dtype is not torch.uint8:
+                raise TypeError("a packed cache is uint8, got %s" % x.dtype)
+        if dtype not in _DTYPES:
+            raise TypeError("queries are float32 or bfloat16, got %s" % dtype)
+        pages, kv_heads, page_size, half = k.shape
+        if half % 16:
+            raise ValueError("head_dim=%d is not a multiple of 32" % (2 * half))
+        blocks = (pages, kv_heads, half // 16, page_size)
+        if k_scale.shape != blocks or v_scale.shape != blocks:
+            raise ValueError("k_scale and v_scale must be %s, got %s and %s" % (blocks, tuple(k_scale.shape), tuple(v_scale.shape)))
+        if table.dim() != 2 or table.dtype != torch.int32:
+            raise ValueError("table must be int32 [sequences, width]")
+        if not k.is_cuda or any(x.device != k.device for x in (v, k_scale, v_scale, table)):
+            raise ValueError("k, v, their scales and table must live on one GPU")
+        if any(x.stride(3) != 1 for x in (k, v, k_scale, v_scale)) or (table.shape[1] > 1 and table.stride(1) != 1):
+            raise ValueError("the last dimension of k, v, their scales and table must be dense")
+        self.k, self.v, self.k_scale, self.v_scale, self.table = k, v, k_scale, v_scale, table
+        self.pages, self.kv_heads, self.page_size, self.head_dim = pages, kv_heads, page_size, 2 * half
+        self.sequences, self.width = table.shape
+        self.dtype, self.device, self._index = dtype, k.device, k.get_device()
+        self._c = _PACKED.pack(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), table.data_ptr(), *k.stride()[:3], *v.stride()[:3],
+                               *k_scale.stride()[:3], *v_scale.stride()[:3], _between(table.stride(0), self.sequences, self.width), pages, kv_heads,
+                               page_size, self.head_dim, self.sequences, self.width, _DTYPES[dtype], 0)
+
+    @classmethod
+    def empty(cls, pages, kv_heads, page_size, head_dim, table, dtype=torch.bfloat16):
+        """A cache of new memory, all of it zero, beside a table."""
+        if head_dim % 32:
+            raise ValueError("head_dim=%d is not a multiple of 32" % head_dim)
+        k, v = (torch.zeros((pages, kv_heads, page_size, head_dim // 2), dtype=torch.uint8, device=table.device) for _ in range(2))
+        ks, vs = (torch.zeros((pages, kv_heads, head_dim // 32, page_size), dtype=torch.uint8, device=table.device) for _ in range(2))
+        return cls(k, v, ks, vs, table, dtype)
+
+
+def specgbv_packed_append(cache: PackedCache, q, k, v, positions, *, inv_freq=None, interleaved: bool = False, q_weight=None,
+                          k_weight=None, eps: float = 1e-6, out=None, stream: Optional[int] = None):
+    """specgbv_cache_append to a cache that holds its entries in 4 bits: keys are normalised and rotated in float64 before they are
+    rounded.  Returns the rotated queries."""
+    lib = load_library()
+    out, args = _append_args(cache, q, k, v, positions, inv_freq, interleaved, q_weight, k_weight, eps, out)
+    _check(_on(cache._index, lib.specgbv_packed_append, cache._c, args, _stream(cache.device, stream)))
+    return out
+
+
+def specgbv_packed_read(cache: PackedCache, positions, *, k=None, v=None, stream: Optional[int] = None):
+    """Enqueue the reading of tokens' keys and values as the cache holds them: (k, v), each [S, T, kv_heads, D] of the cache's dtype, for
+    positions [S, T]; 0 where there is no token (position below 0, behind the table's width, no page)."""
+    lib = load_library()
+    if positions.dim() != 2:
+        raise ValueError("positions must be int32 [sequences, tokens]")
+    T = positions.shape[1]
+    ps = cache._positions(positions, T)
+    shape = (cache.sequences, T, cache.kv_heads, cache.head_dim)
+    strides = []
+    made = []
+    for name, x in (("k", k), ("v", v)):
+        if x is None:
+            x = torch.empty(shape, dtype=cache.dtype, device=positions.device)
+        t, _, s = cache._heads(name, x, cache.kv_heads)
+        if t != T:
+            raise ValueError("%s must have the tokens of positions, %d, got %d" % (name, T, t))
+        made.append(x)
+        strides += s[:3]
+    args = _READ.pack(made[0].data_ptr(), made[1].data_ptr(), positions.data_ptr(), *strides, ps, T, 0)
+    _check(_on(cache._index, lib.specgbv_packed_read, cache._c, args, _stream(cache.device, stream)))
+    return made[0], made[1]
+
+
+def specgbv_packed_attend_workspace_bytes(cache: PackedCache, q, *, window: int = 0, shared_len=None, max_len: Optional[int] = None) -> int:
+    T, H, qs = cache._heads("q", q)
+    args = _attend_args(cache, q, qs, T, H, 0, (0, 0, 0), 0, T, window, shared_len, max_len, None)
+    return int(_on(cache._index, load_library().specgbv_packed_attend_workspace_bytes, cache._c, args))
+
+
+def specgbv_packed_attend(cache: PackedCache, q, positions, *, window: int = 0, shared_len=None, max_len: Optional[int] = None,
+                          scale: Optional[float] = None, out=None, workspace=None, stream: Optional[int] = None):
+    """specgbv_attend_paged over a cache that holds its entries in 4 bits, with the same arguments and results."""
+    lib = load_library()
+    out, args = _attend_call(cache, q, positions, window, shared_len, max_len, scale, out)
+    workspace = _attend_workspace(cache, args, workspace, lambda *a: _on(cache._index, lib.specgbv_packed_attend_workspace_bytes, *a))
+    _check(_on(cache._index, lib.specgbv_packed_attend, cache._c, args, workspace.data_ptr(), workspace.numel() * workspace.element_size(),
+               _stream(cache.device, stream)))
+    return out, workspace
+
+
+class PagePool:
+    """Pages dealt out on the GPU to requests, each a prefix with `drafts` sequences.  table int32 [prefixes * drafts, width] (-1 where a
+    sequence has no page; pass it to a cache); held int32 [prefixes, 2]: how many first pages a request's drafts share, and how many each
+    draft has in all; ring int32 [pages] and ends int32 [2] (head, count): the free pages are ring[(head + i) % pages] for i < count.
+    The tensors stay the caller's.  ``empty`` makes them for a batch without requests."""
+
+    def __init__(self, table, ring, ends, held, *, drafts: int = 1, page_size: int):
+        for name, x, dim in (("table", table, 2), ("ring", ring, 1), ("ends", ends, 1), ("held", held, 2)):
+            if x.dim() != dim or x.dtype is not torch.int32:
+                raise ValueError("%s must be int32 with %d dimensions" % (name, dim))
+        if not table.is_cuda or any(x.device != table.device for x in (ring, ends, held)):
+            raise ValueError("table, ring, ends and held must live on one GPU")
+        if not all(x.is_contiguous() for x in (ring, ends, held)) or (table.shape[1] > 1 and table.stride(1) != 1):
+            raise ValueError("ring, ends and held must be dense, and so must the rows of table")
+        if drafts < 1 or table.shape[0] % drafts:
+            raise ValueError("%d sequences are not prefixes of %d drafts" % (table.shape[0], drafts))
+        if ends.shape[0] != 2 or tuple(held.shape) != (table.shape[0] // drafts, 2):
+            raise ValueError("ends must be [2] and held [%d, 2], got %s and %s" % (table.shape[0] // drafts, tuple(ends.shape), tuple(held.shape)))
+        self.table, self.ring, self.ends, self.held = table, ring, ends, held
+        self.drafts, self.page_size, self.pages, self.prefixes, self.width = drafts, page_size, ring.shape[0], table.shape[0] // drafts, table.shape[1]
+        self.device, self._index = table.device, table.get_device()
+        self._c = _POOL.pack(table.data_ptr(), ring.data_ptr(), ends.data_ptr(), held.data_ptr(), _between(table.stride(0), table.shape[0], self.width),
+                             self.pages, page_size, self.prefixes, drafts, self.width, 0)
+
+    @classmethod
+    def empty(cls, prefixes, width, pages, *, page_size: int, drafts: int = 1, device="cuda"):
+        """A pool of all `pages`, none of them dealt out."""
+        table = torch.full((prefixes * drafts, width), -1, dtype=torch.int32, device=device)
+        ring = torch.arange(pages, dtype=torch.int32, device=device)
+        ends = torch.tensor([0, pages], dtype=torch.int32, device=device)
+        return cls(table, ring, ends, torch.zeros((prefixes, 2), dtype=torch.int32, device=device), drafts=drafts, page_size=page_size)
+
+
+def _numbers(name, x, shape, index, dtype=torch.int32):
+    if tuple(x.shape) != shape or x.dtype is not dtype or x.get_device() != index or not x.is_contiguous():
+        raise ValueError("%s must be dense %s %s on the call's GPU" % (name, dtype, list(shape)))
+    return x
+
+
+def specgbv_pages_workspace_bytes(pool: PagePool) -> int:
+    return int(load_library().specgbv_pages_workspace_bytes(pool._c))
+
+
+def specgbv_pages_advance(pool: PagePool, length, *, chosen=None, room: int = 0, shared_len=None, served=None, workspace=None,
+                          stream: Optional[int] = None):
+    """Enqueue the bringing of every request's pages to its length: length [prefixes] int32 tokens stay (0 and below: the request has ended)
+    and `room` more may be written by the next step; chosen [prefixes] int32 (as the verification returns it): the draft whose pages the
+    prefix's drafts share from here on.  Requests that need more pages than they give back are served in their order while there are enough; one that is
+    not served keeps what it has.  Returns (shared_len [prefixes], tokens in shared pages; served [prefixes]: 1, 0: too few pages, -1:
+    longer than the table; workspace)."""
+    lib = load_library()
+    shape = (pool.prefixes,)
+    _numbers("length", length, shape, pool._index)
+    if chosen is not None:
+        _numbers("chosen", chosen, shape, pool._index)
+    if shared_len is None:
+        shared_len = torch.empty(shape, dtype=torch.int32, device=length.device)
+    if served is None:
+        served = torch.empty(shape, dtype=torch.int32, device=length.device)
+    _numbers("shared_len", shared_len, shape, pool._index)
+    _numbers("served", served, shape, pool._index)
+    if workspace is None:
+        workspace = torch.empty(max(int(lib.specgbv_pages_workspace_bytes(pool._c)), 256), dtype=torch.uint8, device=pool.device)
+    else:
+        _scratch(workspace, pool.device)
+    args = _ADVANCE.pack(length.data_ptr(), chosen.data_ptr() if chosen is not None else 0, shared_len.data_ptr(), served.data_ptr(), room, 0)
+    _check(_on(pool._index, lib.specgbv_pages_advance, pool._c, args, workspace.data_ptr(), workspace.numel() * workspace.element_size(),
+               _stream(pool.device, stream)))
+    return shared_len, served, workspace
+
+
+def specgbv_slot_map(table, start, count, tokens: int, *, page_size: int, pages: int, drafts: int = 1, right: bool = False, flat: bool = True,
+                     positions=None, slots=None, stream: Optional[int] = None):
+    """Enqueue where new tokens lie: each of a prefix's `drafts` sequences has count [prefixes] tokens (int32, at most `tokens`) from position
+    start [prefixes] on.  Returns (positions [S, tokens] int32, -1 where there is no token, slots [S, tokens] int64: page * page_size + slot of the
+    token's place, -1: none; None where `flat` is false).  right: the tokens stand in a row's last places instead of its first ones."""
+    lib = load_library()
+    if table.dim() != 2 or table.dtype is not torch.int32 or not table.is_cuda or (table.shape[1] > 1 and table.stride(1) != 1):
+        raise ValueError("table must be int32 [sequences, width] on the GPU, its rows dense")
+    S, index = table.shape[0], table.get_device()
+    if drafts < 1 or S % drafts:
+        raise ValueError("%d sequences are not prefixes of %d drafts" % (S, drafts))
+    if tokens < 0:
+        raise ValueError("tokens must be >= 0, got %d" % tokens)
+    _numbers("start", start, (S // drafts,), index)
+    _numbers("count", count, (S // drafts,), index)
+    if positions is None:
+        positions = torch.empty((S, tokens), dtype=torch.int32, device=table.device)
+    if flat and slots is None:
+        slots = torch.empty((S, tokens), dtype=torch.int64, device=table.device)
+    elif not flat:
+        slots = None
+    between = []
+    for name, x, dtype in (("positions", positions, torch.int32), ("slots", slots, torch.int64)):
+        if x is None:
+            between.append(tokens)
+            continue
+        if tuple(x.shape) != (S, tokens) or x.dtype is not dtype or x.get_device() != index or (tokens > 1 and x.stride(1) != 1):
+            raise ValueError("%s must be %s [%d, %d] on the table's GPU, its rows dense" % (name, dtype, S, tokens))
+        between.append(_between(x.stride(0), S, tokens))
+    args = _SLOTS.pack(table.data_ptr(), start.data_ptr(), count.data_ptr(), positions.data_ptr(), slots.data_ptr() if slots is not None else 0,
+                       _between(table.stride(0), S, table.shape[1]), between[0], between[1], S, drafts, table.shape[1], page_size, pages, tokens,
+                       1 if right else 0, 0)
+    _check(_on(index, lib.specgbv_slot_map, args, _stream(table.device, stream)))
+    return positions, slots
 
 
 def specgbv_filter_workspace_bytes(rows: int, V: int, dtype: int) -> int:
