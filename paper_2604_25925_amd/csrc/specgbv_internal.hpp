@@ -229,26 +229,31 @@ struct PackedAppendProblem {
     const int32_t *positions;
     const double *inv_freq;
     PageMap map;
-    Divider by_tokens, by_heads;   // tokens of a sequence; heads of q, k and v together
+    Divider by_tokens, by_slices;  // tokens of a sequence; waves of a token (set by the launch)
     int64_t q_stride[3], k_stride[3], v_stride[3], q_out_stride[3];
     int64_t k_cache_stride[3], v_cache_stride[3], k_scale_stride[3], v_scale_stride[3];      // page, head, slot; of the scales page, head, block
     int64_t positions_stride;
+    int32_t q_head, k_head, v_head, q_out_head, k_cache_head, v_cache_head, k_scale_head, v_scale_head, k_scale_block, v_scale_block;      // strides of heads and blocks
     double eps;
+    float inv_dim;
     int tokens_all, heads, kv_heads, head_dim, pairs, interleaved;
-    int lane_bits, block_tokens;   // set by launch_packed_append
+    int lane_bits, q_passes, k_passes, first_pass, passes, slice;   // set by launch_packed_append; slice: a wave's passes
 };
 // wide: strides and addresses allow 16-byte loads, and a vector's partners in the rotation are a vector.
 hipError_t launch_packed_append(const PackedAppendProblem &p, int dtype, bool wide, hipStream_t stream);
+// Whether that launch takes keys and values alone, and launch_append the queries.
+bool packed_append_apart(int tokens_all);
 
 struct PackedReadProblem {
     const uint8_t *k_cache, *v_cache, *k_scale, *v_scale;
     void *k, *v;
     const int32_t *positions;
     PageMap map;
-    Divider by_tokens, by_heads;   // tokens of a sequence; kv heads, twice
+    Divider by_tokens, by_slices;
     int64_t k_cache_stride[3], v_cache_stride[3], k_scale_stride[3], v_scale_stride[3], k_stride[3], v_stride[3], positions_stride;
+    int32_t k_head, v_head, k_cache_head, v_cache_head, k_scale_head, v_scale_head, k_scale_block, v_scale_block;
     int tokens_all, kv_heads, head_dim;
-    int lane_bits;                 // set by launch_packed_read
+    int lane_bits, k_passes, slice;    // set by launch_packed_read
 };
 hipError_t launch_packed_read(const PackedReadProblem &p, int dtype, bool wide, hipStream_t stream);
 

@@ -6,19 +6,18 @@
 // half step of 1 that entries between 4 and 6 are off by; a power more for all the others would cost each of them a bit.)  A block that holds
 // what is not finite has the byte 255, and all of it is no number.
 //
-// Keys are normalised and rotated in float64 and only what decides the code is kept of it: a float32 cut off behind its last bit, with that
-// bit set where anything was cut (no border lies there, so the conversion, which rounds once, decides as it would for the float64).  So a code
-// differs from the definition's only where the float64 lies within its own error of a border, 2^-50 of the entry instead of 2^-20.
+// Keys are normalised and rotated in float64, and what decides the code is kept of it: a float32 cut off behind its last bit, with that bit set
+// where anything was cut (no border lies there, so the conversion, which rounds once, decides as it would for the float64).  So a code differs from the
+// definition's only where the float64 lies within its own error of a border, 2^-50 of the entry instead of 2^-20.
 //
 // A lane has 8 adjacent entries, which are one word of the cache, and four lanes a block; the entry that another one turns with is read a second
-// time (from the cache) instead of exchanged.  Every entry is read from memory once, so memory bounds it.
+// time (from the cache) instead of exchanged.  Every entry is read from memory once.
 #include "specgbv_internal.hpp"
 
 namespace specgbv {
 namespace {
 
-constexpr int kThreads = 256;
-constexpr int kTokens = 2;                    // tokens of a workgroup at most
+constexpr int kThreads = 256, kWaves = kThreads / 64;
 constexpr int kMaxPairs = 128;
 constexpr int kLane = 8;                      // entries of a lane
 
@@ -30,19 +29,33 @@ template <> __device__ __forceinline__ uint16_t narrow<uint16_t>(float x) { retu
 
 template <typename T> struct alignas(16) Vec { T e[16 / sizeof(T)]; };
 
-template <typename T, bool WIDE> __device__ __forceinline__ void load8(const T *src, float (&x)[kLane])
+// Eight adjacent entries as they come from memory: words of two (bfloat16) or one.
+template <typename T> struct Entries {
+    static constexpr int kWords = kLane * sizeof(T) / 4;
+    uint32_t w[kWords];
+    __device__ __forceinline__ float operator[](int j) const
+    {
+        if constexpr (sizeof(T) == 4) return __uint_as_float(w[j]);
+        else return __uint_as_float(j % 2 ? w[j / 2] & 0xFFFF0000u : w[j / 2] << 16);
+    }
+    __device__ __forceinline__ void put(int j, T x)
+    {
+        if constexpr (sizeof(T) == 4) w[j] = __float_as_uint(x);
+        else w[j / 2] = j % 2 ? (w[j / 2] & 0xFFFFu) | static_cast<uint32_t>(x) << 16 : x;
+    }
+};
+
+template <typename T, bool WIDE> __device__ __forceinline__ void load8(const T *src, Entries<T> &x)
 {
-    constexpr int W = 16 / sizeof(T);
     if constexpr (WIDE) {
 #pragma unroll
-        for (int i = 0; i < kLane / W; ++i) {
-            const Vec<T> v = reinterpret_cast<const Vec<T> *>(src)[i];
-#pragma unroll
-            for (int j = 0; j < W; ++j) x[i * W + j] = widen(v.e[j]);
+        for (int i = 0; i < Entries<T>::kWords / 4; ++i) {
+            const U4 v = reinterpret_cast<const U4 *>(src)[i];
+            x.w[4 * i] = v.x; x.w[4 * i + 1] = v.y; x.w[4 * i + 2] = v.z; x.w[4 * i + 3] = v.w;
         }
     } else
 #pragma unroll
-        for (int j = 0; j < kLane; ++j) x[j] = widen(src[j]);
+        for (int j = 0; j < kLane; ++j) x.put(j, src[j]);
 }
 
 template <typename T, bool WIDE> __device__ __forceinline__ void store8(T *dst, const float (&x)[kLane])
@@ -61,206 +74,279 @@ template <typename T, bool WIDE> __device__ __forceinline__ void store8(T *dst, 
         for (int j = 0; j < kLane; ++j) dst[j] = narrow<T>(x[j]);
 }
 
-// A lane's entries of a head, normalised and rotated, in F (float or double).  x: its entries, b: those they turn with.
-template <typename T, bool WIDE, typename F>
-__device__ __forceinline__ void turned(const PackedAppendProblem &p, const T *src, const T *weight, const double2 *turn, int e0, bool there, int lanes, F (&y)[kLane])
+// The entries that a lane's entries e0.. of a head turn with; 0 for those that do not turn.  (WIDE: pairs are whole vectors, or lie in one.)
+template <typename T, bool WIDE> __device__ __forceinline__ void load_partners(const T *head, int e0, int pairs, int interleaved, Entries<T> &b)
 {
-    float x[kLane], b[kLane], w[kLane], wb[kLane];
-    const bool turning = there && e0 < 2 * p.pairs;
-    const bool split = turning && !p.interleaved;
-#pragma unroll
-    for (int j = 0; j < kLane; ++j) { x[j] = b[j] = 0.0f; w[j] = wb[j] = 1.0f; }
-    int other[WIDE ? 1 : kLane];                              // where the entries that turn with these begin, or each of them
-    if constexpr (WIDE) other[0] = e0 < p.pairs ? e0 + p.pairs : e0 - p.pairs;
+    if (WIDE && !interleaved) load8<T, true>(head + (e0 < pairs ? e0 + pairs : e0 - pairs), b);
     else
 #pragma unroll
-        for (int j = 0; j < kLane; ++j) other[j] = e0 + j >= 2 * p.pairs ? e0 + j : (e0 + j < p.pairs ? e0 + j + p.pairs : e0 + j - p.pairs);
-    if (there) load8<T, WIDE>(src + e0, x);
-    if (split) {
-        if constexpr (WIDE) load8<T, true>(src + other[0], b);
-        else
-#pragma unroll
-            for (int j = 0; j < kLane; ++j) b[j] = widen(src[other[j]]);
-    }
-    F inv = 1;
-    if (weight) {                                             // the same for the head's lanes
-        if (there) load8<T, WIDE>(weight + e0, w);
-        if (split) {
-            if constexpr (WIDE) load8<T, true>(weight + other[0], wb);
-            else
-#pragma unroll
-                for (int j = 0; j < kLane; ++j) wb[j] = widen(weight[other[j]]);
+        for (int j = 0; j < kLane; ++j) {
+            const int e = e0 + j;
+            if (e < 2 * pairs) b.put(j, head[interleaved ? e ^ 1 : (e < pairs ? e + pairs : e - pairs)]);
         }
-        F sum = 0;
+}
+
+// The pair that entry e belongs to, where it turns; and whether it is the pair's first.
+__device__ __forceinline__ int pair_of(const PackedAppendProblem &p, int e) { return p.interleaved ? e >> 1 : (e < p.pairs ? e : e - p.pairs); }
+__device__ __forceinline__ bool first_of_pair(const PackedAppendProblem &p, int e) { return p.interleaved ? e % 2 == 0 : e < p.pairs; }
+
+// A lane's entries x of a key's head, normalised and rotated in float64; b: those they turn with (0 where they do not turn).
+template <typename T, bool WIDE>
+__device__ __forceinline__ void turned(const PackedAppendProblem &p, const Entries<T> &x, const Entries<T> &b, const double2 *turn, int e0, bool there, int lanes, double (&y)[kLane])
+{
+    const T *weight = static_cast<const T *>(p.k_weight);
+    const bool turning = there && e0 < 2 * p.pairs;
+    double o[kLane];
 #pragma unroll
-        for (int j = 0; j < kLane; ++j) sum += static_cast<F>(x[j]) * static_cast<F>(x[j]);
+    for (int j = 0; j < kLane; ++j) { y[j] = x[j]; o[j] = b[j]; }
+    if (weight) {                                             // the same for the head's lanes
+        Entries<T> w{}, wb{};
+        if (there) load8<T, WIDE>(weight + e0, w);
+        if (turning) load_partners<T, WIDE>(weight, e0, p.pairs, p.interleaved, wb);
+        double sum = 0;
+#pragma unroll
+        for (int j = 0; j < kLane; ++j) sum += y[j] * y[j];
         for (int m = lanes >> 1; m > 0; m >>= 1) sum += __shfl_xor(sum, m, 64);
-        if constexpr (sizeof(F) == 8) inv = 1.0 / sqrt(sum / p.head_dim + p.eps);
-        else inv = 1.0f / sqrtf(sum / static_cast<float>(p.head_dim) + static_cast<float>(p.eps));
+        const double inv = 1.0 / sqrt(sum / p.head_dim + p.eps);
+#pragma unroll
+        for (int j = 0; j < kLane; ++j) {
+            y[j] *= inv * static_cast<double>(w[j]);
+            o[j] *= inv * static_cast<double>(wb[j]);
+        }
     }
-#pragma unroll
-    for (int j = 0; j < kLane; ++j) y[j] = weight ? static_cast<F>(x[j]) * inv * static_cast<F>(w[j]) : static_cast<F>(x[j]);
     if (!turning) return;
-    if (p.interleaved) {
+    if (WIDE && !p.interleaved) {                             // all of a lane's entries are first ones, or none
+        const double2 *mine = turn + (e0 < p.pairs ? e0 : e0 - p.pairs);
+        const double sign = e0 < p.pairs ? -1.0 : 1.0;
 #pragma unroll
-        for (int j = 0; j < kLane; j += 2)
-            if (e0 + j < 2 * p.pairs) {
-                const double2 cs = turn[(e0 + j) / 2];
-                const F a = y[j], c = y[j + 1];
-                y[j] = a * static_cast<F>(cs.x) - c * static_cast<F>(cs.y);
-                y[j + 1] = c * static_cast<F>(cs.x) + a * static_cast<F>(cs.y);
-            }
+        for (int j = 0; j < kLane; ++j) y[j] = y[j] * mine[j].x + o[j] * (mine[j].y * sign);
         return;
     }
 #pragma unroll
-    for (int j = 0; j < kLane; ++j) {
-        const int e = e0 + j;
-        if (!WIDE && e >= 2 * p.pairs) continue;
-        const bool lower = e < p.pairs;
-        const double2 cs = turn[lower ? e : e - p.pairs];
-        const F o = weight ? static_cast<F>(b[j]) * inv * static_cast<F>(wb[j]) : static_cast<F>(b[j]);
-        const F side = o * static_cast<F>(cs.y);
-        y[j] = lower ? y[j] * static_cast<F>(cs.x) - side : y[j] * static_cast<F>(cs.x) + side;
-    }
+    for (int j = 0; j < kLane; ++j)
+        if (e0 + j < 2 * p.pairs) {
+            const double2 cs = turn[pair_of(p, e0 + j)];
+            y[j] = y[j] * cs.x + o[j] * (first_of_pair(p, e0 + j) ? -cs.y : cs.y);
+        }
 }
 
-// A float32 that lies on the same side of every border between codes as x.
-__device__ __forceinline__ float decisive(double x)
+// A float64's bits as those of a float32 that lies on the same side of every border between codes: cut off, with the last bit set where anything was cut.
+// Beyond float32's range it is the largest or a smallest one, whose codes are the same; what is not finite is looked at elsewhere.
+__device__ __forceinline__ uint32_t decisive(double x)
 {
-    const float r = static_cast<float>(x);
-    const double back = r;
-    uint32_t bits = __float_as_uint(r);
-    if (back != x) bits = (fabs(back) > fabs(x) ? bits - 1 : bits) | 1u;
-    return __uint_as_float(bits);
+    const uint64_t bits = static_cast<uint64_t>(__double_as_longlong(x));
+    const uint32_t hi = static_cast<uint32_t>(bits >> 32), size = hi & 0x7FFFFFFFu;
+    const uint32_t in_range = min(max(size, 0x38000000u), 0x47EFFFFFu);                  // 2^-127 and the last below 2^128
+    return (in_range - 0x38000000u) << 3 | min(static_cast<uint32_t>(bits), 1u) | (hi & 0x80000000u);
 }
 
-// The word of a lane's 8 entries; `byte`: its block's power of two (four lanes have a block).
-__device__ __forceinline__ uint32_t packed(const double (&y)[kLane], uint32_t &byte)
+// The word of a lane's 8 entries, given by a float32's bits each; `odd`: the lane has one that is not finite.  `byte`: its block's power of two (four lanes have a block).
+__device__ __forceinline__ uint32_t packed(const uint32_t (&y)[kLane], bool odd, uint32_t &byte)
 {
-    double most = 0.0;
+    uint32_t most = odd ? 0x7FFFFFFFu : 0u;                            // as bits: in order
 #pragma unroll
-    for (int j = 0; j < kLane; ++j) most = fabs(y[j]) < INFINITY ? fmax(most, fabs(y[j])) : INFINITY;
-    most = fmax(most, __shfl_xor(most, 1, 64));
-    most = fmax(most, __shfl_xor(most, 2, 64));
-    const uint64_t bits = static_cast<uint64_t>(__double_as_longlong(most));
-    int e = static_cast<int>(bits >> 52) - 1023 - 2 + ((bits & 0xFFFFFFFFFFFFFull) > 0xC000000000000ull ? 1 : 0);      // 1.75 2^n = 7 2^(n - 2)
-    e = max(-120, min(e, 125));
+    for (int j = 0; j < kLane; ++j) most = max(most, y[j] & 0x7FFFFFFFu);
+    most = max(most, static_cast<uint32_t>(__shfl_xor(static_cast<int>(most), 1, 64)));
+    most = max(most, static_cast<uint32_t>(__shfl_xor(static_cast<int>(most), 2, 64)));
+    // the least e with most <= 7 2^e = 7/4 2^(e + 2)
+    const int e = max(-120, min(static_cast<int>(most >> 23) - 127 - 2 + ((most & 0x7FFFFFu) > 0x600000u ? 1 : 0), 125));
     byte = static_cast<uint32_t>(e + 127);
-    const double up = __longlong_as_double(static_cast<long long>(1023 - e) << 52);
+    const float power = __uint_as_float(byte << 23);
     uint32_t word = 0;
-    const float one = 1.0f;
-    word = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(word, decisive(y[0] * up), decisive(y[1] * up), one, 0);
-    word = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(word, decisive(y[2] * up), decisive(y[3] * up), one, 1);
-    word = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(word, decisive(y[4] * up), decisive(y[5] * up), one, 2);
-    word = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(word, decisive(y[6] * up), decisive(y[7] * up), one, 3);
-    if (most == INFINITY) { byte = 255u; word = 0u; }
+    word = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(word, __uint_as_float(y[0]), __uint_as_float(y[1]), power, 0);
+    word = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(word, __uint_as_float(y[2]), __uint_as_float(y[3]), power, 1);
+    word = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(word, __uint_as_float(y[4]), __uint_as_float(y[5]), power, 2);
+    word = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(word, __uint_as_float(y[6]), __uint_as_float(y[7]), power, 3);
+    if (most >= 0x7F800000u) { byte = 255u; word = 0u; }
     return word;
 }
 
-template <typename T, bool WIDE>
-__global__ void __launch_bounds__(kThreads) k_packed_append(PackedAppendProblem p)
+// What does not change in a kernel, by scalar loads.
+typedef const int32_t __attribute__((address_space(4))) *ConstInts;
+__device__ __forceinline__ int scalar_at(const int32_t *p, int64_t i) { return reinterpret_cast<ConstInts>(reinterpret_cast<uintptr_t>(p))[i]; }
+
+// A token of a wave: its sequence, its place among the sequence's tokens and its position; all scalar.
+struct Token { int s, t, pos; };
+__device__ __forceinline__ Token token_of(const Divider &by_tokens, const int32_t *positions, int64_t stride, int n)
 {
-    __shared__ double2 sh_turn[kTokens][kMaxPairs];
-    __shared__ int sh_pos[kTokens], sh_page[kTokens], sh_slot[kTokens];
-    const int tid = threadIdx.x;
-    const int heads_all = p.heads + 2 * p.kv_heads;
-    const int n0 = blockIdx.x * p.block_tokens;
-    const int nt = min(p.block_tokens, p.tokens_all - n0);
+    const int s = by_tokens.div(n), t = by_tokens.mod(n, s);
+    return {s, t, scalar_at(positions, s * stride + t)};
+}
+__device__ __forceinline__ Place scalar_place(const PageMap &m, int sequence, int pos)
+{
+    const int n = m.page.div(pos);
+    if (pos < 0 || n >= m.width) return {-1, 0};
+    const int page = scalar_at(m.table, sequence * m.table_stride + n);
+    return {static_cast<uint32_t>(page) < static_cast<uint32_t>(m.pages) ? page : -1, m.page.mod(pos, n)};
+}
 
-    if (tid < nt) {
-        const int s = p.by_tokens.div(n0 + tid), t = p.by_tokens.mod(n0 + tid, s);
-        const int pos = p.positions[s * p.positions_stride + t];
-        Place at{-1, 0};
-        if (pos >= 0) at = place_of(p.map, s, pos);
-        sh_pos[tid] = pos; sh_page[tid] = at.page; sh_slot[tid] = at.slot;
-    }
-    for (int i = tid; i < nt * p.pairs; i += kThreads) {
-        const int k = i / p.pairs, r = i - k * p.pairs;
-        const int s = p.by_tokens.div(n0 + k), t = p.by_tokens.mod(n0 + k, s);
-        // a turn in float64: whole turns are taken off before the sine and cosine
-        const double turns = static_cast<double>(p.positions[s * p.positions_stride + t]) * p.inv_freq[r] * 0.15915494309189533577;
-        double sn, cs;
-        sincospi(2.0 * (turns - rint(turns)), &sn, &cs);
-        sh_turn[k][r] = make_double2(cs, sn);
-    }
-    __syncthreads();
+// A wave has one token, and of its heads' passes (as many heads at once as 64 lanes hold; of q, then k, then v) a slice, so that all that belongs to the
+// token is scalar arithmetic; no barrier stands anywhere.
+template <typename T, bool WIDE>
+__global__ void __launch_bounds__(kThreads, WIDE ? (sizeof(T) == 2 ? 5 : 4) : 3) k_packed_append(PackedAppendProblem p)
+{
+    __shared__ double2 sh_turn[kWaves][kMaxPairs];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int at_all = static_cast<int>(blockIdx.x) * kWaves + wave;
+    const int n = p.by_slices.div(at_all), slice = p.by_slices.mod(at_all, n);
+    if (n >= p.tokens_all) return;
+    const int first = p.first_pass + slice * p.slice, last = min(p.passes, first + p.slice);
+    const int k_pass = p.q_passes, v_pass = p.q_passes + p.k_passes;
+    const Token tk = token_of(p.by_tokens, p.positions, p.positions_stride, n);
+    const int lanes = 1 << p.lane_bits, u = lane & (lanes - 1), e0 = u * kLane, head = lane >> p.lane_bits, heads = 64 >> p.lane_bits;
+    const bool mine = e0 < p.head_dim;
 
-    const int lanes = 1 << p.lane_bits, u = tid & (lanes - 1), e0 = u * kLane;
-    const int slots = kThreads >> p.lane_bits;
-    const int todo = nt * heads_all;
-    for (int base = 0; base < todo; base += slots) {                   // uniform
-        const int item = base + (tid >> p.lane_bits);
-        if (item >= todo) continue;                                    // whole groups of lanes
-        const int k = p.by_heads.div(item), h = p.by_heads.mod(item, k);
-        const int s = p.by_tokens.div(n0 + k), t = p.by_tokens.mod(n0 + k, s);
-        const bool mine = e0 < p.head_dim;
-        if (h < p.heads) {
-            const bool there = mine && sh_pos[k] >= 0;
-            float y[kLane];
-            turned<T, WIDE, float>(p, static_cast<const T *>(p.q) + s * p.q_stride[0] + t * p.q_stride[1] + h * p.q_stride[2],
-                                   static_cast<const T *>(p.q_weight), sh_turn[k], e0, there, lanes, y);
-            if (!there)
+    Place at{-1, 0};
+    if (last > k_pass && tk.pos >= 0) at = scalar_place(p.map, tk.s, tk.pos);
+    const int64_t page = at.page, slot = at.slot;
+
+    auto load = [&](const T *src, bool there, Entries<T> &x, Entries<T> &b) {
+        x = b = Entries<T>{};
+        if (!there) return;
+        load8<T, WIDE>(src + e0, x);
+        if (e0 < 2 * p.pairs) load_partners<T, WIDE>(src, e0, p.pairs, p.interleaved, b);
+    };
+    auto store = [&](uint8_t *data, int32_t data_head, uint8_t *scale, int32_t scale_head, int32_t scale_block, int hd, uint32_t word, uint32_t byte) {
+        *reinterpret_cast<uint32_t *>(data + (static_cast<int64_t>(hd) * data_head + e0 / 2)) = word;
+        if (u % 4 == 0) scale[static_cast<int64_t>(hd) * scale_head + static_cast<int64_t>(u / 4) * scale_block] = static_cast<uint8_t>(byte);
+    };
+
+    // ---- values: as they are
+    if (at.page >= 0) {
+        const T *base = static_cast<const T *>(p.v) + (tk.s * p.v_stride[0] + tk.t * p.v_stride[1]);
+        uint8_t *data = p.v_cache + (page * p.v_cache_stride[0] + slot * p.v_cache_stride[2]), *scale = p.v_scale + (page * p.v_scale_stride[0] + slot);
+#pragma unroll 2
+        for (int pass = max(first, v_pass); pass < last; ++pass) {
+            const int hd = (pass - v_pass) * heads + head;
+            const bool there = mine && hd < p.kv_heads;
+            Entries<T> x{};
+            if (there) load8<T, WIDE>(base + static_cast<int64_t>(hd) * p.v_head + e0, x);
+            uint32_t bits[kLane], byte;
 #pragma unroll
-                for (int j = 0; j < kLane; ++j) y[j] = 0.0f;
-            if (mine) store8<T, WIDE>(static_cast<T *>(p.q_out) + s * p.q_out_stride[0] + t * p.q_out_stride[1] + h * p.q_out_stride[2] + e0, y);
-            continue;
+            for (int j = 0; j < kLane; ++j) bits[j] = __float_as_uint(x[j]);
+            const uint32_t word = packed(bits, false, byte);
+            if (there) store(data, p.v_cache_head, scale, p.v_scale_head, p.v_scale_block, hd, word, byte);
         }
-        if (sh_pos[k] < 0 || sh_page[k] < 0) continue;                 // the same for the token's lanes
-        const bool value = h >= p.heads + p.kv_heads;
-        const int hd = value ? h - p.heads - p.kv_heads : h - p.heads;
-        double y[kLane];
-        if (value) {
-            float x[kLane];
+    }
+    if (first >= v_pass) return;
+
+    // ---- what q and k turn by
+    if (tk.pos >= 0)
+        for (int i = lane; i < p.pairs; i += 64) {
+            // a turn in float64: whole turns are taken off before the sine and cosine
+            const double turns = static_cast<double>(tk.pos) * p.inv_freq[i] * 0.15915494309189533577;
+            double sn, cs;
+            sincospi(2.0 * (turns - rint(turns)), &sn, &cs);
+            sh_turn[wave][i] = make_double2(cs, sn);
+        }
+    __builtin_amdgcn_wave_barrier();                                   // (a wave's accesses to LDS are done in their order)
+
+    if (at.page >= 0) {
+        const T *base = static_cast<const T *>(p.k) + (tk.s * p.k_stride[0] + tk.t * p.k_stride[1]);
+        uint8_t *data = p.k_cache + (page * p.k_cache_stride[0] + slot * p.k_cache_stride[2]), *scale = p.k_scale + (page * p.k_scale_stride[0] + slot);
+#pragma unroll 1
+        for (int pass = max(first, k_pass); pass < min(last, v_pass); ++pass) {
+            const int hd = (pass - k_pass) * heads + head;
+            const bool there = mine && hd < p.kv_heads;
+            Entries<T> x, b;
+            load(base + static_cast<int64_t>(hd) * p.k_head, there, x, b);
+            double y[kLane];
+            turned<T, WIDE>(p, x, b, sh_turn[wave], e0, there, lanes, y);
+            uint32_t bits[kLane], byte, top = 0;
 #pragma unroll
-            for (int j = 0; j < kLane; ++j) x[j] = 0.0f;
-            if (mine) load8<T, WIDE>(static_cast<const T *>(p.v) + s * p.v_stride[0] + t * p.v_stride[1] + hd * p.v_stride[2] + e0, x);
+            for (int j = 0; j < kLane; ++j) {
+                bits[j] = decisive(y[j]);
+                top = max(top, static_cast<uint32_t>(__double2hiint(y[j])) & 0x7FFFFFFFu);
+            }
+            const uint32_t word = packed(bits, top >= 0x7FF00000u, byte);
+            if (there) store(data, p.k_cache_head, scale, p.k_scale_head, p.k_scale_block, hd, word, byte);
+        }
+    }
+
+    // ---- queries, in float32: what a lane's entries are multiplied by is the same for all heads
+    if (first >= min(last, k_pass)) return;
+    const T *base = static_cast<const T *>(p.q) + (tk.s * p.q_stride[0] + tk.t * p.q_stride[1]), *weight = static_cast<const T *>(p.q_weight);
+    T *out = static_cast<T *>(p.q_out) + (tk.s * p.q_out_stride[0] + tk.t * p.q_out_stride[1]);
+    float cs[kLane], sn[kLane];
+    Entries<T> w{}, wb{};
+    if (weight && mine) {
+        load8<T, WIDE>(weight + e0, w);
+        if (e0 < 2 * p.pairs) load_partners<T, WIDE>(weight, e0, p.pairs, p.interleaved, wb);
+    }
 #pragma unroll
-            for (int j = 0; j < kLane; ++j) y[j] = x[j];
+    for (int j = 0; j < kLane; ++j) {
+        cs[j] = 1.0f; sn[j] = 0.0f;
+        if (e0 + j < 2 * p.pairs) {
+            const double2 t = sh_turn[wave][pair_of(p, e0 + j)];
+            cs[j] = static_cast<float>(t.x);
+            sn[j] = static_cast<float>(first_of_pair(p, e0 + j) ? -t.y : t.y);
+        }
+    }
+#pragma unroll 2
+    for (int pass = first; pass < min(last, k_pass); ++pass) {
+        const int hd = pass * heads + head;
+        const bool there = mine && hd < p.heads && tk.pos >= 0;
+        Entries<T> x, b;
+        load(base + static_cast<int64_t>(hd) * p.q_head, there, x, b);
+        float y[kLane];
+        if (weight) {
+            float sum = 0.0f;
+#pragma unroll
+            for (int j = 0; j < kLane; ++j) sum = fmaf(x[j], x[j], sum);
+            for (int m = lanes >> 1; m > 0; m >>= 1) sum += __shfl_xor(sum, m, 64);
+            const float inv = 1.0f / sqrtf(sum * p.inv_dim + static_cast<float>(p.eps));
+#pragma unroll
+            for (int j = 0; j < kLane; ++j) y[j] = x[j] * inv * w[j] * cs[j] + b[j] * inv * wb[j] * sn[j];
         } else
-            turned<T, WIDE, double>(p, static_cast<const T *>(p.k) + s * p.k_stride[0] + t * p.k_stride[1] + hd * p.k_stride[2],
-                                    static_cast<const T *>(p.k_weight), sh_turn[k], e0, mine, lanes, y);
-        uint32_t byte;
-        const uint32_t word = packed(y, byte);
-        if (!mine) continue;
-        const int64_t page = sh_page[k], slot = sh_slot[k];
-        const int64_t *cs = value ? p.v_cache_stride : p.k_cache_stride, *ss = value ? p.v_scale_stride : p.k_scale_stride;
-        *reinterpret_cast<uint32_t *>((value ? p.v_cache : p.k_cache) + page * cs[0] + hd * cs[1] + slot * cs[2] + e0 / 2) = word;
-        if (u % 4 == 0) (value ? p.v_scale : p.k_scale)[page * ss[0] + hd * ss[1] + u / 4 * ss[2] + slot] = static_cast<uint8_t>(byte);
+#pragma unroll
+            for (int j = 0; j < kLane; ++j) y[j] = x[j] * cs[j] + b[j] * sn[j];
+        if (!there)
+#pragma unroll
+            for (int j = 0; j < kLane; ++j) y[j] = 0.0f;
+        if (mine && hd < p.heads) store8<T, WIDE>(out + static_cast<int64_t>(hd) * p.q_out_head + e0, y);
     }
 }
 
+// A wave has a token and a slice of its passes, of k and then of v, as above.
 template <typename T, bool WIDE>
 __global__ void __launch_bounds__(kThreads) k_packed_read(PackedReadProblem p)
 {
-    const int lanes = 1 << p.lane_bits, u = threadIdx.x & (lanes - 1), e0 = u * kLane;
-    const int64_t all = static_cast<int64_t>(blockIdx.x) * (kThreads >> p.lane_bits) + (threadIdx.x >> p.lane_bits);
-    if (all >= static_cast<int64_t>(p.tokens_all) * 2 * p.kv_heads || e0 >= p.head_dim) return;
-    const int item = static_cast<int>(all);                            // (fewer than 2^31)
-    const int n = p.by_heads.div(item), h = p.by_heads.mod(item, n);
-    const int s = p.by_tokens.div(n), t = p.by_tokens.mod(n, s);
-    const int pos = p.positions[s * p.positions_stride + t];
-    Place at{-1, 0};
-    if (pos >= 0) at = place_of(p.map, s, pos);
-    const bool value = h >= p.kv_heads;
-    const int hd = value ? h - p.kv_heads : h;
-    float x[kLane];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int at_all = static_cast<int>(blockIdx.x) * kWaves + wave;
+    const int n = p.by_slices.div(at_all), slice = p.by_slices.mod(at_all, n);
+    if (n >= p.tokens_all) return;
+    const int first = slice * p.slice, last = min(2 * p.k_passes, first + p.slice);
+    const Token tk = token_of(p.by_tokens, p.positions, p.positions_stride, n);
+    const Place at = scalar_place(p.map, tk.s, tk.pos);
+    const int lanes = 1 << p.lane_bits, u = lane & (lanes - 1), e0 = u * kLane, heads = 64 >> p.lane_bits;
+    if (e0 >= p.head_dim) return;
+    const int64_t page = at.page, slot = at.slot;
+    const uint8_t *data[2] = {p.k_cache + (page * p.k_cache_stride[0] + slot * p.k_cache_stride[2]), p.v_cache + (page * p.v_cache_stride[0] + slot * p.v_cache_stride[2])};
+    const uint8_t *scale[2] = {p.k_scale + (page * p.k_scale_stride[0] + slot), p.v_scale + (page * p.v_scale_stride[0] + slot)};
+    T *out[2] = {static_cast<T *>(p.k) + (tk.s * p.k_stride[0] + tk.t * p.k_stride[1]), static_cast<T *>(p.v) + (tk.s * p.v_stride[0] + tk.t * p.v_stride[1])};
+#pragma unroll 4
+    for (int pass = first; pass < last; ++pass) {
+        const bool value = pass >= p.k_passes;
+        const int hd = (value ? pass - p.k_passes : pass) * heads + (lane >> p.lane_bits);
+        if (hd >= p.kv_heads) continue;
+        const int64_t h = hd;
+        float x[kLane];
 #pragma unroll
-    for (int j = 0; j < kLane; ++j) x[j] = 0.0f;
-    if (at.page >= 0) {
-        const int64_t *cs = value ? p.v_cache_stride : p.k_cache_stride, *ss = value ? p.v_scale_stride : p.k_scale_stride;
-        const uint32_t word = *reinterpret_cast<const uint32_t *>((value ? p.v_cache : p.k_cache) + at.page * cs[0] + hd * cs[1] + at.slot * cs[2] + e0 / 2);
-        const float power = __uint_as_float(static_cast<uint32_t>((value ? p.v_scale : p.k_scale)[at.page * ss[0] + hd * ss[1] + u / 4 * ss[2] + at.slot]) << 23);
-        uint32_t two[4];
-        two[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word, power, 0));
-        two[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word, power, 1));
-        two[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word, power, 2));
-        two[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word, power, 3));
+        for (int j = 0; j < kLane; ++j) x[j] = 0.0f;
+        if (at.page >= 0) {
+            const uint32_t word = *reinterpret_cast<const uint32_t *>(data[value] + (h * (value ? p.v_cache_head : p.k_cache_head) + e0 / 2));
+            const uint32_t byte = scale[value][h * (value ? p.v_scale_head : p.k_scale_head) + static_cast<int64_t>(u / 4) * (value ? p.v_scale_block : p.k_scale_block)];
+            const float power = __uint_as_float(byte << 23);
+            uint32_t two[4];
+            two[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word, power, 0));
+            two[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word, power, 1));
+            two[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word, power, 2));
+            two[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word, power, 3));
 #pragma unroll
-        for (int j = 0; j < kLane; ++j) x[j] = __uint_as_float(j % 2 ? two[j / 2] & 0xFFFF0000u : two[j / 2] << 16);
+            for (int j = 0; j < kLane; ++j) x[j] = __uint_as_float(j % 2 ? two[j / 2] & 0xFFFF0000u : two[j / 2] << 16);
+        }
+        store8<T, WIDE>(out[value] + h * (value ? p.v_head : p.k_head) + e0, x);
     }
-    T *dst = value ? static_cast<T *>(p.v) + s * p.v_stride[0] + t * p.v_stride[1] + hd * p.v_stride[2]
-                   : static_cast<T *>(p.k) + s * p.k_stride[0] + t * p.k_stride[1] + hd * p.k_stride[2];
-    store8<T, WIDE>(dst + e0, x);
 }
 
 int lane_bits_of(int head_dim)
@@ -272,12 +358,25 @@ int lane_bits_of(int head_dim)
 
 }  // namespace
 
+// Tokens from which on the queries are left to the launch that appends to caches of 16 and 32 bits, without keys and values, and a wave takes all of a token's keys and
+// values; with fewer, a wave takes one pass.
+bool packed_append_apart(int tokens_all) { return tokens_all >= 8 * compute_units(); }
+
+static int passes_of(int heads, int lane_bits) { return (heads + (64 >> lane_bits) - 1) / (64 >> lane_bits); }
+
 hipError_t launch_packed_append(const PackedAppendProblem &given, int dtype, bool wide, hipStream_t stream)
 {
     PackedAppendProblem p = given;
+    const bool apart = packed_append_apart(p.tokens_all);
     p.lane_bits = lane_bits_of(p.head_dim);
-    p.block_tokens = p.tokens_all >= 8 * compute_units() ? kTokens : 1;
-    const int64_t grid = (static_cast<int64_t>(p.tokens_all) + p.block_tokens - 1) / p.block_tokens;
+    p.q_passes = passes_of(p.heads, p.lane_bits);
+    p.k_passes = passes_of(p.kv_heads, p.lane_bits);
+    p.first_pass = apart ? p.q_passes : 0;
+    p.passes = p.q_passes + 2 * p.k_passes;
+    p.slice = apart ? 2 * p.k_passes : 1;
+    const int slices = (p.passes - p.first_pass + p.slice - 1) / p.slice;
+    p.by_slices = Divider::of(slices);
+    const int64_t grid = (static_cast<int64_t>(p.tokens_all) * slices + kWaves - 1) / kWaves;
     if (grid >= kLaunchGroups) return hipErrorInvalidConfiguration;
     const dim3 groups(static_cast<unsigned>(grid)), threads(kThreads);
     if (dtype == 1) {
@@ -294,7 +393,11 @@ hipError_t launch_packed_read(const PackedReadProblem &given, int dtype, bool wi
 {
     PackedReadProblem p = given;
     p.lane_bits = lane_bits_of(p.head_dim);
-    const int64_t per = kThreads >> p.lane_bits, grid = (static_cast<int64_t>(p.tokens_all) * 2 * p.kv_heads + per - 1) / per;
+    p.k_passes = passes_of(p.kv_heads, p.lane_bits);
+    p.slice = p.tokens_all >= 8 * compute_units() ? 2 * p.k_passes : 1;
+    const int slices = (2 * p.k_passes + p.slice - 1) / p.slice;
+    p.by_slices = Divider::of(slices);
+    const int64_t grid = (static_cast<int64_t>(p.tokens_all) * slices + kWaves - 1) / kWaves;
     if (grid >= kLaunchGroups) return hipErrorInvalidConfiguration;
     const dim3 groups(static_cast<unsigned>(grid)), threads(kThreads);
     if (dtype == 1) {

@@ -84,23 +84,10 @@ static int allowed_width(int width, const void *p, const int64_t *stride, int co
     return width;
 }
 
-}  // namespace specgbv
-
-using namespace specgbv;
-
-extern "C" {
-
-specgbv_status specgbv_cache_append(const specgbv_paged_cache *cache, const specgbv_append_args *args, void *hip_stream)
+// The launch's arguments, from a cache and a call's arguments that have passed their checks; `width`: entries of a vector.
+static AppendProblem append_problem(const specgbv_paged_cache &c, const specgbv_append_args &a, int &width)
 {
-    specgbv_status st = check_cache(cache, true);
-    if (st != SPECGBV_OK) return st;
-    if (!args) return fail(SPECGBV_EINVAL, "null arguments");
-    const specgbv_paged_cache &c = *cache;
-    const specgbv_append_args &a = *args;
-    st = check_append(c, a);
-    if (st != SPECGBV_OK || c.sequences == 0 || a.tokens == 0) return st;
     const size_t esz = element_bytes(c.dtype);
-
     AppendProblem p{};
     p.q = a.q; p.k = a.k; p.v = a.v; p.q_out = a.q_out; p.k_cache = c.k; p.v_cache = c.v;
     p.q_weight = a.q_weight; p.k_weight = a.k_weight; p.positions = a.positions; p.inv_freq = a.inv_freq;
@@ -108,7 +95,7 @@ specgbv_status specgbv_cache_append(const specgbv_paged_cache *cache, const spec
     p.tokens_all = c.sequences * a.tokens;
     p.by_tokens = Divider::of(a.tokens);
     p.by_heads = Divider::of(a.heads + 2 * c.kv_heads);
-    int width = static_cast<int>(16 / esz);
+    width = static_cast<int>(16 / esz);
     while (a.pairs % width || c.head_dim % (2 * width)) width >>= 1;
     width = allowed_width(width, a.q, a.q_stride, 3, esz);
     width = allowed_width(width, a.k, a.k_stride, 3, esz);
@@ -124,6 +111,26 @@ specgbv_status specgbv_cache_append(const specgbv_paged_cache *cache, const spec
     p.positions_stride = a.positions_stride;
     p.eps = static_cast<float>(a.eps); p.inv_dim = 1.0f / c.head_dim;
     p.heads = a.heads; p.kv_heads = c.kv_heads; p.head_dim = c.head_dim; p.pairs = a.pairs; p.interleaved = a.interleaved != 0;
+    return p;
+}
+
+}  // namespace specgbv
+
+using namespace specgbv;
+
+extern "C" {
+
+specgbv_status specgbv_cache_append(const specgbv_paged_cache *cache, const specgbv_append_args *args, void *hip_stream)
+{
+    specgbv_status st = check_cache(cache, true);
+    if (st != SPECGBV_OK) return st;
+    if (!args) return fail(SPECGBV_EINVAL, "null arguments");
+    const specgbv_paged_cache &c = *cache;
+    const specgbv_append_args &a = *args;
+    st = check_append(c, a);
+    if (st != SPECGBV_OK || c.sequences == 0 || a.tokens == 0) return st;
+    int width;
+    const AppendProblem p = append_problem(c, a, width);
     const hipError_t e = launch_append(p, c.dtype == SPECGBV_BF16 ? 1 : 0, width, static_cast<hipStream_t>(hip_stream));
     if (e == hipErrorInvalidConfiguration) return fail(SPECGBV_EUNSUPPORTED, "too many tokens for one launch (%d)", p.tokens_all);
     if (e != hipSuccess) return fail(SPECGBV_EHIP, "append kernel launch: %s", hipGetErrorString(e));
@@ -324,6 +331,9 @@ template <typename P> static void set_packed_strides(P &p, const specgbv_packed_
     p.v_cache_stride[0] = c.v_page_stride; p.v_cache_stride[1] = c.v_head_stride; p.v_cache_stride[2] = c.v_token_stride;
     p.k_scale_stride[0] = c.k_scale_page_stride; p.k_scale_stride[1] = c.k_scale_head_stride; p.k_scale_stride[2] = c.k_scale_block_stride;
     p.v_scale_stride[0] = c.v_scale_page_stride; p.v_scale_stride[1] = c.v_scale_head_stride; p.v_scale_stride[2] = c.v_scale_block_stride;
+    p.k_cache_head = static_cast<int32_t>(c.k_head_stride); p.v_cache_head = static_cast<int32_t>(c.v_head_stride);
+    p.k_scale_head = static_cast<int32_t>(c.k_scale_head_stride); p.v_scale_head = static_cast<int32_t>(c.v_scale_head_stride);
+    p.k_scale_block = static_cast<int32_t>(c.k_scale_block_stride); p.v_scale_block = static_cast<int32_t>(c.v_scale_block_stride);
 }
 
 static bool wide_rows(const void *p, const int64_t *stride, size_t esz)
@@ -359,6 +369,8 @@ specgbv_status specgbv_packed_append(const specgbv_packed_cache *cache, const sp
     const specgbv_append_args &a = *args;
     st = check_append(c, a);
     if (st != SPECGBV_OK || c.sequences == 0 || a.tokens == 0) return st;
+    for (int64_t stride : {a.q_stride[2], a.k_stride[2], a.v_stride[2], a.q_out_stride[2]})
+        if (stride > INT32_MAX) return fail(SPECGBV_EUNSUPPORTED, "heads lie more than 2^31 - 1 entries apart");
     const size_t esz = element_bytes(c.dtype);
     PackedAppendProblem p{};
     p.q = a.q; p.k = a.k; p.v = a.v; p.q_out = a.q_out;
@@ -368,17 +380,27 @@ specgbv_status specgbv_packed_append(const specgbv_packed_cache *cache, const sp
     p.map = page_map(c);
     p.tokens_all = c.sequences * a.tokens;
     p.by_tokens = Divider::of(a.tokens);
-    p.by_heads = Divider::of(a.heads + 2 * c.kv_heads);
     for (int i = 0; i < 3; ++i) {
         p.q_stride[i] = a.q_stride[i]; p.k_stride[i] = a.k_stride[i]; p.v_stride[i] = a.v_stride[i]; p.q_out_stride[i] = a.q_out_stride[i];
     }
     set_packed_strides(p, *cache);
+    p.q_head = static_cast<int32_t>(a.q_stride[2]); p.k_head = static_cast<int32_t>(a.k_stride[2]);
+    p.v_head = static_cast<int32_t>(a.v_stride[2]); p.q_out_head = static_cast<int32_t>(a.q_out_stride[2]);
     p.positions_stride = a.positions_stride;
-    p.eps = a.eps;
+    p.eps = a.eps; p.inv_dim = 1.0f / c.head_dim;
     p.heads = a.heads; p.kv_heads = c.kv_heads; p.head_dim = c.head_dim; p.pairs = a.pairs; p.interleaved = a.interleaved != 0;
     const bool wide = a.pairs % 8 == 0 && wide_rows(a.q, a.q_stride, esz) && wide_rows(a.k, a.k_stride, esz) && wide_rows(a.v, a.v_stride, esz) &&
                       wide_rows(a.q_out, a.q_out_stride, esz) && aligned(a.q_weight, 16) && aligned(a.k_weight, 16);
-    const hipError_t e = launch_packed_append(p, c.dtype == SPECGBV_BF16 ? 1 : 0, wide, static_cast<hipStream_t>(hip_stream));
+    const int dtype = c.dtype == SPECGBV_BF16 ? 1 : 0;
+    hipError_t e = hipSuccess;
+    if (packed_append_apart(p.tokens_all)) {
+        int width;
+        AppendProblem queries = append_problem(c, a, width);
+        queries.kv_heads = 0;
+        queries.by_heads = Divider::of(a.heads);
+        e = launch_append(queries, dtype, width, static_cast<hipStream_t>(hip_stream));
+    }
+    if (e == hipSuccess) e = launch_packed_append(p, dtype, wide, static_cast<hipStream_t>(hip_stream));
     if (e == hipErrorInvalidConfiguration) return fail(SPECGBV_EUNSUPPORTED, "too many tokens for one launch (%d)", p.tokens_all);
     if (e != hipSuccess) return fail(SPECGBV_EHIP, "append kernel launch: %s", hipGetErrorString(e));
     return SPECGBV_OK;
@@ -400,6 +422,7 @@ specgbv_status specgbv_packed_read(const specgbv_packed_cache *cache, const spec
     const size_t esz = element_bytes(c.dtype);
     if (!aligned(a.k, esz) || !aligned(a.v, esz) || !aligned(a.positions, 4)) return fail(SPECGBV_EINVAL, "pointer not aligned to its element size");
     if (c.kv_heads > (1 << 29)) return fail(SPECGBV_EUNSUPPORTED, "a token has more than 2^29 heads");
+    if (a.k_stride[2] > INT32_MAX || a.v_stride[2] > INT32_MAX) return fail(SPECGBV_EUNSUPPORTED, "heads lie more than 2^31 - 1 entries apart");
     PackedReadProblem p{};
     p.k_cache = static_cast<const uint8_t *>(cache->k); p.v_cache = static_cast<const uint8_t *>(cache->v);
     p.k_scale = static_cast<const uint8_t *>(cache->k_scale); p.v_scale = static_cast<const uint8_t *>(cache->v_scale);
@@ -407,9 +430,9 @@ specgbv_status specgbv_packed_read(const specgbv_packed_cache *cache, const spec
     p.map = page_map(c);
     p.tokens_all = c.sequences * a.tokens;
     p.by_tokens = Divider::of(a.tokens);
-    p.by_heads = Divider::of(2 * c.kv_heads);
     set_packed_strides(p, *cache);
     for (int i = 0; i < 3; ++i) { p.k_stride[i] = a.k_stride[i]; p.v_stride[i] = a.v_stride[i]; }
+    p.k_head = static_cast<int32_t>(a.k_stride[2]); p.v_head = static_cast<int32_t>(a.v_stride[2]);
     p.positions_stride = a.positions_stride;
     p.kv_heads = c.kv_heads; p.head_dim = c.head_dim;
     const hipError_t e = launch_packed_read(p, c.dtype == SPECGBV_BF16 ? 1 : 0, wide_rows(a.k, a.k_stride, esz) && wide_rows(a.v, a.v_stride, esz),

@@ -229,9 +229,10 @@ class PackedCache(_Cache):
         self.pages, self.kv_heads, self.page_size, self.head_dim = pages, kv_heads, page_size, 2 * half
         self.sequences, self.width = table.shape
         self.dtype, self.device, self._index = dtype, k.device, k.get_device()
-        self._c = _PACKED.pack(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), table.data_ptr(), *k.stride()[:3], *v.stride()[:3],
-                               *k_scale.stride()[:3], *v_scale.stride()[:3], _between(table.stride(0), self.sequences, self.width), pages, kv_heads,
-                               page_size, self.head_dim, self.sequences, self.width, _DTYPES[dtype], 0)
+        # (the stride of a dimension of one is of no matter)
+        strides = [s if n > 1 else 0 for x in (k, v, k_scale, v_scale) for n, s in zip(x.shape[:3], x.stride()[:3])]
+        self._c = _PACKED.pack(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), table.data_ptr(), *strides, _between(table.stride(0), self.sequences, self.width),
+                               pages, kv_heads, page_size, self.head_dim, self.sequences, self.width, _DTYPES[dtype], 0)
 
     @classmethod
     def empty(cls, pages, kv_heads, page_size, head_dim, table, dtype=torch.bfloat16):

@@ -206,6 +206,17 @@ def test_what_a_packed_cache_is_made_of():
 
 
 @needs_no_gpu
+def test_the_stride_of_a_dimension_of_one_is_of_no_matter():
+    kv = [_said(torch.zeros(4096, dtype=torch.uint8).as_strided((1, 1, 8, 16), (7, 3, 16, 1))) for _ in range(2)]
+    scale = [_said(torch.zeros(4096, dtype=torch.uint8).as_strided((1, 1, 1, 8), (5, 1, 1, 1))) for _ in range(2)]
+    cache = sg.PackedCache(*kv, *scale, _said(torch.zeros((0, 4), dtype=torch.int32)))
+    pos = _said(torch.zeros((0, 2), dtype=torch.int32))
+    assert sg.specgbv_packed_read(cache, pos, stream=0)[0].shape == (0, 2, 1, 32)
+    q = _said(torch.zeros((0, 2, 4, 32), dtype=torch.bfloat16))
+    assert sg.specgbv_packed_attend(cache, q, pos, stream=0)[0].shape == q.shape
+
+
+@needs_no_gpu
 def test_what_calls_on_a_packed_cache_look_at():
     cache = sg.PackedCache(*_parts())
     pos = _said(torch.zeros((3, 2), dtype=torch.int32))
