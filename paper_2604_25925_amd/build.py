@@ -10,9 +10,10 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libspecgbv.so")
 SOURCES = ["specgbv_api.hip", "specgbv_split.hip", "specgbv_rows.hip", "specgbv_chain.hip", "specgbv_decide.hip", "specgbv_modify.hip", "specgbv_sample.hip", "specgbv_kseq.hip",
-           "specgbv_append.hip", "specgbv_attend.hip", "specgbv_filter.hip", "specgbv_packed.hip", "specgbv_packed_attend.hip", "specgbv_pages.hip",
+           "specgbv_append.hip", "specgbv_attend.hip", "specgbv_filter.hip", "specgbv_packed.hip", "specgbv_packed_attend.hip", "specgbv_packed_attend_64.hip",
+           "specgbv_packed_attend_128.hip", "specgbv_packed_attend_256.hip", "specgbv_pages.hip",
            "specgbv_step_api.hip"]
-HEADERS = ["specgbv_device.hpp", "specgbv_internal.hpp", "specgbv_paged.hpp", "specgbv_attend.hpp", os.path.join("..", "..", "include", "specgbv.h")]
+HEADERS = ["specgbv_device.hpp", "specgbv_internal.hpp", "specgbv_paged.hpp", "specgbv_attend.hpp", "specgbv_packed_attend.hpp", os.path.join("..", "..", "include", "specgbv.h")]
 FLAGS = ["-O3", "--offload-arch=gfx950", "-fPIC", "-std=c++17", "-Wall", "-Wno-unused-function",
          # packed-FP32 instructions are not to be generated on the test machines
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
@@ -52,7 +53,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
             raise RuntimeError("hipcc failed:\n%s\n%s" % (" ".join(cmd), r.stderr))
         return r.stderr
 
-    with ThreadPoolExecutor(max_workers=4) as ex:
+    with ThreadPoolExecutor(max_workers=8) as ex:
         for err in ex.map(run, jobs):
             if verbose and err.strip():
                 print(err, file=sys.stderr)

@@ -219,6 +219,9 @@ AttendPlan plan_packed_attend(int sequences, int drafts, bool shared, int tokens
 size_t packed_attend_bytes(int sequences, int drafts, bool shared, int tokens, int heads, int kv_heads, int head_dim, int element_bytes, int window,
                            int64_t held);
 hipError_t launch_packed_attend(const PackedProblem &p, int dtype, hipStream_t stream);
+hipError_t launch_packed_attend_64(const PackedProblem &p, int dtype, hipStream_t stream);       // by the entries of a head
+hipError_t launch_packed_attend_128(const PackedProblem &p, int dtype, hipStream_t stream);
+hipError_t launch_packed_attend_256(const PackedProblem &p, int dtype, hipStream_t stream);
 
 // Appending to a paged cache of 4-bit entries (see specgbv_packed_append); strides of q, k, v in elements, of the cache in bytes.
 struct PackedAppendProblem {
