@@ -415,22 +415,32 @@ __global__ void __launch_bounds__(kAttendThreads, (packed_waves(sizeof(T), DP, R
         // weights
         const bool lost = lost_here >> quad / kRuns & 1;
         const bool partial = tile < lo_most || tile + kTile > hi_least || tile + kTile > end || lost_here != 0;
+        if (partial) {
+            const int base = tile + quad * kRunKeys;
 #pragma unroll
-        for (int r = 0; r < RT; ++r) {
-            if (partial) {
-                const int base = tile + quad * kRunKeys;
+            for (int r = 0; r < RT; ++r) {
                 const int from = max(row_low[r] - base, 0), to = lost ? 0 : min(max(row_high[r] - base, 0), kRunKeys);
 #pragma unroll
                 for (int k = 0; k < kRunKeys; ++k) s[r][k / 4][k % 4] = k >= from && k < to ? s[r][k / 4][k % 4] : -INFINITY;
             }
-            float top = s[r][0][0];
+        }
+        // (all rows' maxima first, and one branch for all: the rows' exponentials then stand side by side)
+        float top[RT];
+        bool raise = false;
 #pragma unroll
-            for (int k = 1; k < kRunKeys; ++k) top = fmaxf(top, s[r][k / 4][k % 4]);
-            top *= p.c;
-            if (__any(top > ref[r] + kRaise)) {
+        for (int r = 0; r < RT; ++r) {
+            top[r] = s[r][0][0];
+#pragma unroll
+            for (int k = 1; k < kRunKeys; ++k) top[r] = fmaxf(top[r], s[r][k / 4][k % 4]);
+            top[r] *= p.c;
+            raise = raise || top[r] > ref[r] + kRaise;
+        }
+        if (__any(raise)) {
+#pragma unroll
+            for (int r = 0; r < RT; ++r) {
                 // (row by row: what a row gets does not hang on the rows next to it)
-                top = row_largest(top);
-                const float now = top > ref[r] + kRaise ? top : ref[r];
+                const float most = row_largest(top[r]);
+                const float now = most > ref[r] + kRaise ? most : ref[r];
                 const float f = now == ref[r] ? 1.0f : exp2_of(ref[r] - now);        // (-inf to -inf: nothing summed yet)
                 vast = vast || __any(fabsf(now) > 1048576.0f && now != -INFINITY);
                 ref[r] = now;
@@ -438,21 +448,30 @@ __global__ void __launch_bounds__(kAttendThreads, (packed_waves(sizeof(T), DP, R
 #pragma unroll
                 for (int c = 0; c < kCols; ++c) acc[r][c] *= f;
             }
-            const float m = ref[r] == -INFINITY ? 0.0f : ref[r];
-            if (vast) {
+        }
+        if (vast) {
+#pragma unroll
+            for (int r = 0; r < RT; ++r) {
+                const float m = ref[r] == -INFINITY ? 0.0f : ref[r];
 #pragma unroll
                 for (int k = 0; k < kRunKeys; ++k) {
                     float x = s[r][k / 4][k % 4] * p.c;
                     asm volatile("" : "+v"(x));                // (rounded by itself)
                     s[r][k / 4][k % 4] = exp2_of(x - m);
                 }
-            } else {
+            }
+        } else {
+#pragma unroll
+            for (int r = 0; r < RT; ++r) {
+                const float m = ref[r] == -INFINITY ? 0.0f : ref[r];
 #pragma unroll
                 for (int k = 0; k < kRunKeys; ++k) s[r][k / 4][k % 4] = exp2_of(fmaf(s[r][k / 4][k % 4], p.c, -m));
             }
+        }
+#pragma unroll
+        for (int r = 0; r < RT; ++r)
 #pragma unroll
             for (int k = 0; k < kRunKeys; ++k) sum[r] += s[r][k / 4][k % 4];
-        }
 
         // A value is not finite only where its block's power says so (bytes above 252), and a weight of 0 does not take it out.  In tiles that some rows
         // do not see whole, keys that no row sees are cleared, blocks of the others that are not finite as well, and the rows that do see one get NaN:
