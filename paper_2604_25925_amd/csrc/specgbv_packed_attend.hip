@@ -16,21 +16,33 @@ static AttendPlan plan_for(int sequences, int drafts, bool shared, int tokens, i
     a.all_parts = a.units;
     if (window > 0) longest = longest < static_cast<int64_t>(window) + tokens ? longest : static_cast<int64_t>(window) + tokens;
     const int64_t base = static_cast<int64_t>(a.units) * kv_heads * a.row_blocks;             // stretches of rows with keys of their own
-    a.few = rows <= 1024;
-    const int64_t slots = static_cast<int64_t>(compute_units()) * packed_waves(element_bytes, dp, a.block_rows / 16) * (a.few ? 1 : kWavesPerGroup);
-    const int least = a.few ? 256 : 128;
+    a.few = 1;                                                 // (the waves of a workgroup share its rows)
+    const int RT = a.block_rows / 16;
+    const int64_t slots = static_cast<int64_t>(compute_units()) * packed_waves(element_bytes, dp, RT);      // workgroups on the card at once
+    // Keys of a part at least.  128 / 256 / 512, us: one query of 32 heads on 8 kv heads of 128, 10.0 / 10.7 / 12.1 at 4000 tokens; 4 sequences, 9 queries, 22.7 / 20.1 / 21.7 at 2000
+    // and 25.4 / 25.5 / 23.1 at 4000; 8 sequences at heads of 256 11.8 / 12.9 / 15.2 at 2000, 14.9 / 13.1 / 15.0 at 4000.
+    const int least = RT == 1 && dp <= 128 ? 128 : 256;
     int64_t chunks = slots / (base < 1 ? 1 : base);
     const int64_t most = (longest + least - 1) / least;
     if (chunks > most) chunks = most;
     if (chunks > kMaxParts) chunks = kMaxParts;
+    // Parts cost a join, 4 us and more, and pay from a length on that is the greater the fewer there can be.  In one pass / in parts, us: one query of 32 heads 7.1 / 10.0 at 300 tokens,
+    // 8.6 / 10.0 at 600, 10.9 / 10.0 at 1000; of 32 sequences 9.2 / 14.0 at 600, 13.7 / 17.4 at 1000, 22.0 / 22.9 at 2000; 4 sequences, 9 queries, 17.1 / 16.6 at 300, 20.2 / 17.1 at 600;
+    // 24 float32 sequences, 5 queries of 14 heads on 2 kv heads of 64, 10.5 / 13.9 at 300, 16.3 / 16.0 at 1000; 8 at heads of 256 9.9 / 11.6 at 300, 12.1 / 11.8 at 600.
+    const int64_t one_pass = RT == 4 ? 256 : (RT == 2 || dp == 256 ? 480 : 800);
+    if (longest * slots <= one_pass * (slots + 6 * base)) chunks = 1;
     if (chunks < 1) chunks = 1;
-    if (chunks == 1 && !shared) {                              // one pass, nothing to join
-        if (a.few && longest <= 208 && base > slots) a.few = 0;        // few tiles, and more workgroups than the card holds at once: each wave by itself
+    if (chunks == 1 && !shared) {                              // nothing to join
+        // Few tiles, and more workgroups than the card holds at once: each wave by itself, which saves turns and the join in LDS.  Waves / workgroups, us, one query of 256 sequences, 32 heads
+        // on 8 kv heads of 128: 10.4 / 14.7 at 40 tokens, 18.6 / 20.8 at 300, 23.7 / 23.5 at 440; at heads of 256 9.2 / 15.6, 21.8 / 23.4, 27.2 / 26.3; of 64 5.7 / 6.7, 8.7 / 8.3 at 200;
+        // 9 queries of 64 sequences (64 rows a workgroup) 25.8 / 24.4 at 40 and 51 / 33 at 640, in float32 (32 rows) 22 / 49 and 50 / 72.
+        const int64_t by_waves = RT == 4 ? 0 : (RT == 2 ? 1024 : (dp == 64 ? 128 : 400));
+        if (longest <= by_waves && base > slots) a.few = 0;
         return a;
     }
     a.own_keys = shared ? drafts * 32 : 0;
     a.chunk_keys = least;
-    a.grain = a.few ? kWavesPerGroup * kTile : kTile;
+    a.grain = kWavesPerGroup * kTile;
     a.balanced = a.units <= 64 && (shared || tokens <= 64);
     if (a.balanced) {
         int64_t parts = slots / (static_cast<int64_t>(kv_heads) * a.row_blocks);
@@ -50,17 +62,37 @@ static AttendPlan plan_for(int sequences, int drafts, bool shared, int tokens, i
     return a;
 }
 
+// Drafts that share short prefixes are sequences like others: each reads the prefix again, which in 4 bits is little, and what it has of its own needs no
+// turn of its own and nothing is to be joined.  Shared / alone, us: 32 prefixes of 8 drafts, a token each (32 heads, 8 kv heads of 128, bfloat16) 22 / 10 at 40 tokens,
+// 23 / 20 at 320, 25 / 24 at 640, 29 / 40 at 1280; 8 of 8, 9 tokens each, 28 / 24 at 40, 45 / 38 at 1280, 55 / 53 at 2560, 69 / 105 at 5120; 16 of 4, 5 tokens each of 10 heads on
+// 2 kv heads (float32) 21 / 13 at 40, 35 / 34 at 2560; 4 of 4, 9 tokens each, heads of 256, 18 / 14 at 40, 28 / 26 at 1280, 32 / 36 at 2560; one of 8, a token each, 8 kv heads of 128,
+// 14.6 / 14.6 at 2560, 18 / 24 at 10240.  Up to which length they are taken by themselves:
+static int64_t alone_up_to(int sequences, int kv_heads, int head_dim)
+{
+    const int64_t entries = (head_dim > 128 ? int64_t{1} << 25 : int64_t{1} << 27) / (static_cast<int64_t>(sequences) * kv_heads * head_dim);
+    return entries < 2560 ? entries : 2560;
+}
+
+// (a call asks for the workspace of either way)
 AttendPlan plan_packed_attend(int sequences, int drafts, bool shared, int tokens, int heads, int kv_heads, int head_dim, int element_bytes, int window,
                               int64_t longest)
 {
-    return plan_for(sequences, drafts, shared, tokens, heads, kv_heads, head_dim, element_bytes, window, longest);
+    const AttendPlan plan = plan_for(sequences, drafts, shared, tokens, heads, kv_heads, head_dim, element_bytes, window, longest);
+    if (!shared || longest > alone_up_to(sequences, kv_heads, head_dim)) return plan;
+    AttendPlan alone = plan_for(sequences, 1, false, tokens, heads, kv_heads, head_dim, element_bytes, window, longest);
+    if (alone.bytes < plan.bytes) alone.bytes = plan.bytes;
+    return alone;
 }
 
 // The parts of a plan, and so its bytes, do not get fewer with the length: the longest one of each way asks for most.
 size_t packed_attend_bytes(int sequences, int drafts, bool shared, int tokens, int heads, int kv_heads, int head_dim, int element_bytes, int window,
                            int64_t held)
 {
-    return plan_for(sequences, drafts, shared, tokens, heads, kv_heads, head_dim, element_bytes, window, held).bytes;
+    const size_t whole = plan_for(sequences, drafts, shared, tokens, heads, kv_heads, head_dim, element_bytes, window, held).bytes;
+    const int64_t near = shared ? alone_up_to(sequences, kv_heads, head_dim) : 0;
+    if (near < 1) return whole;
+    const size_t alone = plan_for(sequences, 1, false, tokens, heads, kv_heads, head_dim, element_bytes, window, near < held ? near : held).bytes;
+    return alone > whole ? alone : whole;
 }
 
 hipError_t launch_packed_attend(const PackedProblem &p, int dtype, hipStream_t stream)
