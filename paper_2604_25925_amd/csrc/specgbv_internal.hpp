@@ -240,12 +240,10 @@ struct PackedAppendProblem {
     double eps;
     float inv_dim;
     int tokens_all, heads, kv_heads, head_dim, pairs, interleaved;
-    int lane_bits, q_passes, k_passes, first_pass, passes, slice;   // set by launch_packed_append; slice: a wave's passes
+    int lane_bits, q_passes, k_passes, passes, slice;   // set by launch_packed_append; slice: a wave's passes
 };
 // wide: strides and addresses allow 16-byte loads, and a vector's partners in the rotation are a vector.
 hipError_t launch_packed_append(const PackedAppendProblem &p, int dtype, bool wide, hipStream_t stream);
-// Whether that launch takes keys and values alone, and launch_append the queries.
-bool packed_append_apart(int tokens_all);
 
 struct PackedReadProblem {
     const uint8_t *k_cache, *v_cache, *k_scale, *v_scale;

@@ -190,7 +190,7 @@ __global__ void __launch_bounds__(kThreads, WIDE ? (sizeof(T) == 2 ? 5 : 4) : 3)
     const int at_all = static_cast<int>(blockIdx.x) * kWaves + wave;
     const int n = p.by_slices.div(at_all), slice = p.by_slices.mod(at_all, n);
     if (n >= p.tokens_all) return;
-    const int first = p.first_pass + slice * p.slice, last = min(p.passes, first + p.slice);
+    const int first = slice * p.slice, last = min(p.passes, first + p.slice);
     const int k_pass = p.q_passes, v_pass = p.q_passes + p.k_passes;
     const Token tk = token_of(p.by_tokens, p.positions, p.positions_stride, n);
     const int lanes = 1 << p.lane_bits, u = lane & (lanes - 1), e0 = u * kLane, head = lane >> p.lane_bits, heads = 64 >> p.lane_bits;
@@ -358,23 +358,19 @@ int lane_bits_of(int head_dim)
 
 }  // namespace
 
-// Tokens from which on the queries are left to the launch that appends to caches of 16 and 32 bits, without keys and values, and a wave takes all of a token's keys and
-// values; with fewer, a wave takes one pass.
-bool packed_append_apart(int tokens_all) { return tokens_all >= 8 * compute_units(); }
-
 static int passes_of(int heads, int lane_bits) { return (heads + (64 >> lane_bits) - 1) / (64 >> lane_bits); }
 
 hipError_t launch_packed_append(const PackedAppendProblem &given, int dtype, bool wide, hipStream_t stream)
 {
     PackedAppendProblem p = given;
-    const bool apart = packed_append_apart(p.tokens_all);
     p.lane_bits = lane_bits_of(p.head_dim);
     p.q_passes = passes_of(p.heads, p.lane_bits);
     p.k_passes = passes_of(p.kv_heads, p.lane_bits);
-    p.first_pass = apart ? p.q_passes : 0;
     p.passes = p.q_passes + 2 * p.k_passes;
-    p.slice = apart ? 2 * p.k_passes : 1;
-    const int slices = (p.passes - p.first_pass + p.slice - 1) / p.slice;
+    // Few tokens: a wave takes one pass.  Many: all of a token's, which then needs its sines and cosines once.  All / 4 / 2 / 1 of 12 passes a wave, 5 prompts of up to 4001
+    // tokens: 83 / 89 / 107 / 157 us.
+    p.slice = p.tokens_all >= 8 * compute_units() ? p.passes : 1;
+    const int slices = (p.passes + p.slice - 1) / p.slice;
     p.by_slices = Divider::of(slices);
     const int64_t grid = (static_cast<int64_t>(p.tokens_all) * slices + kWaves - 1) / kWaves;
     if (grid >= kLaunchGroups) return hipErrorInvalidConfiguration;

@@ -391,16 +391,7 @@ specgbv_status specgbv_packed_append(const specgbv_packed_cache *cache, const sp
     p.heads = a.heads; p.kv_heads = c.kv_heads; p.head_dim = c.head_dim; p.pairs = a.pairs; p.interleaved = a.interleaved != 0;
     const bool wide = a.pairs % 8 == 0 && wide_rows(a.q, a.q_stride, esz) && wide_rows(a.k, a.k_stride, esz) && wide_rows(a.v, a.v_stride, esz) &&
                       wide_rows(a.q_out, a.q_out_stride, esz) && aligned(a.q_weight, 16) && aligned(a.k_weight, 16);
-    const int dtype = c.dtype == SPECGBV_BF16 ? 1 : 0;
-    hipError_t e = hipSuccess;
-    if (packed_append_apart(p.tokens_all)) {
-        int width;
-        AppendProblem queries = append_problem(c, a, width);
-        queries.kv_heads = 0;
-        queries.by_heads = Divider::of(a.heads);
-        e = launch_append(queries, dtype, width, static_cast<hipStream_t>(hip_stream));
-    }
-    if (e == hipSuccess) e = launch_packed_append(p, dtype, wide, static_cast<hipStream_t>(hip_stream));
+    const hipError_t e = launch_packed_append(p, c.dtype == SPECGBV_BF16 ? 1 : 0, wide, static_cast<hipStream_t>(hip_stream));
     if (e == hipErrorInvalidConfiguration) return fail(SPECGBV_EUNSUPPORTED, "too many tokens for one launch (%d)", p.tokens_all);
     if (e != hipSuccess) return fail(SPECGBV_EHIP, "append kernel launch: %s", hipGetErrorString(e));
     return SPECGBV_OK;
