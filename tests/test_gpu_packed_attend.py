@@ -120,6 +120,59 @@ def test_drafts_of_a_prefix(B, K, T, H, G, D, page, dtype, window):
         check(again, cache, q, positions, dtype, window=window, label=label + " max_len %d" % max_len)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("B,K,T,H,G,D,page", [(3, 4, 1, 8, 2, 64, 16), (2, 8, 3, 8, 2, 128, 8), (2, 2, 9, 4, 4, 64, 32), (1, 8, 9, 16, 2, 128, 16), (70, 2, 1, 4, 1, 64, 8),
+                                              (2, 3, 2, 4, 1, 256, 16)])
+@pytest.mark.parametrize("window", [0, 50])
+def test_drafts_of_a_prefix_in_a_table_for_long_ones(B, K, T, H, G, D, page, dtype, window):
+    """Tables of more than 2560 tokens: the drafts' shared pages are read once, also where a prefix is short, empty or all that a draft has."""
+    import torch
+    gen = np.random.default_rng(B * 100 + K + 7)
+    width = 2700 // page + 1
+    cache = make_packed(gen, B * K, width, page, G, D, dtype)
+    whole = gen.integers(0, (2680 if B < 5 else 400) // page, B)
+    whole[0] = 0
+    whole[-1] = 100 // page
+    if B > 2:
+        whole[1] = width - 1
+    _share(cache, K, whole)
+    shared = whole * page
+    rows = [[int(shared[b]) + int(gen.integers(0, page)) + t if gen.random() > 0.1 else -1 for t in range(T)] for b in range(B) for _ in range(K)]
+    rows[0] = [-1] * T                                       # a draft of padding alone
+    rows[-1] = [int(shared[-1]) - 1] * T                     # one that has nothing but the prefix
+    positions = _positions(rows)
+    q = _q(gen, (B * K, T, H, D), dtype)
+    out, _ = sg.specgbv_packed_attend(cache, q, positions, window=window, shared_len=torch.from_numpy(shared.astype(np.int32)).cuda())
+    check(out, cache, q, positions, dtype, window=window, label=_label(B, K, T, H, G, D, page, dtype, window))
+
+
+@pytest.mark.parametrize("S,T,H,G,D,length,dtype", [(70, 1, 4, 1, 64, 3000, "bf16"), (66, 1, 4, 1, 64, 3000, "f32"), (1, 70, 2, 1, 128, 2900, "bf16"), (2, 100, 4, 2, 64, 1500, "f32")])
+def test_more_units_than_are_weighed_in_parts(S, T, H, G, D, length, dtype):
+    """Parts of equal lengths: more than 64 sequences, or prompts in chunks, over long tables, some of which hold little."""
+    gen = np.random.default_rng(S + T)
+    cache = make_packed(gen, S, (length + 15) // 16, 16, G, D, dtype)
+    q = _q(gen, (S, T, H, D), dtype)
+    last = [length - 1] + [int(n) for n in gen.integers(T - 1, length, S - 1)]
+    positions = _positions([[n - T + 1 + t for t in range(T)] for n in last])
+    for window in (0, 1200):
+        out, _ = sg.specgbv_packed_attend(cache, q, positions, window=window)
+        check(out, cache, q, positions, dtype, window=window, label=_label(S, T, H, G, D, length, dtype, window))
+
+
+@pytest.mark.parametrize("S,T,H,G,D,length,dtype", [(600, 1, 4, 2, 64, 100, "bf16"), (530, 1, 4, 2, 64, 100, "f32"), (300, 1, 8, 4, 128, 260, "bf16"), (140, 9, 8, 4, 128, 130, "f32"),
+                                                    (300, 1, 4, 2, 256, 150, "bf16"), (260, 1, 2, 2, 256, 70, "f32"), (200, 9, 16, 4, 128, 50, "bf16")])
+@pytest.mark.parametrize("window", [0, 33])
+def test_more_sequences_than_workgroups_at_once(S, T, H, G, D, length, dtype, window):
+    """Each wave by itself, in workgroups whose last waves have nothing."""
+    gen = np.random.default_rng(S + D)
+    page = 16 if D == 64 else 8
+    cache = make_packed(gen, S, (length + page - 1) // page, page, G, D, dtype)
+    q = _q(gen, (S, T, H, D), dtype)
+    positions = _positions([[int(n) - T + 1 + t if n >= 0 else -1 for t in range(T)] for n in gen.integers(-1, length, S)])
+    out, _ = sg.specgbv_packed_attend(cache, q, positions, window=window)
+    check(out, cache, q, positions, dtype, window=window, label=_label(S, T, H, G, D, length, dtype, window))
+
+
 def test_long_sequences_in_parts():
     gen = np.random.default_rng(8)
     for S, T, H, G, D, length, hint in ((1, 1, 8, 2, 128, 20000, None), (2, 3, 4, 1, 64, 9000, 100), (1, 40, 8, 1, 128, 5000, None)):
@@ -261,6 +314,18 @@ def test_strides_and_addresses(dtype):
         sg.specgbv_packed_attend(cache, q, positions, out=out)
         check(out, cache, q, positions, dtype, label=_label(dtype, q.stride()))
         assert (back[:, :, H] == 3).all() and (back[..., :3] == 3).all() and (back[..., D + 3:] == 3).all()
+
+
+@pytest.mark.parametrize("D,page,S", [(64, 32, 2), (128, 8, 2), (256, 32, 2), (64, 24, 2)])
+def test_pages_of_other_sizes_more_than_2_to_the_32_bytes_apart(D, page, S):
+    gen = np.random.default_rng(D + page)
+    T, H, G, width = 2, 4, 2, 1
+    cache = make_packed(gen, S, width, page, G, D, extra=1, page_stride=2 ** 31 - 16)
+    cache.table[0, 0], cache.table[1, 0] = 2, 0
+    q = _q(gen, (S, T, H, D), "bf16")
+    positions = _positions([[5, 6], [page - 2, page - 1]])
+    out, _ = sg.specgbv_packed_attend(cache, q, positions)
+    check(out, cache, q, positions, "bf16", label=_label(D, page))
 
 
 @pytest.mark.parametrize("D", [64, 128])
