@@ -103,9 +103,8 @@ __global__ void __launch_bounds__(kAttendThreads, (packed_waves(sizeof(T), DP, R
     constexpr int kSteps = S::kSteps, kPieces = S::kPieces, kWords = S::kWords, kVec = S::kVec, kGroups = S::kGroups, kCols = S::kCols,
                   N = sizeof(T) == 2 ? 1 : 3;
     constexpr bool kQueriesInLds = RT == 4;                   // 64 rows: registers are left for their sums alone
-    constexpr int kOperands = RT * kSteps * 64;               // of a wave's queries, 16 bytes each
     const AttendProblem &p = pk.a;
-    __shared__ F4 sh_acc[SHARED ? kWavesPerGroup * RT * kGroups * 4 * 64 : (kQueriesInLds ? kWavesPerGroup * kOperands : 1)];
+    __shared__ F4 sh_acc[SHARED ? kWavesPerGroup * RT * kGroups * 4 * 64 : 1];
     __shared__ float sh_m[kWavesPerGroup][RT * 16], sh_l[kWavesPerGroup][RT * 16];
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -144,13 +143,13 @@ __global__ void __launch_bounds__(kAttendThreads, (packed_waves(sizeof(T), DP, R
     }
 
     // ---- queries
-    static_assert(!kQueriesInLds || (N == 1 && RT == kWavesPerGroup), "a wave brings one tile of 16 rows to LDS");
+    static_assert(!kQueriesInLds || (SHARED && N == 1 && RT == kWavesPerGroup), "a wave brings one tile of 16 rows to LDS");
     U4 qf[kQueriesInLds ? 1 : RT][kQueriesInLds ? 1 : kSteps][N];
-    U4 *q_lds = reinterpret_cast<U4 *>(sh_acc) + (SHARED ? 0 : wave * kOperands) + lane;
+    U4 *q_lds = reinterpret_cast<U4 *>(sh_acc) + lane;
     const T *q = static_cast<const T *>(p.q);
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
-        if (kQueriesInLds && SHARED && r != wave) continue;
+        if (kQueriesInLds && r != wave) continue;
 #pragma unroll
         for (int i = 0; i < kSteps; ++i) {
             const int e = S::entry(i, quad);
@@ -191,10 +190,7 @@ __global__ void __launch_bounds__(kAttendThreads, (packed_waves(sizeof(T), DP, R
             }
         }
     }
-    if constexpr (kQueriesInLds) {
-        if constexpr (SHARED) __syncthreads();
-        else __builtin_amdgcn_wave_barrier();
-    }
+    if constexpr (kQueriesInLds) __syncthreads();
 #pragma unroll
     for (int r = 0; r < RT; ++r)
         if (row0 + r * 16 + col >= row_end) pos[r] = -1;
@@ -668,7 +664,7 @@ hipError_t launch_tall(const PackedProblem &p, hipStream_t stream)
         if (pages == 2) return launch_pages<T, DP, RT, true, true, 2, uint32_t>(p, stream);
         return p.near ? launch_pages<T, DP, RT, true, true, 4, uint32_t>(p, stream) : launch_pages<T, DP, RT, true, true, 4, uint64_t>(p, stream);
     }
-    if (!p.a.few) {
+    if constexpr (RT < 4) if (!p.a.few) {                      // (64 rows: the waves always share them)
         if (pages == 1) return launch_pages<T, DP, RT, false, false, 1, uint64_t>(p, stream);
         if (pages == 2) return launch_pages<T, DP, RT, false, false, 2, uint32_t>(p, stream);
         if (p.near) return launch_pages<T, DP, RT, false, false, 4, uint32_t>(p, stream);

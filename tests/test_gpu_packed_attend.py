@@ -316,6 +316,26 @@ def test_strides_and_addresses(dtype):
         assert (back[:, :, H] == 3).all() and (back[..., :3] == 3).all() and (back[..., D + 3:] == 3).all()
 
 
+@pytest.mark.parametrize("way,page", [(way, page) for way in ("one pass", "parts", "waves") for page in (32, 16, 8)] + [("one pass", "far"), ("parts", "far")])
+@pytest.mark.parametrize("dtype,D,T", [("bf16", 64, 5), ("bf16", 64, 17), ("bf16", 64, 40), ("bf16", 128, 5), ("bf16", 128, 17), ("bf16", 128, 40), ("bf16", 256, 5),
+                                       ("bf16", 256, 17), ("f32", 64, 5), ("f32", 64, 17), ("f32", 128, 5), ("f32", 128, 17), ("f32", 256, 5)])
+def test_rows_pages_and_ways(dtype, D, T, way, page):
+    """16, 32 and 64 rows at once; pages of whole, half and quarter tiles; one pass, parts, and (with more rows than workgroups) waves by themselves."""
+    gen = np.random.default_rng(D + T)
+    far = page == "far"
+    page = 8 if far else page
+    S, G, length = {"one pass": (3, 2, 90), "parts": (2, 1, 2500), "waves": (265, 4, 60)}[way]
+    width = (length + page - 1) // page
+    stride = None
+    if far:
+        stride = 2 ** 32 // (S * width - 2) // 16 * 16
+    cache = make_packed(gen, S, width, page, G, D, dtype, extra=1, page_stride=stride)
+    q = _q(gen, (S, T, G, D), dtype)
+    positions = _positions([[int(n) - T + 1 + t for t in range(T)] for n in gen.integers(length // 2, length, S)])
+    out, _ = sg.specgbv_packed_attend(cache, q, positions)
+    check(out, cache, q, positions, dtype, label=_label(dtype, D, T, way, page, far))
+
+
 @pytest.mark.parametrize("D,page,S", [(64, 32, 2), (128, 8, 2), (256, 32, 2), (64, 24, 2)])
 def test_pages_of_other_sizes_more_than_2_to_the_32_bytes_apart(D, page, S):
     gen = np.random.default_rng(D + page)
