@@ -32,7 +32,8 @@ def _check(pool, host, label):
 
 
 @pytest.mark.parametrize("B,K,width,page,pages", [(1, 1, 4, 8, 4), (1, 8, 40, 16, 200), (3, 2, 9, 8, 30), (32, 8, 20, 16, 2000), (40, 3, 30, 8, 700), (130, 1, 12, 16, 600),
-                                                  (1000, 2, 20, 16, 9000), (1025, 1, 10, 8, 4000), (70, 4, 300, 8, 30000), (2500, 1, 30, 8, 20000), (1024, 4, 16, 8, 30000)])
+                                                  (1000, 2, 20, 16, 9000), (1025, 1, 10, 8, 4000), (70, 4, 300, 8, 30000), (2500, 1, 30, 8, 20000), (1024, 4, 16, 8, 30000), (1024, 1, 30, 8, 9000), (128, 8, 64, 16, 50000),
+                                                  (341, 3, 30, 8, 20000), (342, 3, 30, 8, 20000)])
 def test_steps_of_a_batch(B, K, width, page, pages):
     import torch
     gen = np.random.default_rng(B * 10 + K)
