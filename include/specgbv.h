@@ -422,7 +422,8 @@ specgbv_status specgbv_read_sample_intermediates(
 /*
  * A decoding step around the verification: keys and values of new tokens are appended to a paged cache, their queries
  * attend over it, draft tokens are drawn from truncated distributions and the rows handed to the verification are truncated
- * the same way.  All three calls are asynchronous on hip_stream, allocate nothing and can be captured into a HIP graph.
+ * the same way; the cache may hold its entries in 4 bits, and its pages may be dealt out on the device.  All these calls are asynchronous on
+ * hip_stream, allocate nothing and can be captured into a HIP graph.
  *
  * The cache.  Token t of sequence s lives in slot t % page_size of page table[s * table_stride + t / page_size]; element
  * (page, head, slot, i) of k is k[page * k_page_stride + head * k_head_stride + slot * k_token_stride + i], so a page may hold its
@@ -510,7 +511,8 @@ size_t specgbv_attend_workspace_bytes(const specgbv_paged_cache *cache, const sp
  * that sees such entries may get what is not finite).
  *
  * Table, pages and limits are those of specgbv_paged_cache, and head_dim is a multiple of 32; k_scale and v_scale are 8-byte aligned with
- * strides of whole 8 bytes, blocks at most 2^26 bytes apart.
+ * strides of whole 8 bytes, blocks at most 2^26 bytes apart.  Strides of the cache are at most 2^31 - 1 bytes, and so, in elements, are the strides between the
+ * heads of what is appended, rotated and read.
  */
 typedef struct {
     void *k, *v;               /* device, uint8 */

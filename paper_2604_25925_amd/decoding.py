@@ -31,6 +31,8 @@ _DTYPES = {torch.float32: F32, torch.bfloat16: BF16}
 
 # The handle of a device's current stream without a Stream object around it (1.8 us of a call's 9), where this torch has it.
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+# (and the current device without a check that CUDA is up, which tensors on it say)
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 
 def _stream(device, stream: Optional[int]) -> int:
@@ -46,7 +48,7 @@ def _between(stride: int, rows: int, length: int) -> int:
 
 def _on(index: int, call, *args):
     """The call with the GPU `index` as the current one, which a launch on its streams needs."""
-    if index < 0 or index == torch.cuda.current_device():
+    if index < 0 or index == _current_device():
         return call(*args)
     with torch.cuda.device(index):
         return call(*args)
@@ -329,7 +331,7 @@ class PagePool:
 
 
 def _numbers(name, x, shape, index, dtype=torch.int32):
-    if tuple(x.shape) != shape or x.dtype is not dtype or x.get_device() != index or not x.is_contiguous():
+    if x.shape != shape or x.dtype is not dtype or x.get_device() != index or not x.is_contiguous():
         raise ValueError("%s must be dense %s %s on the call's GPU" % (name, dtype, list(shape)))
     return x
 
@@ -350,12 +352,8 @@ def specgbv_pages_advance(pool: PagePool, length, *, chosen=None, room: int = 0,
     _numbers("length", length, shape, pool._index)
     if chosen is not None:
         _numbers("chosen", chosen, shape, pool._index)
-    if shared_len is None:
-        shared_len = torch.empty(shape, dtype=torch.int32, device=length.device)
-    if served is None:
-        served = torch.empty(shape, dtype=torch.int32, device=length.device)
-    _numbers("shared_len", shared_len, shape, pool._index)
-    _numbers("served", served, shape, pool._index)
+    shared_len = length.new_empty(shape) if shared_len is None else _numbers("shared_len", shared_len, shape, pool._index)
+    served = length.new_empty(shape) if served is None else _numbers("served", served, shape, pool._index)
     if workspace is None:
         workspace = torch.empty(max(int(lib.specgbv_pages_workspace_bytes(pool._c)), 256), dtype=torch.uint8, device=pool.device)
     else:
@@ -364,6 +362,15 @@ def specgbv_pages_advance(pool: PagePool, length, *, chosen=None, room: int = 0,
     _check(_on(pool._index, lib.specgbv_pages_advance, pool._c, args, workspace.data_ptr(), workspace.numel() * workspace.element_size(),
                _stream(pool.device, stream)))
     return shared_len, served, workspace
+
+
+def _rows(name, x, table, rows, length, dtype):
+    """(x, entries between its rows): int [rows, length] beside a table, new where x is None."""
+    if x is None:
+        return table.new_empty((rows, length), dtype=dtype), length
+    if x.shape != (rows, length) or x.dtype is not dtype or x.get_device() != table.get_device() or (length > 1 and x.stride(1) != 1):
+        raise ValueError("%s must be %s [%d, %d] on the table's GPU, its rows dense" % (name, dtype, rows, length))
+    return x, _between(x.stride(0), rows, length)
 
 
 def specgbv_slot_map(table, start, count, tokens: int, *, page_size: int, pages: int, drafts: int = 1, right: bool = False, flat: bool = True,
@@ -381,22 +388,10 @@ def specgbv_slot_map(table, start, count, tokens: int, *, page_size: int, pages:
         raise ValueError("tokens must be >= 0, got %d" % tokens)
     _numbers("start", start, (S // drafts,), index)
     _numbers("count", count, (S // drafts,), index)
-    if positions is None:
-        positions = torch.empty((S, tokens), dtype=torch.int32, device=table.device)
-    if flat and slots is None:
-        slots = torch.empty((S, tokens), dtype=torch.int64, device=table.device)
-    elif not flat:
-        slots = None
-    between = []
-    for name, x, dtype in (("positions", positions, torch.int32), ("slots", slots, torch.int64)):
-        if x is None:
-            between.append(tokens)
-            continue
-        if tuple(x.shape) != (S, tokens) or x.dtype is not dtype or x.get_device() != index or (tokens > 1 and x.stride(1) != 1):
-            raise ValueError("%s must be %s [%d, %d] on the table's GPU, its rows dense" % (name, dtype, S, tokens))
-        between.append(_between(x.stride(0), S, tokens))
-    args = _SLOTS.pack(table.data_ptr(), start.data_ptr(), count.data_ptr(), positions.data_ptr(), slots.data_ptr() if slots is not None else 0,
-                       _between(table.stride(0), S, table.shape[1]), between[0], between[1], S, drafts, table.shape[1], page_size, pages, tokens,
+    positions, positions_stride = _rows("positions", positions, table, S, tokens, torch.int32)
+    slots, slots_stride = _rows("slots", slots, table, S, tokens, torch.int64) if flat else (None, tokens)
+    args = _SLOTS.pack(table.data_ptr(), start.data_ptr(), count.data_ptr(), positions.data_ptr(), slots.data_ptr() if flat else 0,
+                       _between(table.stride(0), S, table.shape[1]), positions_stride, slots_stride, S, drafts, table.shape[1], page_size, pages, tokens,
                        1 if right else 0, 0)
     _check(_on(index, lib.specgbv_slot_map, args, _stream(table.device, stream)))
     return positions, slots
