@@ -3,8 +3,9 @@
 
 namespace specgbv {
 
+// in_parts: the plan that needs most workspace.
 static AttendPlan plan_for(int sequences, int drafts, bool shared, int tokens, int heads, int kv_heads, int head_dim, int element_bytes, int window,
-                           int64_t longest)
+                           int64_t longest, bool in_parts = false)
 {
     AttendPlan a{};
     a.drafts = drafts; a.shared = shared;
@@ -16,7 +17,7 @@ static AttendPlan plan_for(int sequences, int drafts, bool shared, int tokens, i
     a.all_parts = a.units;
     if (window > 0) longest = longest < static_cast<int64_t>(window) + tokens ? longest : static_cast<int64_t>(window) + tokens;
     const int64_t base = static_cast<int64_t>(a.units) * kv_heads * a.row_blocks;             // stretches of rows with keys of their own
-    a.few = 1;                                                 // (the waves of a workgroup share its rows)
+    a.few = kWavesPerGroup;                                    // (that share a workgroup's rows; 0: none do)
     const int RT = a.block_rows / 16;
     const int64_t slots = static_cast<int64_t>(compute_units()) * packed_waves(element_bytes, dp, RT);      // workgroups on the card at once
     // Keys of a part at least.  128 / 256 / 512, us: one query of 32 heads on 8 kv heads of 128, 10.0 / 10.7 / 12.1 at 4000 tokens; 4 sequences, 9 queries, 22.7 / 20.1 / 21.7 at 2000
@@ -32,6 +33,15 @@ static AttendPlan plan_for(int sequences, int drafts, bool shared, int tokens, i
     const int64_t one_pass = RT == 4 ? 256 : (RT == 2 || dp == 256 ? 480 : 800);
     if (longest * slots <= one_pass * (slots + 6 * base)) chunks = 1;
     if (chunks < 1) chunks = 1;
+    // About a workgroup for each compute unit: one that fills it, and no parts.  Parts / filled, us: 32 sequences, a query of 32 heads on 8 kv heads of 128 (16 waves) 10.8 / 11.6 at 800 tokens,
+    // 18.8 / 17.2 at 1600, 29.9 / 25.5 at 3200; 16 of them 17.3 / 14.3 at 1600, 21.7 / 20.6 at 3200; 16 with 5 queries (8 waves) 11.1 / 11.4 at 400, 14.0 / 13.0 at 800, 20.2 / 17.6 at 1600,
+    // 25.6 / 26.2 at 3200; 24 float32 sequences, 5 queries of 14 heads on 2 kv heads of 64, 15.0 / 13.7 at 800, 18.8 / 18.6 at 1600, 22.6 / 28.5 at 3200.  Drafts that share a prefix: 32 of 8 (a query
+    // each, 8 waves) 25.1 / 21.3 at 800, 30.2 / 26.2 at 1600, 39.4 / 36.8 at 3200; 16 of 8 24.4 / 21.9 at 1600, 29.2 / 31.8 at 3200.
+    const int wide = packed_wide(element_bytes, dp, RT);
+    if (!in_parts && wide > kWavesPerGroup && base <= compute_units() && longest <= 14 * base && longest > (shared ? 0 : (wide == 16 ? 1000 : 600))) {
+        a.few = wide;
+        return a;
+    }
     if (chunks == 1 && !shared) {                              // nothing to join
         // Few tiles, and more workgroups than the card holds at once: each wave by itself, which saves turns and the join in LDS.  Waves / workgroups, us, one query of 256 sequences, 32 heads
         // on 8 kv heads of 128: 10.4 / 14.7 at 40 tokens, 18.6 / 20.8 at 300, 23.7 / 23.5 at 440; at heads of 256 9.2 / 15.6, 21.8 / 23.4, 27.2 / 26.3; of 64 5.7 / 6.7, 8.7 / 8.3 at 200;
@@ -67,9 +77,10 @@ static AttendPlan plan_for(int sequences, int drafts, bool shared, int tokens, i
 // 23 / 20 at 320, 25 / 24 at 640, 29 / 40 at 1280; 8 of 8, 9 tokens each, 28 / 24 at 40, 45 / 38 at 1280, 55 / 53 at 2560, 69 / 105 at 5120; 16 of 4, 5 tokens each of 10 heads on
 // 2 kv heads (float32) 21 / 13 at 40, 35 / 34 at 2560; 4 of 4, 9 tokens each, heads of 256, 18 / 14 at 40, 28 / 26 at 1280, 32 / 36 at 2560; one of 8, a token each, 8 kv heads of 128,
 // 14.6 / 14.6 at 2560, 18 / 24 at 10240.  Up to which length they are taken by themselves:
-static int64_t alone_up_to(int sequences, int kv_heads, int head_dim)
+// Where their prefixes would be taken whole by workgroups that fill a compute unit, up to half of it: 32 of 8 17.9 / 17.9 at 200, 18 / 25 at 400; 16 of 8 15.8 / 14.6 at 400, 16.8 / 21.2 at 800.
+static int64_t alone_up_to(int sequences, int kv_heads, int head_dim, bool filled)
 {
-    const int64_t entries = (head_dim > 128 ? int64_t{1} << 25 : int64_t{1} << 27) / (static_cast<int64_t>(sequences) * kv_heads * head_dim);
+    const int64_t entries = (head_dim > 128 ? int64_t{1} << 25 : int64_t{1} << 27) / (static_cast<int64_t>(sequences) * kv_heads * head_dim) / (filled ? 2 : 1);
     return entries < 2560 ? entries : 2560;
 }
 
@@ -78,20 +89,20 @@ AttendPlan plan_packed_attend(int sequences, int drafts, bool shared, int tokens
                               int64_t longest)
 {
     const AttendPlan plan = plan_for(sequences, drafts, shared, tokens, heads, kv_heads, head_dim, element_bytes, window, longest);
-    if (!shared || longest > alone_up_to(sequences, kv_heads, head_dim)) return plan;
+    if (!shared || longest > alone_up_to(sequences, kv_heads, head_dim, plan.few > kWavesPerGroup)) return plan;
     AttendPlan alone = plan_for(sequences, 1, false, tokens, heads, kv_heads, head_dim, element_bytes, window, longest);
     if (alone.bytes < plan.bytes) alone.bytes = plan.bytes;
     return alone;
 }
 
-// The parts of a plan, and so its bytes, do not get fewer with the length: the longest one of each way asks for most.
+// The parts of a plan in parts, and so its bytes, do not get fewer with the length: the longest one of each way asks for most.
 size_t packed_attend_bytes(int sequences, int drafts, bool shared, int tokens, int heads, int kv_heads, int head_dim, int element_bytes, int window,
                            int64_t held)
 {
-    const size_t whole = plan_for(sequences, drafts, shared, tokens, heads, kv_heads, head_dim, element_bytes, window, held).bytes;
-    const int64_t near = shared ? alone_up_to(sequences, kv_heads, head_dim) : 0;
+    const size_t whole = plan_for(sequences, drafts, shared, tokens, heads, kv_heads, head_dim, element_bytes, window, held, true).bytes;
+    const int64_t near = shared ? alone_up_to(sequences, kv_heads, head_dim, false) : 0;
     if (near < 1) return whole;
-    const size_t alone = plan_for(sequences, 1, false, tokens, heads, kv_heads, head_dim, element_bytes, window, near < held ? near : held).bytes;
+    const size_t alone = plan_for(sequences, 1, false, tokens, heads, kv_heads, head_dim, element_bytes, window, near < held ? near : held, true).bytes;
     return alone > whole ? alone : whole;
 }
 

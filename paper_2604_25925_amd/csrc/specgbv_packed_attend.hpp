@@ -14,8 +14,8 @@
 // takes its right operand.  Of the values a lane takes 8 adjacent entries (4 for heads of 64 and less) of the 8 keys of its run, one word a key, and the 8
 // keys' powers in one load (they lie next to each other).
 //
-// SHARED (few rows): the waves of a workgroup have the same rows, take the tiles in turn and join at the end through LDS.  Else every wave has rows of its own and
-// walks all tiles by itself; no barrier anywhere, and the waves of a workgroup find each other's tiles in the cache.
+// SHARED: the waves of a workgroup have the same rows, take the tiles in turn and join at the end through LDS: four of them, or as many as a compute unit holds where there is
+// about one workgroup for each.  Else every wave has rows of its own and walks all tiles by itself; no barrier anywhere, and the waves of a workgroup find each other's tiles in the cache.
 #pragma once
 
 #include "specgbv_attend.hpp"
@@ -43,6 +43,13 @@ constexpr int packed_waves(int element_bytes, int DP, int RT)
 {
     if (element_bytes == 4) return DP == 64 ? (RT == 1 ? 4 : 2) : (DP == 128 && RT == 1 ? 3 : 1);
     return DP == 256 ? (RT == 1 ? 2 : 1) : (RT == 1 ? 4 : RT == 2 ? (DP == 64 ? 3 : 2) : 2);
+}
+
+// Waves of a workgroup that has a compute unit for itself (4: there is none but the usual one).
+constexpr int packed_wide(int element_bytes, int DP, int RT)
+{
+    const int waves = packed_waves(element_bytes, DP, RT);
+    return RT == 4 || waves == 1 ? 4 : (waves >= 4 ? 16 : 8);
 }
 
 // Most tiles of 16 rows that a wave takes.
@@ -96,16 +103,18 @@ template <int N> __device__ __forceinline__ void operands(const float (&x)[8], U
     }
 }
 
-template <typename T, int DP, int RT, bool SHARED, bool PARTS, int PAGES, typename Off>
-__global__ void __launch_bounds__(kAttendThreads, (packed_waves(sizeof(T), DP, RT))) k_packed_attend(PackedProblem pk)
+// WAVES: of a workgroup that share its rows; 0: each of four by itself.
+template <typename T, int DP, int RT, int WAVES, bool PARTS, int PAGES, typename Off>
+__global__ void __launch_bounds__(WAVES > 0 ? WAVES * 64 : kAttendThreads, (packed_waves(sizeof(T), DP, RT))) k_packed_attend(PackedProblem pk)
 {
+    constexpr bool SHARED = WAVES > 0, kOwn = PARTS || WAVES > kWavesPerGroup;      // kOwn: drafts may share keys and have keys of their own
     using S = Packed<DP>;
     constexpr int kSteps = S::kSteps, kPieces = S::kPieces, kWords = S::kWords, kVec = S::kVec, kGroups = S::kGroups, kCols = S::kCols,
                   N = sizeof(T) == 2 ? 1 : 3;
     constexpr bool kQueriesInLds = RT == 4;                   // 64 rows: registers are left for their sums alone
     const AttendProblem &p = pk.a;
-    __shared__ F4 sh_acc[SHARED ? kWavesPerGroup * RT * kGroups * 4 * 64 : 1];
-    __shared__ float sh_m[kWavesPerGroup][RT * 16], sh_l[kWavesPerGroup][RT * 16];
+    __shared__ F4 sh_acc[SHARED ? WAVES * RT * kGroups * 4 * 64 : 1];
+    __shared__ float sh_m[SHARED ? WAVES : 1][RT * 16], sh_l[SHARED ? WAVES : 1][RT * 16];
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int col = lane & 15, quad = lane >> 4;
@@ -143,7 +152,7 @@ __global__ void __launch_bounds__(kAttendThreads, (packed_waves(sizeof(T), DP, R
     }
 
     // ---- queries
-    static_assert(!kQueriesInLds || (SHARED && N == 1 && RT == kWavesPerGroup), "a wave brings one tile of 16 rows to LDS");
+    static_assert(!kQueriesInLds || (N == 1 && RT <= WAVES), "a wave brings one tile of 16 rows to LDS");
     U4 qf[kQueriesInLds ? 1 : RT][kQueriesInLds ? 1 : kSteps][N];
     U4 *q_lds = reinterpret_cast<U4 *>(sh_acc) + lane;
     const T *q = static_cast<const T *>(p.q);
@@ -232,15 +241,15 @@ __global__ void __launch_bounds__(kAttendThreads, (packed_waves(sizeof(T), DP, R
 
     // the drafts' own keys, behind the shared ones: the unit's parts take the drafts in turn, and so do the waves of a workgroup that share its rows
     const int draft0 = p.by_in_draft.div(row0), draft1 = p.by_in_draft.div(row_end - 1) + 1;       // drafts with rows here
-    const int own_to = !PARTS || !p.shared_len ? 0 : draft1;
-    const int own_from = draft0 + (SHARED ? kWavesPerGroup * part + wave : part), own_step = (SHARED ? kWavesPerGroup : 1) * share.parts;
-    bool any = draft0 + (SHARED ? kWavesPerGroup : 1) * part < own_to;        // something may have been summed (the same for waves that share their rows)
+    const int own_to = !kOwn || !p.shared_len ? 0 : draft1;
+    const int own_from = draft0 + WAVES * part + wave, own_step = WAVES * share.parts;
+    bool any = draft0 + WAVES * part < own_to;        // something may have been summed (the same for waves that share their rows)
     bool vast = false;                                        // a row of this wave has a reference beyond 2^20
 #pragma unroll 1
     for (int seg = -1; seg < own_to; seg = seg < 0 ? own_from : seg + own_step) {
     const bool own = seg >= 0;                                // -1: what the unit's sequences share
     const bool turns = SHARED && !own;                        // the waves take the tiles in turn
-    const int step = turns ? kWavesPerGroup * kTile : kTile;
+    const int step = turns ? WAVES * kTile : kTile;
     const int sequence = first + max(seg, 0);
     int row_low[RT], row_high[RT];
     int lo_all = INT32_MAX, lo_most = -1, hi_all = 0, hi_least = INT32_MAX;
@@ -571,9 +580,9 @@ __global__ void __launch_bounds__(kAttendThreads, (packed_waves(sizeof(T), DP, R
         for (int r = 0; r < RT; ++r) {
             float most = -INFINITY, total = 0.0f;
 #pragma unroll
-            for (int w = 0; w < kWavesPerGroup; ++w) most = fmaxf(most, sh_m[w][r * 16 + col]);
+            for (int w = 0; w < WAVES; ++w) most = fmaxf(most, sh_m[w][r * 16 + col]);
 #pragma unroll
-            for (int w = 0; w < kWavesPerGroup; ++w) {
+            for (int w = 0; w < WAVES; ++w) {
                 const float m = sh_m[w][r * 16 + col];
                 total += sh_l[w][r * 16 + col] * (m == most ? 1.0f : exp2_of(m - most));
             }
@@ -621,10 +630,12 @@ __global__ void __launch_bounds__(kAttendThreads, (packed_waves(sizeof(T), DP, R
             for (int r = 0; r < RT; ++r)
 #pragma unroll
                 for (int g = 0; g < kGroups; ++g) {
+                    if (WAVES > kWavesPerGroup && (r * kGroups + g) % (WAVES / kWavesPerGroup) != wave / kWavesPerGroup) continue;
+                    const int i = wave % kWavesPerGroup;
                     F4 v{0, 0, 0, 0};
 #pragma unroll
-                    for (int w = 0; w < kWavesPerGroup; ++w) v += sh_acc[(((w * RT + r) * kGroups + g) * 4 + wave) * 64 + lane];
-                    emit(r, g, wave, n, v);
+                    for (int w = 0; w < WAVES; ++w) v += sh_acc[(((w * RT + r) * kGroups + g) * 4 + i) * 64 + lane];
+                    emit(r, g, i, n, v);
                 }
         } else {
 #pragma unroll
@@ -638,40 +649,42 @@ __global__ void __launch_bounds__(kAttendThreads, (packed_waves(sizeof(T), DP, R
     }
 }
 
-template <typename T, int DP, int RT, bool SHARED, bool PARTS, int PAGES, typename Off>
+template <typename T, int DP, int RT, int WAVES, bool PARTS, int PAGES, typename Off>
 hipError_t launch_pages(PackedProblem p, hipStream_t stream)
 {
     p.a.items = p.a.all_parts * p.a.kv_heads;
     p.a.by_blocks = Divider::of(p.a.row_blocks);
-    const int64_t all = static_cast<int64_t>(p.a.items) * p.a.row_blocks, groups = SHARED ? all : (all + kWavesPerGroup - 1) / kWavesPerGroup;
+    const int64_t all = static_cast<int64_t>(p.a.items) * p.a.row_blocks, groups = WAVES > 0 ? all : (all + kWavesPerGroup - 1) / kWavesPerGroup;
     // a strip: the row blocks of an item (of four items where waves have rows of their own), shorter where there would be few strips for 8 XCDs
     int64_t strip = groups / 32 < 1 ? 1 : groups / 32;
     if (strip > p.a.row_blocks) strip = p.a.row_blocks;
     p.by_strip = Divider::of(static_cast<int32_t>(strip));
     const int64_t grid = (groups + 8 * strip - 1) / (8 * strip) * (8 * strip);
     if (grid >= kLaunchGroups) return hipErrorInvalidConfiguration;
-    hipLaunchKernelGGL((k_packed_attend<T, DP, RT, SHARED, PARTS, PAGES, Off>), dim3(static_cast<unsigned>(grid)), dim3(kAttendThreads), 0, stream, p);
+    hipLaunchKernelGGL((k_packed_attend<T, DP, RT, WAVES, PARTS, PAGES, Off>), dim3(static_cast<unsigned>(grid)), dim3(WAVES > 0 ? WAVES * 64 : kAttendThreads), 0, stream, p);
     return hipGetLastError();
+}
+
+template <typename T, int DP, int RT, int WAVES, bool PARTS>
+hipError_t launch_ways(const PackedProblem &p, hipStream_t stream)
+{
+    const int page = static_cast<int>(p.a.map.page.d);
+    if (page % 32 == 0) return launch_pages<T, DP, RT, WAVES, PARTS, 1, uint64_t>(p, stream);
+    if (p.near && page % 16 == 0) return launch_pages<T, DP, RT, WAVES, PARTS, 2, uint32_t>(p, stream);
+    if constexpr (WAVES > 0) if (!p.near) return launch_pages<T, DP, RT, WAVES, PARTS, 4, uint64_t>(p, stream);
+    return launch_pages<T, DP, RT, WAVES, PARTS, 4, uint32_t>(p, stream);
 }
 
 template <typename T, int DP, int RT>
 hipError_t launch_tall(const PackedProblem &p, hipStream_t stream)
 {
-    const int page = static_cast<int>(p.a.map.page.d);
-    const int pages = page % 32 == 0 ? 1 : (p.near && page % 16 == 0 ? 2 : 4);
-    if (p.a.ml) {
-        if (pages == 1) return launch_pages<T, DP, RT, true, true, 1, uint64_t>(p, stream);
-        if (pages == 2) return launch_pages<T, DP, RT, true, true, 2, uint32_t>(p, stream);
-        return p.near ? launch_pages<T, DP, RT, true, true, 4, uint32_t>(p, stream) : launch_pages<T, DP, RT, true, true, 4, uint64_t>(p, stream);
-    }
-    if constexpr (RT < 4) if (!p.a.few) {                      // (64 rows: the waves always share them)
-        if (pages == 1) return launch_pages<T, DP, RT, false, false, 1, uint64_t>(p, stream);
-        if (pages == 2) return launch_pages<T, DP, RT, false, false, 2, uint32_t>(p, stream);
-        if (p.near) return launch_pages<T, DP, RT, false, false, 4, uint32_t>(p, stream);
-    }
-    if (pages == 1) return launch_pages<T, DP, RT, true, false, 1, uint64_t>(p, stream);
-    if (pages == 2) return launch_pages<T, DP, RT, true, false, 2, uint32_t>(p, stream);
-    return p.near ? launch_pages<T, DP, RT, true, false, 4, uint32_t>(p, stream) : launch_pages<T, DP, RT, true, false, 4, uint64_t>(p, stream);
+    constexpr int kWide = packed_wide(sizeof(T), DP, RT);
+    if (p.a.ml) return launch_ways<T, DP, RT, kWavesPerGroup, true>(p, stream);
+    if constexpr (RT < 4)                                      // (64 rows: the waves always share them)
+        if (!p.a.few && (p.near || p.a.map.page.d % 32 == 0)) return launch_ways<T, DP, RT, 0, false>(p, stream);
+    if constexpr (kWide > kWavesPerGroup)
+        if (p.a.few == kWide) return launch_ways<T, DP, RT, kWide, false>(p, stream);
+    return launch_ways<T, DP, RT, kWavesPerGroup, false>(p, stream);
 }
 
 template <typename T, int DP>

@@ -336,6 +336,52 @@ def test_rows_pages_and_ways(dtype, D, T, way, page):
     check(out, cache, q, positions, dtype, label=_label(dtype, D, T, way, page, far))
 
 
+@pytest.mark.parametrize("page", [32, 16, 8, "far"])
+@pytest.mark.parametrize("dtype,D,T", [("bf16", 64, 5), ("bf16", 64, 17), ("bf16", 128, 5), ("bf16", 128, 17), ("bf16", 256, 5), ("f32", 64, 5), ("f32", 64, 17), ("f32", 128, 5)])
+def test_workgroups_that_fill_a_compute_unit(dtype, D, T, page):
+    """About as many rows of workgroups as compute units, over lengths that parts would be made of; sequences with little or nothing among them."""
+    gen = np.random.default_rng(D + T + 1)
+    far = page == "far"
+    page = 8 if far else page
+    S, G, length = 40, 2, 1060
+    width = (length + page - 1) // page
+    cache = make_packed(gen, S, width, page, G, D, dtype, extra=1, page_stride=2 ** 32 // (S * width - 2) // 16 * 16 if far else None)
+    q = _q(gen, (S, T, G, D), dtype)
+    last = [length - 1, T - 1, -1, 40] + [int(n) for n in gen.integers(T - 1, length, S - 4)]
+    positions = _positions([[max(n - T + 1 + t, -1) for t in range(T)] for n in last])
+    label = _label(dtype, D, T, page, far)
+    out, ws = sg.specgbv_packed_attend(cache, q, positions)
+    check(out, cache, q, positions, dtype, label=label)
+    for window, max_len in ((700, None), (0, 300)):          # (the workspace serves the parts of other lengths too)
+        out, _ = sg.specgbv_packed_attend(cache, q, positions, window=window, max_len=max_len, workspace=ws)
+        check(out, cache, q, positions, dtype, window=window, label=label + " %d %s" % (window, max_len))
+
+
+@pytest.mark.parametrize("B,K,T,H,G,D,page,dtype", [(24, 8, 1, 8, 8, 64, 16, "bf16"), (16, 8, 1, 16, 8, 128, 16, "f32"), (16, 8, 3, 8, 8, 128, 32, "bf16"), (16, 8, 2, 8, 8, 256, 8, "bf16"),
+                                                    (12, 16, 1, 16, 8, 64, 8, "f32"), (16, 8, 4, 8, 8, 64, 64, "bf16")])
+def test_drafts_in_workgroups_that_fill_a_compute_unit(B, K, T, H, G, D, page, dtype):
+    import torch
+    gen = np.random.default_rng(B + K + D)
+    width = 900 // page + 2
+    cache = make_packed(gen, B * K, width, page, G, D, dtype)
+    whole = gen.integers(0, 900 // page, B)
+    whole[0], whole[1] = 0, width - 1
+    _share(cache, K, whole)
+    shared = whole * page
+    rows = [[int(shared[b]) + int(gen.integers(0, page)) + t if gen.random() > 0.1 else -1 for t in range(T)] for b in range(B) for _ in range(K)]
+    rows[0] = [-1] * T
+    rows[-1] = [max(int(shared[-1]) - 1, 0)] * T
+    positions = _positions(rows)
+    q = _q(gen, (B * K, T, H, D), dtype)
+    shared = torch.from_numpy(shared.astype(np.int32)).cuda()
+    label = _label(B, K, T, H, G, D, page, dtype)
+    ws = None
+    for window, max_len in ((0, None), (60, None), (0, 2000), (0, 200)):
+        out, used = sg.specgbv_packed_attend(cache, q, positions, window=window, shared_len=shared, max_len=max_len, workspace=ws)
+        ws = used if ws is None else ws
+        check(out, cache, q, positions, dtype, window=window, label=label + " %d %s" % (window, max_len))
+
+
 @pytest.mark.parametrize("D,page,S", [(64, 32, 2), (128, 8, 2), (256, 32, 2), (64, 24, 2)])
 def test_pages_of_other_sizes_more_than_2_to_the_32_bytes_apart(D, page, S):
     gen = np.random.default_rng(D + page)
