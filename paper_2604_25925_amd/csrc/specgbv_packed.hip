@@ -12,6 +12,11 @@
 //
 // A lane has 8 adjacent entries, which are one word of the cache, and four lanes a block; the entry that another one turns with is read a second
 // time (from the cache) instead of exchanged.  Every entry is read from memory once.
+//
+// What bounds it.  5 prompts of up to 4001 tokens (32 heads, 8 kv heads of 128, bfloat16, norms): appending 82 us for 276 MB, 3.4 TB/s: waits, 74 % of the waves' time, for the chain from the
+// position over the table to the inputs, of which the registers (5 waves a SIMD) hold no more at once: inputs one pass ahead spill (87 us), 4 and 6 waves 87 us.  Keys in
+// float32 first, and in float64 only near borders: 22 us more, nearly every wave has one that lies near.  Reading back 18 us for 91 MB, 5 TB/s.  256 tokens of drafts 6.5 and 3.5 us, one
+// token 3.4 and 2.4: the same chain once.
 #include "specgbv_internal.hpp"
 
 namespace specgbv {

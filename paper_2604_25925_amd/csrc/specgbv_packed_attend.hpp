@@ -16,6 +16,12 @@
 //
 // SHARED: the waves of a workgroup have the same rows, take the tiles in turn and join at the end through LDS: four of them, or as many as a compute unit holds where there is
 // about one workgroup for each.  Else every wave has rows of its own and walks all tiles by itself; no barrier anywhere, and the waves of a workgroup find each other's tiles in the cache.
+//
+// What bounds it (heads of 128, 32 on 8 kv heads, bfloat16, unless said).  4 sequences of 131072 tokens: the reads, 570 MB in 104 + 5 us, 5.5 TB/s.  32 prefixes of up to 2048 tokens with 8
+// drafts, a query each: 26 us for 43 MB; the start (positions, rows, queries, table, 3.5 us) and the join in LDS (2 us) stand beside 4 to 8 tiles a wave, each of which
+// waits for its loads.  8 prefixes of up to 4096 tokens, 8 drafts, 9 queries each (32 rows at once): 47 + 8 us for 19 GFLOP, the longest prefix's parts last longest.  With 64 rows at once a tile takes
+// a wave 4000 cycles, of which 1024 are the matrix unit's: scores 1270, weights 1310, values 1110 follow each other, and two waves a SIMD (the sums are 128 registers) cover little of it.
+// 24 float32 sequences, 5 queries of 14 heads on 2 kv heads of 64, window 1000: 13 us, 2 tiles a wave between the start and the join of 16 waves.  One query of 200 tokens: 5.5 us, all latency.
 #pragma once
 
 #include "specgbv_attend.hpp"
@@ -41,8 +47,8 @@ constexpr int kTile = 32, kRunKeys = 8;
 // Waves per SIMD that the registers of rows, sums and a tile leave room for.
 constexpr int packed_waves(int element_bytes, int DP, int RT)
 {
-    if (element_bytes == 4) return DP == 64 ? (RT == 1 ? 4 : 2) : (DP == 128 && RT == 1 ? 3 : 1);
-    return DP == 256 ? (RT == 1 ? 2 : 1) : (RT == 1 ? 4 : RT == 2 ? (DP == 64 ? 3 : 2) : 2);
+    if (element_bytes == 4) return DP == 64 ? 4 : (DP == 128 ? 3 : 1);
+    return DP == 256 ? 2 : (RT == 1 ? 4 : RT == 2 && DP == 64 ? 3 : 2);
 }
 
 // Waves of a workgroup that has a compute unit for itself (4: there is none but the usual one).
@@ -52,8 +58,9 @@ constexpr int packed_wide(int element_bytes, int DP, int RT)
     return RT == 4 || waves == 1 ? 4 : (waves >= 4 ? 16 : 8);
 }
 
-// Most tiles of 16 rows that a wave takes.
-constexpr int rows_tall(int element_bytes, int DP) { return element_bytes == 4 ? (DP == 256 ? 1 : 2) : (DP == 256 ? 2 : 4); }
+// Most tiles of 16 rows that a wave takes: more pay for bfloat16 heads of up to 128 only.  Two for one, us: float32, 200 sequences of 36 rows, heads of 64, 73 / 54 at 1024 tokens, 199 / 152 at 4096; 32 of 85
+// rows, heads of 128, 57 / 34 and 150 / 89 (one wave a SIMD); bfloat16 heads of 256, 64 of 72 rows 53 / 43 and 130 / 109, 128 of 68 79 / 66 and 214 / 195.
+constexpr int rows_tall(int element_bytes, int DP) { return element_bytes == 4 || DP == 256 ? 1 : 4; }
 
 // Two entries of a word (byte SEL) at a power of two, whose exponent stands in bits 23 to 30; the other bits are of no matter, an exponent of
 // all ones gives NaN.
@@ -602,9 +609,11 @@ __global__ void __launch_bounds__(WAVES > 0 ? WAVES * 64 : kAttendThreads, (pack
     }
     if (PARTS && !any) return;                                // (the same for waves that share their rows)
     T *out[RT];
+    int row1 = row0;
+    asm volatile("" : "+s"(row1));                            // (worked out anew: kept over the loop, the rows' places would be registers)
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
-        const int row = min(row0 + r * 16 + col, row_end - 1), d = p.by_in_draft.div(row), in = p.by_in_draft.mod(row, d), t = p.by_group.div(in);
+        const int row = min(row1 + r * 16 + col, row_end - 1), d = p.by_in_draft.div(row), in = p.by_in_draft.mod(row, d), t = p.by_group.div(in);
         out[r] = static_cast<T *>(p.out) + (PARTS ? 0 : (first + d) * p.out_stride[0] + t * p.out_stride[1] + (head0 * p.group + p.by_group.mod(in, t)) * p.out_stride[2]);
     }
     auto emit = [&](int r, int g, int i, int n, F4 v) {
@@ -691,11 +700,12 @@ template <typename T, int DP>
 hipError_t launch_typed(const PackedProblem &p, hipStream_t stream)
 {
     if (p.a.ml && join_grid<DP>(p.a) >= kLaunchGroups) return hipErrorInvalidConfiguration;
-    constexpr int kTall = rows_tall(sizeof(T), DP);
-    hipError_t e;
+    hipError_t e = hipErrorInvalidValue;
     if (p.a.block_rows == 16) e = launch_tall<T, DP, 1>(p, stream);
-    else if (kTall > 2 && p.a.block_rows == 32) e = launch_tall<T, DP, kTall < 2 ? kTall : 2>(p, stream);
-    else e = launch_tall<T, DP, kTall>(p, stream);
+    if constexpr (rows_tall(sizeof(T), DP) > 1) {
+        if (p.a.block_rows == 32) e = launch_tall<T, DP, 2>(p, stream);
+        if (p.a.block_rows == 64) e = launch_tall<T, DP, 4>(p, stream);
+    }
     return e != hipSuccess || !p.a.ml ? e : launch_join<T, DP, Packed<DP>::kVec>(p.a, stream);
 }
 

@@ -65,9 +65,12 @@ def make_packed(gen, S, width, page, G, D, dtype="bf16", token_major=False, extr
 
 def dense(cache):
     """(k, v) of a cache as float64 [pages, G, page, D] on the host."""
+    both = np.stack((CODES[np.arange(256) & 15], CODES[np.arange(256) >> 4]), axis=-1)         # of a byte
     out = []
     for x, s in ((cache.k, cache.k_scale), (cache.v, cache.v_scale)):
-        out.append(values(unpack(x.cpu().numpy()), np.swapaxes(s.cpu().numpy(), 2, 3)))
+        x, byte = x.cpu().numpy(), np.swapaxes(s.cpu().numpy(), 2, 3)
+        scale = np.where(byte == 255, np.nan, 2.0 ** (byte.astype(np.float64) - 127.0))
+        out.append((both[x].reshape(x.shape[:3] + (-1, 32)) * scale[..., None]).reshape(x.shape[:3] + (-1,)))
     return out
 
 

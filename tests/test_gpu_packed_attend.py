@@ -382,6 +382,26 @@ def test_drafts_in_workgroups_that_fill_a_compute_unit(B, K, T, H, G, D, page, d
         check(out, cache, q, positions, dtype, window=window, label=label + " %d %s" % (window, max_len))
 
 
+@pytest.mark.parametrize("tiles,way,page", [(tiles, way, page) for tiles, way in ((2, "one pass"), (2, "parts"), (2, "filled"), (2, "waves"), (4, "one pass"), (4, "parts"))
+                                            for page in (32, 16, 8, "far") if (way, page) != ("waves", "far")])         # (far pages of 8 tokens are not taken by waves alone)
+@pytest.mark.parametrize("D", [64, 128])
+def test_many_rows_of_bfloat16_at_once(D, tiles, way, page):
+    """So many rows that a wave takes 32 or 64 of them, in each way in which it does."""
+    gen = np.random.default_rng(D + tiles)
+    far = page == "far"
+    page = 8 if far else page
+    S, T, length = {(2, "one pass"): (129, 1, 90), (2, "parts"): (129, 1, 1900), (2, "filled"): (129, 1, 1060), (2, "waves"): (1024, 1, 60), (4, "one pass"): (128, 4, 320),
+                    (4, "parts"): (128, 4, 1100)}[tiles, way]
+    width = (length + page - 1) // page
+    cache = make_packed(gen, S, width, page, 1, D, extra=1, page_stride=2 ** 32 // (S * width - 2) // 16 * 16 + 16 if far else None)
+    q = _q(gen, (S, T, 32, D), "bf16")
+    last = [length - 1, T - 1, -1, 40] + [int(n) for n in gen.integers(T - 1, length, S - 4)]
+    positions = _positions([[max(n - T + 1 + t, -1) for t in range(T)] for n in last])
+    for window in (0, length - 7):
+        out, _ = sg.specgbv_packed_attend(cache, q, positions, window=window)
+        check(out, cache, q, positions, "bf16", window=window, label=_label(D, tiles, way, page, far, window))
+
+
 @pytest.mark.parametrize("D,page,S", [(64, 32, 2), (128, 8, 2), (256, 32, 2), (64, 24, 2)])
 def test_pages_of_other_sizes_more_than_2_to_the_32_bytes_apart(D, page, S):
     gen = np.random.default_rng(D + page)
