@@ -21,11 +21,11 @@ static int tiles_of(const AttendShape &c, int64_t longest)
     const int rows = c.tokens * (c.heads / c.kv_heads) * c.drafts, tall = rows_tall(c.element_bytes, padded_dim(c.head_dim));
     const int64_t seen = seen_of(c, longest), own = c.shared ? 600 : 0, units = compute_units();
     int best = 1;
-    int64_t least = INT64_MAX;
+    double least = INFINITY;
     for (int tiles = 1; tiles <= tall; tiles *= 2) {
         const int64_t blocks = (rows + 16 * tiles - 1) / (16 * tiles), groups = c.sequences / c.drafts * static_cast<int64_t>(c.kv_heads) * blocks;
         const int64_t start = tiles == 1 ? 450 : (tiles == 2 ? 900 : 1900), tenths = tiles == 1 ? 10 : (tiles == 2 ? 16 : (c.shared || blocks <= 2 ? 28 : 33));
-        const int64_t cost = ((groups + units - 1) / units * units + groups) * (10 * (start + own) + tenths * seen);
+        const double cost = static_cast<double>((groups + units - 1) / units * units + groups) * static_cast<double>(10 * (start + own) + tenths * seen);
         if (cost < least) { least = cost; best = tiles; }
         if (blocks == 1) break;                                // (more would be empty)
     }

@@ -173,6 +173,22 @@ def test_more_sequences_than_workgroups_at_once(S, T, H, G, D, length, dtype, wi
     check(out, cache, q, positions, dtype, window=window, label=_label(S, T, H, G, D, length, dtype, window))
 
 
+@pytest.mark.parametrize("B,K,T,H,G,D,width,dtype", [(3, 4, 3, 8, 2, 64, 20, "bf16"), (2, 3, 9, 8, 2, 128, 170, "bf16"), (2, 4, 2, 4, 1, 64, 170, "f32"), (24, 8, 1, 8, 8, 64, 45, "bf16")])
+def test_shared_lengths_that_are_no_whole_pages(B, K, T, H, G, D, width, dtype):
+    """Drafts whose tables are the same: whatever number of tokens is said to be shared, also below 0 and behind what queries see or the table holds, the result is that of their tokens."""
+    import torch
+    gen = np.random.default_rng(B + D)
+    page = 16
+    cache = make_packed(gen, B * K, width, page, G, D, dtype)
+    _share(cache, K, [width] * B)
+    positions = _positions([[int(n) + t for t in range(T)] for n in gen.integers(0, width * page - T, B * K)])
+    q = _q(gen, (B * K, T, H, D), dtype)
+    for said in ([-5, 7, 10 ** 9], [0, width * page, 33], [2 ** 31 - 1, -2 ** 31, width * page - 1]):
+        shared = torch.tensor((said * B)[:B], dtype=torch.int32, device="cuda")
+        out, _ = sg.specgbv_packed_attend(cache, q, positions, shared_len=shared)
+        check(out, cache, q, positions, dtype, label=_label(B, K, T, D, dtype, said))
+
+
 def test_long_sequences_in_parts():
     gen = np.random.default_rng(8)
     for S, T, H, G, D, length, hint in ((1, 1, 8, 2, 128, 20000, None), (2, 3, 4, 1, 64, 9000, 100), (1, 40, 8, 1, 128, 5000, None)):

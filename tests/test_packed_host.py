@@ -244,6 +244,26 @@ def test_what_calls_on_a_packed_cache_look_at():
 
 
 @needs_no_gpu
+def test_a_workspace_serves_every_max_len_of_drawn_shapes():
+    """What is asked for at any max_len is no more than the size that is given for all."""
+    import random
+    rng = random.Random(5)
+    lib = sg.load_library()
+    for _ in range(3000):
+        G, D, T = rng.choice([1, 2, 3, 8]), rng.choice([32, 64, 96, 128, 192, 256]), rng.choice([1, 2, 5, 9, 17, 40, 100, 400])
+        H, K, page = G * rng.choice([1, 2, 4, 7, 32]), rng.choice([1, 1, 2, 8]), rng.choice([8, 16, 64])
+        B, width, dtype = rng.choice([1, 2, 7, 16, 33, 64, 65, 130, 300]), rng.choice([1, 3, 20, 130, 600, 5000]), rng.choice([0, 1])
+        S, prefixes, window = B * K, B if K > 1 else rng.choice([0, B]), rng.choice([0, 0, 1, 90, 1500])
+        cache = _cache(S=S, G=G, D=D, page=page, width=width, ts=width, dtype=dtype, kp=page * G * D // 2, kh=page * D // 2, kt=D // 2, vp=page * G * D // 2, vh=page * D // 2, vt=D // 2,
+                       ksp=G * D // 32 * page, ksh=D // 32 * page, ksb=page, vsp=G * D // 32 * page, vsh=D // 32 * page, vsb=page)
+        rows = dict(T=T, H=H, window=window, prefixes=prefixes, shared=P if prefixes else 0, qs=(T * H * D, H * D, D), os=(T * H * D, H * D, D), ps=T)
+        packed = decoding._ATTEND.pack(P, P, P, rows["shared"], *rows["qs"], *rows["os"], T, T, H, window, prefixes, 0, 0.0)
+        need = lib.specgbv_packed_attend_workspace_bytes(cache, packed)
+        for n in [0] + [rng.randint(1, width * page + 5) for _ in range(12)]:
+            assert _attend(cache, wsb=need, max_len=n, **rows) == 4, (n, need, rows, B, K, G, D, page, width, dtype, sg.specgbv_last_error())         # (no GPU: it comes to the launch)
+
+
+@needs_no_gpu
 @pytest.mark.parametrize("prefixes,drafts", [(1, 1), (4, 8), (70, 1), (70, 2), (300, 1)])
 @pytest.mark.parametrize("window", [0, 700])
 def test_a_workspace_serves_every_max_len(prefixes, drafts, window):
