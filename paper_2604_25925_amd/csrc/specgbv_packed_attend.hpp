@@ -44,10 +44,16 @@ template <int DP> struct Packed {
 };
 constexpr int kTile = 32, kRunKeys = 8;
 
-// Waves per SIMD that the registers of rows, sums and a tile leave room for.
-constexpr int packed_waves(int element_bytes, int DP, int RT)
+// Whether a workgroup's queries stand in LDS and not in registers: where so many rows or operands would leave few waves.  (Waves with rows of their own hold theirs.)  Registers / LDS, us: float32 heads of 256
+// (2 waves a SIMD instead of 1), 64 sequences of 72 rows 75 / 59 at 1024 tokens, 190 / 149 at 4096, 32 of 8 rows 25 / 23 and, at 3000, 39 / 36, one query of 8 sequences 17.0 / 16.8; not so bfloat16 heads of 256 (3
+// instead of 2), 64 of 72 rows 43 / 39 and 109 / 94, but 32 of 8 rows 16.4 / 17.0 and, at 3000, 28.5 / 31.9, one query of 8 sequences 12.6 / 13.3; nor float32 heads of 128 (4 instead of 3), 32 of 85
+// rows 32 / 31 and 84 / 88, 64 of 4 22 / 22 and 71 / 75.
+constexpr bool queries_in_lds(int element_bytes, int DP, int RT) { return RT == 4 || (element_bytes == 4 && DP == 256); }
+
+// Waves per SIMD that the registers of rows, sums and a tile leave room for; alone: of waves with rows of their own.
+constexpr int packed_waves(int element_bytes, int DP, int RT, bool alone = false)
 {
-    if (element_bytes == 4) return DP == 64 ? 4 : (DP == 128 ? 3 : 1);
+    if (element_bytes == 4) return DP == 64 ? 4 : (DP == 128 ? 3 : (alone ? 1 : 2));
     return DP == 256 ? 2 : (RT == 1 ? 4 : RT == 2 && DP == 64 ? 3 : 2);
 }
 
@@ -112,13 +118,13 @@ template <int N> __device__ __forceinline__ void operands(const float (&x)[8], U
 
 // WAVES: of a workgroup that share its rows; 0: each of four by itself.
 template <typename T, int DP, int RT, int WAVES, bool PARTS, int PAGES, typename Off>
-__global__ void __launch_bounds__(WAVES > 0 ? WAVES * 64 : kAttendThreads, (packed_waves(sizeof(T), DP, RT))) k_packed_attend(PackedProblem pk)
+__global__ void __launch_bounds__(WAVES > 0 ? WAVES * 64 : kAttendThreads, (packed_waves(sizeof(T), DP, RT, WAVES == 0))) k_packed_attend(PackedProblem pk)
 {
     constexpr bool SHARED = WAVES > 0, kOwn = PARTS || WAVES > kWavesPerGroup;      // kOwn: drafts may share keys and have keys of their own
     using S = Packed<DP>;
     constexpr int kSteps = S::kSteps, kPieces = S::kPieces, kWords = S::kWords, kVec = S::kVec, kGroups = S::kGroups, kCols = S::kCols,
                   N = sizeof(T) == 2 ? 1 : 3;
-    constexpr bool kQueriesInLds = RT == 4;                   // 64 rows: registers are left for their sums alone
+    constexpr bool kQueriesInLds = WAVES > 0 && queries_in_lds(sizeof(T), DP, RT);
     const AttendProblem &p = pk.a;
     __shared__ F4 sh_acc[SHARED ? WAVES * RT * kGroups * 4 * 64 : 1];
     __shared__ float sh_m[SHARED ? WAVES : 1][RT * 16], sh_l[SHARED ? WAVES : 1][RT * 16];
@@ -159,7 +165,7 @@ __global__ void __launch_bounds__(WAVES > 0 ? WAVES * 64 : kAttendThreads, (pack
     }
 
     // ---- queries
-    static_assert(!kQueriesInLds || (N == 1 && RT <= WAVES), "a wave brings one tile of 16 rows to LDS");
+    static_assert(!kQueriesInLds || RT <= WAVES, "a wave brings one tile of 16 rows to LDS");
     U4 qf[kQueriesInLds ? 1 : RT][kQueriesInLds ? 1 : kSteps][N];
     U4 *q_lds = reinterpret_cast<U4 *>(sh_acc) + lane;
     const T *q = static_cast<const T *>(p.q);
@@ -171,14 +177,14 @@ __global__ void __launch_bounds__(WAVES > 0 ? WAVES * 64 : kAttendThreads, (pack
             const int e = S::entry(i, quad);
             const bool there = e < p.head_dim;
             const T *src = q + q_at[r] + (there ? e : 0);
+            U4 (&mine_q)[N] = qf[kQueriesInLds ? 0 : r][kQueriesInLds ? 0 : i];
             if constexpr (N == 1) {
                 U4 w;
                 if (p.q_wide) w = *reinterpret_cast<const U4 *>(src);
                 else w = U4{src[0] | static_cast<uint32_t>(src[1]) << 16, src[2] | static_cast<uint32_t>(src[3]) << 16,
                             src[4] | static_cast<uint32_t>(src[5]) << 16, src[6] | static_cast<uint32_t>(src[7]) << 16};
                 if (!there) w = U4{0, 0, 0, 0};
-                if constexpr (kQueriesInLds) q_lds[(r * kSteps + i) * 64] = w;
-                else qf[r][i][0] = w;
+                mine_q[0] = w;
             } else {
                 float x[8];
                 if (p.q_wide) {
@@ -190,7 +196,7 @@ __global__ void __launch_bounds__(WAVES > 0 ? WAVES * 64 : kAttendThreads, (pack
                     for (int k = 0; k < 8; ++k) x[k] = src[k];
 #pragma unroll
                 for (int k = 0; k < 8; ++k) if (!there) x[k] = 0.0f;
-                operands<N>(x, qf[r][i]);
+                operands<N>(x, mine_q);
                 // (what is not finite is in the first operand alone, as a whole; the others would make NaN of an infinity)
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
@@ -198,12 +204,15 @@ __global__ void __launch_bounds__(WAVES > 0 ? WAVES * 64 : kAttendThreads, (pack
                     for (int h = 0; h < 2; ++h) {
                         const uint32_t bits = __float_as_uint(x[2 * j + h]), mine = h ? 0xFFFF0000u : 0x0000FFFFu;
                         if ((bits & 0x7F800000u) == 0x7F800000u) {
-                            uint32_t *o0 = &qf[r][i][0].x + j, *o1 = &qf[r][i][1].x + j, *o2 = &qf[r][i][2].x + j;
+                            uint32_t *o0 = &mine_q[0].x + j, *o1 = &mine_q[1].x + j, *o2 = &mine_q[2].x + j;
                             if (bits & 0x007FFFFFu) *o0 |= 0x00400040u & mine;
                             *o1 &= ~mine; *o2 &= ~mine;
                         }
                     }
             }
+            if constexpr (kQueriesInLds)
+#pragma unroll
+                for (int n = 0; n < N; ++n) q_lds[((r * kSteps + i) * N + n) * 64] = mine_q[n];
         }
     }
     if constexpr (kQueriesInLds) __syncthreads();
@@ -406,7 +415,7 @@ __global__ void __launch_bounds__(WAVES > 0 ? WAVES * 64 : kAttendThreads, (pack
                 U4 b[N];
 #pragma unroll
                 for (int n = 0; n < N; ++n) {
-                    if constexpr (kQueriesInLds) b[n] = q_lds[again + (r * kSteps + i) * 64];
+                    if constexpr (kQueriesInLds) b[n] = q_lds[again + ((r * kSteps + i) * N + n) * 64];
                     else b[n] = qf[r][i][n];
                 }
 #pragma unroll

@@ -353,7 +353,8 @@ def test_rows_pages_and_ways(dtype, D, T, way, page):
 
 
 @pytest.mark.parametrize("page", [32, 16, 8, "far"])
-@pytest.mark.parametrize("dtype,D,T", [("bf16", 64, 5), ("bf16", 64, 17), ("bf16", 128, 5), ("bf16", 128, 17), ("bf16", 256, 5), ("f32", 64, 5), ("f32", 64, 17), ("f32", 128, 5)])
+@pytest.mark.parametrize("dtype,D,T", [("bf16", 64, 5), ("bf16", 64, 17), ("bf16", 128, 5), ("bf16", 128, 17), ("bf16", 256, 5), ("f32", 64, 5), ("f32", 64, 17), ("f32", 128, 5),
+                                       ("f32", 256, 5)])
 def test_workgroups_that_fill_a_compute_unit(dtype, D, T, page):
     """About as many rows of workgroups as compute units, over lengths that parts would be made of; sequences with little or nothing among them."""
     gen = np.random.default_rng(D + T + 1)
