@@ -60,7 +60,9 @@ __device__ __forceinline__ Share share_of(const AttendProblem &p, int index, int
         if (p.window > 0) length = min(length, min(p.window, held) + p.tokens);
         length = max(length + p.own_keys, 1);
     }
-    const double all = wave_sum(static_cast<double>(length));
+    // (in two halves, as whole numbers: exact, and by moves between lanes where a sum of float64 goes through LDS)
+    const uint32_t low = __builtin_amdgcn_readlane(wave_inclusive_count(length & 0xFFFF), 63), high = __builtin_amdgcn_readlane(wave_inclusive_count(length >> 16), 63);
+    const double all = high * 65536.0 + low;
     int part = static_cast<int>(all / p.most_parts) / p.grain * p.grain + p.grain;            // at most most_parts + units parts
     part = max(part, p.chunk_keys);
     uint32_t n = 0, run = 0;

@@ -194,7 +194,7 @@ struct AttendProblem {
 };
 struct AttendPlan {
     int drafts, shared;                          // of a unit; whether its drafts' shared keys are read once
-    int few, lone;                               // lone: each wave by itself; few: the waves of a workgroup share its rows, else they have rows of their own
+    int few, lone;                               // lone: each wave by itself; few: the waves of a workgroup share its rows (over 4 bits: so many of them), else they have rows of their own
     int units, all_parts, balanced, most_parts, own_keys, grain, chunks, chunk_keys, block_rows, row_blocks;
     size_t places_bytes, ml_bytes, bytes;        // bytes: 0 where nothing is to be joined
 };
