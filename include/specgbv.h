@@ -531,9 +531,9 @@ typedef struct {
 /*
  * specgbv_packed_append: as specgbv_cache_append, with keys and values stored in 4 bits.  Of a block of 32 entries y, with A = max |y|, the power is the
  * least 2^e with A <= 7 * 2^e, e in [-120, 125], and an entry becomes the nearest of the values above times 2^e, of two as near the one of even code,
- * +-6 * 2^e beyond 5 * 2^e; a block that holds an entry that is not finite is marked by the byte 255.  Keys are normalised, rotated and
- * rounded in float64, so a code differs from the definition's only where the entry lies within 2^-50 of itself of a border; queries as in
- * specgbv_cache_append.
+ * +-6 * 2^e beyond 5 * 2^e; a block that holds an entry that is not finite is marked by the byte 255.  Keys are normalised, rotated by pos * inv_freq (the product with all its bits) and
+ * rounded in float64, so a code, or a block's power, differs from the definition's only where an entry lies next to a border: within 2^-50 of |y_a| + |y_b| for a pair that turns, and 2^-49
+ * more where there is a norm, whatever the position; queries as in specgbv_cache_append.
  */
 specgbv_status specgbv_packed_append(const specgbv_packed_cache *cache, const specgbv_append_args *args, void *hip_stream);
 

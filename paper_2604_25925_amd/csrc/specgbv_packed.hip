@@ -6,9 +6,10 @@
 // half step of 1 that entries between 4 and 6 are off by; a power more for all the others would cost each of them a bit.)  A block that holds
 // what is not finite has the byte 255, and all of it is no number.
 //
-// Keys are normalised and rotated in float64, and what decides the code is kept of it: a float32 cut off behind its last bit, with that bit set
+// Keys are normalised and rotated in float64, and what decides the code is kept of it: 20 bits of its mantissa, as a float32 with a last bit that is set
 // where anything was cut (no border lies there, so the conversion, which rounds once, decides as it would for the float64).  So a code differs from the
-// definition's only where the float64 lies within its own error of a border, 2^-50 of the entry instead of 2^-20.
+// definition's only where the entry lies within the float64's own error of a border: 2^-50 (|a| + |b|) for a pair (a, b) that turns, whatever the position, since the product
+// of position and frequency and 1 / (2 pi) have tails, and 2^-49 more of it for a norm (a sum of D squares, a root, a quotient and two products).
 //
 // A lane has 8 adjacent entries, which are one word of the cache, and four lanes a block; the entry that another one turns with is read a second
 // time (from the cache) instead of exchanged.  Every entry is read from memory once.
@@ -95,6 +96,17 @@ template <typename T, bool WIDE> __device__ __forceinline__ void load_partners(c
 __device__ __forceinline__ int pair_of(const PackedAppendProblem &p, int e) { return p.interleaved ? e >> 1 : (e < p.pairs ? e : e - p.pairs); }
 __device__ __forceinline__ bool first_of_pair(const PackedAppendProblem &p, int e) { return p.interleaved ? e % 2 == 0 : e < p.pairs; }
 
+// pos * f in turns, without the whole ones.  Both products and 1 / (2 pi) have tails: half a step of a product alone is up to 2^-23 of an angle at the last positions; what is left, half a turn at most, is
+// off by half a step.
+__device__ __forceinline__ double turns_left(double pos, double f)
+{
+#pragma clang fp contract(off)                                         // (a product taken into the subtraction would count its tail twice)
+    constexpr double kTurn = 0.15915494309189533577, kTurnTail = -9.839338337591243e-18;      // 1 / (2 pi) is their sum
+    const double angle = pos * f, angle_tail = fma(pos, f, -angle), turns = angle * kTurn;
+    const double tail = fma(angle, kTurn, -turns) + fma(angle, kTurnTail, angle_tail * kTurn);
+    return (turns - rint(turns)) + tail;
+}
+
 // A lane's entries x of a key's head, normalised and rotated in float64; b: those they turn with (0 where they do not turn).
 template <typename T, bool WIDE>
 __device__ __forceinline__ void turned(const PackedAppendProblem &p, const Entries<T> &x, const Entries<T> &b, const double2 *turn, int e0, bool there, int lanes, double (&y)[kLane])
@@ -135,7 +147,7 @@ __device__ __forceinline__ void turned(const PackedAppendProblem &p, const Entri
         }
 }
 
-// A float64's bits as those of a float32 that lies on the same side of every border between codes: cut off, with the last bit set where anything was cut.
+// A float64's bits as those of a float32 that lies on the same side of every border between codes: the first 20 of the mantissa, and the last bit set where any behind the first 20 were.
 // Beyond float32's range it is the largest or a smallest one, whose codes are the same; what is not finite is looked at elsewhere.
 __device__ __forceinline__ uint32_t decisive(double x)
 {
@@ -238,10 +250,8 @@ __global__ void __launch_bounds__(kThreads, WIDE ? (sizeof(T) == 2 ? 5 : 4) : 3)
     // ---- what q and k turn by
     if (tk.pos >= 0)
         for (int i = lane; i < p.pairs; i += 64) {
-            // a turn in float64: whole turns are taken off before the sine and cosine
-            const double turns = static_cast<double>(tk.pos) * p.inv_freq[i] * 0.15915494309189533577;
             double sn, cs;
-            sincospi(2.0 * (turns - rint(turns)), &sn, &cs);
+            sincospi(2.0 * turns_left(tk.pos, p.inv_freq[i]), &sn, &cs);
             sh_turn[wave][i] = make_double2(cs, sn);
         }
     __builtin_amdgcn_wave_barrier();                                   // (a wave's accesses to LDS are done in their order)
