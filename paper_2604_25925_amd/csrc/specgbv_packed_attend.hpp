@@ -43,6 +43,7 @@ template <int DP> struct Packed {
     __device__ static constexpr int block(int n, int quad) { return DP == 64 ? quad >> 1 : quad + 4 * n; }
 };
 constexpr int kTile = 32, kRunKeys = 8;
+constexpr float kVast = 1048576.0f;           // references beyond it: c <q, k> is rounded as the reference was, before the difference
 
 // Whether a workgroup's queries stand in LDS and not in registers: where so many rows or operands would leave few waves.  (Waves with rows of their own hold theirs.)  Registers / LDS, us: float32 heads of 256
 // (2 waves a SIMD instead of 1), 64 sequences of 72 rows 75 / 59 at 1024 tokens, 190 / 149 at 4096, 32 of 8 rows 25 / 23 and, at 3000, 39 / 36, one query of 8 sequences 17.0 / 16.8; not so bfloat16 heads of 256 (3
@@ -260,7 +261,7 @@ __global__ void __launch_bounds__(WAVES > 0 ? WAVES * 64 : kAttendThreads, (pack
     const int own_to = !kOwn || !p.shared_len ? 0 : draft1;
     const int own_from = draft0 + WAVES * part + wave, own_step = WAVES * share.parts;
     bool any = draft0 + WAVES * part < own_to;        // something may have been summed (the same for waves that share their rows)
-    bool vast = false;                                        // a row of this wave has a reference beyond 2^20
+    bool vast = false;                                        // a row of this wave has, or had, a reference beyond kVast
 #pragma unroll 1
     for (int seg = -1; seg < own_to; seg = seg < 0 ? own_from : seg + own_step) {
     const bool own = seg >= 0;                                // -1: what the unit's sequences share
@@ -463,7 +464,7 @@ __global__ void __launch_bounds__(WAVES > 0 ? WAVES * 64 : kAttendThreads, (pack
                 const float most = row_largest(top[r]);
                 const float now = most > ref[r] + kRaise ? most : ref[r];
                 const float f = now == ref[r] ? 1.0f : exp2_of(ref[r] - now);        // (-inf to -inf: nothing summed yet)
-                vast = vast || __any(fabsf(now) > 1048576.0f && now != -INFINITY);
+                vast = vast || __any(fabsf(now) > kVast && now != -INFINITY);
                 ref[r] = now;
                 sum[r] *= f;
 #pragma unroll
@@ -474,11 +475,12 @@ __global__ void __launch_bounds__(WAVES > 0 ? WAVES * 64 : kAttendThreads, (pack
 #pragma unroll
             for (int r = 0; r < RT; ++r) {
                 const float m = ref[r] == -INFINITY ? 0.0f : ref[r];
+                const bool mine = fabsf(m) > kVast;            // (a row at a time: what the others get is what they get without it)
 #pragma unroll
                 for (int k = 0; k < kRunKeys; ++k) {
                     float x = s[r][k / 4][k % 4] * p.c;
                     asm volatile("" : "+v"(x));                // (rounded by itself)
-                    s[r][k / 4][k % 4] = exp2_of(x - m);
+                    s[r][k / 4][k % 4] = exp2_of(mine ? x - m : fmaf(s[r][k / 4][k % 4], p.c, -m));
                 }
             }
         } else {
