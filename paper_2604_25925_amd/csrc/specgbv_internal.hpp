@@ -233,8 +233,8 @@ struct PackedAppendProblem {
     const double *inv_freq;
     PageMap map;
     Divider by_tokens, by_slices;  // tokens of a sequence; waves of a token (set by the launch)
-    int64_t q_stride[3], k_stride[3], v_stride[3], q_out_stride[3];
-    int64_t k_cache_stride[3], v_cache_stride[3], k_scale_stride[3], v_scale_stride[3];      // page, head, slot; of the scales page, head, block
+    int64_t q_stride[2], k_stride[2], v_stride[2], q_out_stride[2];                          // sequence, token
+    int64_t k_cache_stride[2], v_cache_stride[2], k_scale_page, v_scale_page;                // page, slot
     int64_t positions_stride;
     int32_t q_head, k_head, v_head, q_out_head, k_cache_head, v_cache_head, k_scale_head, v_scale_head, k_scale_block, v_scale_block;      // strides of heads and blocks
     double eps;
@@ -251,7 +251,7 @@ struct PackedReadProblem {
     const int32_t *positions;
     PageMap map;
     Divider by_tokens, by_slices;
-    int64_t k_cache_stride[3], v_cache_stride[3], k_scale_stride[3], v_scale_stride[3], k_stride[3], v_stride[3], positions_stride;
+    int64_t k_cache_stride[2], v_cache_stride[2], k_scale_page, v_scale_page, k_stride[2], v_stride[2], positions_stride;
     int32_t k_head, v_head, k_cache_head, v_cache_head, k_scale_head, v_scale_head, k_scale_block, v_scale_block;
     int tokens_all, kv_heads, head_dim;
     int lane_bits, k_passes, slice;    // set by launch_packed_read

@@ -231,7 +231,7 @@ __global__ void __launch_bounds__(kThreads, WIDE ? (sizeof(T) == 2 ? 5 : 4) : 3)
     // ---- values: as they are
     if (at.page >= 0) {
         const T *base = static_cast<const T *>(p.v) + (tk.s * p.v_stride[0] + tk.t * p.v_stride[1]);
-        uint8_t *data = p.v_cache + (page * p.v_cache_stride[0] + slot * p.v_cache_stride[2]), *scale = p.v_scale + (page * p.v_scale_stride[0] + slot);
+        uint8_t *data = p.v_cache + (page * p.v_cache_stride[0] + slot * p.v_cache_stride[1]), *scale = p.v_scale + (page * p.v_scale_page + slot);
 #pragma unroll 2
         for (int pass = max(first, v_pass); pass < last; ++pass) {
             const int hd = (pass - v_pass) * heads + head;
@@ -258,7 +258,7 @@ __global__ void __launch_bounds__(kThreads, WIDE ? (sizeof(T) == 2 ? 5 : 4) : 3)
 
     if (at.page >= 0) {
         const T *base = static_cast<const T *>(p.k) + (tk.s * p.k_stride[0] + tk.t * p.k_stride[1]);
-        uint8_t *data = p.k_cache + (page * p.k_cache_stride[0] + slot * p.k_cache_stride[2]), *scale = p.k_scale + (page * p.k_scale_stride[0] + slot);
+        uint8_t *data = p.k_cache + (page * p.k_cache_stride[0] + slot * p.k_cache_stride[1]), *scale = p.k_scale + (page * p.k_scale_page + slot);
 #pragma unroll 1
         for (int pass = max(first, k_pass); pass < min(last, v_pass); ++pass) {
             const int hd = (pass - k_pass) * heads + head;
@@ -336,8 +336,8 @@ __global__ void __launch_bounds__(kThreads) k_packed_read(PackedReadProblem p)
     const int lanes = 1 << p.lane_bits, u = lane & (lanes - 1), e0 = u * kLane, heads = 64 >> p.lane_bits;
     if (e0 >= p.head_dim) return;
     const int64_t page = at.page, slot = at.slot;
-    const uint8_t *data[2] = {p.k_cache + (page * p.k_cache_stride[0] + slot * p.k_cache_stride[2]), p.v_cache + (page * p.v_cache_stride[0] + slot * p.v_cache_stride[2])};
-    const uint8_t *scale[2] = {p.k_scale + (page * p.k_scale_stride[0] + slot), p.v_scale + (page * p.v_scale_stride[0] + slot)};
+    const uint8_t *data[2] = {p.k_cache + (page * p.k_cache_stride[0] + slot * p.k_cache_stride[1]), p.v_cache + (page * p.v_cache_stride[0] + slot * p.v_cache_stride[1])};
+    const uint8_t *scale[2] = {p.k_scale + (page * p.k_scale_page + slot), p.v_scale + (page * p.v_scale_page + slot)};
     T *out[2] = {static_cast<T *>(p.k) + (tk.s * p.k_stride[0] + tk.t * p.k_stride[1]), static_cast<T *>(p.v) + (tk.s * p.v_stride[0] + tk.t * p.v_stride[1])};
 #pragma unroll 4
     for (int pass = first; pass < last; ++pass) {

@@ -84,36 +84,6 @@ static int allowed_width(int width, const void *p, const int64_t *stride, int co
     return width;
 }
 
-// The launch's arguments, from a cache and a call's arguments that have passed their checks; `width`: entries of a vector.
-static AppendProblem append_problem(const specgbv_paged_cache &c, const specgbv_append_args &a, int &width)
-{
-    const size_t esz = element_bytes(c.dtype);
-    AppendProblem p{};
-    p.q = a.q; p.k = a.k; p.v = a.v; p.q_out = a.q_out; p.k_cache = c.k; p.v_cache = c.v;
-    p.q_weight = a.q_weight; p.k_weight = a.k_weight; p.positions = a.positions; p.inv_freq = a.inv_freq;
-    p.map = page_map(c);
-    p.tokens_all = c.sequences * a.tokens;
-    p.by_tokens = Divider::of(a.tokens);
-    p.by_heads = Divider::of(a.heads + 2 * c.kv_heads);
-    width = static_cast<int>(16 / esz);
-    while (a.pairs % width || c.head_dim % (2 * width)) width >>= 1;
-    width = allowed_width(width, a.q, a.q_stride, 3, esz);
-    width = allowed_width(width, a.k, a.k_stride, 3, esz);
-    width = allowed_width(width, a.v, a.v_stride, 3, esz);
-    width = allowed_width(width, a.q_out, a.q_out_stride, 3, esz);
-    width = allowed_width(width, a.q_weight, nullptr, 0, esz);
-    width = allowed_width(width, a.k_weight, nullptr, 0, esz);
-    for (int i = 0; i < 3; ++i) {
-        p.q_stride[i] = a.q_stride[i]; p.k_stride[i] = a.k_stride[i]; p.v_stride[i] = a.v_stride[i]; p.q_out_stride[i] = a.q_out_stride[i];
-    }
-    p.k_cache_stride[0] = c.k_page_stride; p.k_cache_stride[1] = c.k_head_stride; p.k_cache_stride[2] = c.k_token_stride;
-    p.v_cache_stride[0] = c.v_page_stride; p.v_cache_stride[1] = c.v_head_stride; p.v_cache_stride[2] = c.v_token_stride;
-    p.positions_stride = a.positions_stride;
-    p.eps = static_cast<float>(a.eps); p.inv_dim = 1.0f / c.head_dim;
-    p.heads = a.heads; p.kv_heads = c.kv_heads; p.head_dim = c.head_dim; p.pairs = a.pairs; p.interleaved = a.interleaved != 0;
-    return p;
-}
-
 }  // namespace specgbv
 
 using namespace specgbv;
@@ -129,8 +99,30 @@ specgbv_status specgbv_cache_append(const specgbv_paged_cache *cache, const spec
     const specgbv_append_args &a = *args;
     st = check_append(c, a);
     if (st != SPECGBV_OK || c.sequences == 0 || a.tokens == 0) return st;
-    int width;
-    const AppendProblem p = append_problem(c, a, width);
+    const size_t esz = element_bytes(c.dtype);
+    AppendProblem p{};
+    p.q = a.q; p.k = a.k; p.v = a.v; p.q_out = a.q_out; p.k_cache = c.k; p.v_cache = c.v;
+    p.q_weight = a.q_weight; p.k_weight = a.k_weight; p.positions = a.positions; p.inv_freq = a.inv_freq;
+    p.map = page_map(c);
+    p.tokens_all = c.sequences * a.tokens;
+    p.by_tokens = Divider::of(a.tokens);
+    p.by_heads = Divider::of(a.heads + 2 * c.kv_heads);
+    int width = static_cast<int>(16 / esz);                   // entries of a vector
+    while (a.pairs % width || c.head_dim % (2 * width)) width >>= 1;
+    width = allowed_width(width, a.q, a.q_stride, 3, esz);
+    width = allowed_width(width, a.k, a.k_stride, 3, esz);
+    width = allowed_width(width, a.v, a.v_stride, 3, esz);
+    width = allowed_width(width, a.q_out, a.q_out_stride, 3, esz);
+    width = allowed_width(width, a.q_weight, nullptr, 0, esz);
+    width = allowed_width(width, a.k_weight, nullptr, 0, esz);
+    for (int i = 0; i < 3; ++i) {
+        p.q_stride[i] = a.q_stride[i]; p.k_stride[i] = a.k_stride[i]; p.v_stride[i] = a.v_stride[i]; p.q_out_stride[i] = a.q_out_stride[i];
+    }
+    p.k_cache_stride[0] = c.k_page_stride; p.k_cache_stride[1] = c.k_head_stride; p.k_cache_stride[2] = c.k_token_stride;
+    p.v_cache_stride[0] = c.v_page_stride; p.v_cache_stride[1] = c.v_head_stride; p.v_cache_stride[2] = c.v_token_stride;
+    p.positions_stride = a.positions_stride;
+    p.eps = static_cast<float>(a.eps); p.inv_dim = 1.0f / c.head_dim;
+    p.heads = a.heads; p.kv_heads = c.kv_heads; p.head_dim = c.head_dim; p.pairs = a.pairs; p.interleaved = a.interleaved != 0;
     const hipError_t e = launch_append(p, c.dtype == SPECGBV_BF16 ? 1 : 0, width, static_cast<hipStream_t>(hip_stream));
     if (e == hipErrorInvalidConfiguration) return fail(SPECGBV_EUNSUPPORTED, "too many tokens for one launch (%d)", p.tokens_all);
     if (e != hipSuccess) return fail(SPECGBV_EHIP, "append kernel launch: %s", hipGetErrorString(e));
@@ -327,10 +319,8 @@ static specgbv_status check_packed(const specgbv_packed_cache *c, bool pointers)
 
 template <typename P> static void set_packed_strides(P &p, const specgbv_packed_cache &c)
 {
-    p.k_cache_stride[0] = c.k_page_stride; p.k_cache_stride[1] = c.k_head_stride; p.k_cache_stride[2] = c.k_token_stride;
-    p.v_cache_stride[0] = c.v_page_stride; p.v_cache_stride[1] = c.v_head_stride; p.v_cache_stride[2] = c.v_token_stride;
-    p.k_scale_stride[0] = c.k_scale_page_stride; p.k_scale_stride[1] = c.k_scale_head_stride; p.k_scale_stride[2] = c.k_scale_block_stride;
-    p.v_scale_stride[0] = c.v_scale_page_stride; p.v_scale_stride[1] = c.v_scale_head_stride; p.v_scale_stride[2] = c.v_scale_block_stride;
+    p.k_cache_stride[0] = c.k_page_stride; p.k_cache_stride[1] = c.k_token_stride; p.v_cache_stride[0] = c.v_page_stride; p.v_cache_stride[1] = c.v_token_stride;
+    p.k_scale_page = c.k_scale_page_stride; p.v_scale_page = c.v_scale_page_stride;
     p.k_cache_head = static_cast<int32_t>(c.k_head_stride); p.v_cache_head = static_cast<int32_t>(c.v_head_stride);
     p.k_scale_head = static_cast<int32_t>(c.k_scale_head_stride); p.v_scale_head = static_cast<int32_t>(c.v_scale_head_stride);
     p.k_scale_block = static_cast<int32_t>(c.k_scale_block_stride); p.v_scale_block = static_cast<int32_t>(c.v_scale_block_stride);
@@ -380,7 +370,7 @@ specgbv_status specgbv_packed_append(const specgbv_packed_cache *cache, const sp
     p.map = page_map(c);
     p.tokens_all = c.sequences * a.tokens;
     p.by_tokens = Divider::of(a.tokens);
-    for (int i = 0; i < 3; ++i) {
+    for (int i = 0; i < 2; ++i) {
         p.q_stride[i] = a.q_stride[i]; p.k_stride[i] = a.k_stride[i]; p.v_stride[i] = a.v_stride[i]; p.q_out_stride[i] = a.q_out_stride[i];
     }
     set_packed_strides(p, *cache);
@@ -422,7 +412,7 @@ specgbv_status specgbv_packed_read(const specgbv_packed_cache *cache, const spec
     p.tokens_all = c.sequences * a.tokens;
     p.by_tokens = Divider::of(a.tokens);
     set_packed_strides(p, *cache);
-    for (int i = 0; i < 3; ++i) { p.k_stride[i] = a.k_stride[i]; p.v_stride[i] = a.v_stride[i]; }
+    for (int i = 0; i < 2; ++i) { p.k_stride[i] = a.k_stride[i]; p.v_stride[i] = a.v_stride[i]; }
     p.k_head = static_cast<int32_t>(a.k_stride[2]); p.v_head = static_cast<int32_t>(a.v_stride[2]);
     p.positions_stride = a.positions_stride;
     p.kv_heads = c.kv_heads; p.head_dim = c.head_dim;
