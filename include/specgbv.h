@@ -589,6 +589,9 @@ typedef struct {
  * Order.  Requests that take no more than they give are all served.  The others are served in their order while pages suffice, counting every page
  * given back in this call; from the first that does not fit on none is.  Pages given back go behind the ring's last, and pages are taken from
  * its head, both by request, in it the chosen draft first and then the others, in a row by entry: the same state gives the same tables.
+ * What a program does next.  The tokens from shared_len[b] to length[b], in the last page that they fill in part, stand in the chosen draft's own page alone: the other drafts' pages there hold what those drafts wrote, or
+ * nothing.  They are appended again for every draft (with the next step's tokens, say) before a query sees them.  A request that is not served has not adopted its chosen draft's pages: the next call is given
+ * the same chosen[b] again, and until it is served the request's drafts stand where they stood.
  * The device only looks at numbers that it can trust: w and h beyond the width, ends beyond the pages are taken into their range.
  * Limits: pages < 2^30, rows times table_width at most 2^30, table_width * page_size at most 2^30.
  */

@@ -211,7 +211,7 @@ __global__ void __launch_bounds__(kAttendThreads, (Shape<T, DP>::waves(RT))) k_a
     const int own_to = !PARTS || !p.shared_len ? 0 : (WK == 4 ? p.drafts : p.by_in_draft.div(last_row) + 1);    // (drafts with rows in this workgroup)
     const int own_step = WK == 4 ? 4 * share.parts : share.parts;
     bool any = own_from < own_to;                             // something may have been summed
-    bool vast = false;                                        // a row of this wave has a reference beyond 2^20
+    bool vast = false;                                        // a row of this wave has a reference beyond 2^20 (its neighbours' products are then rounded by themselves too)
 #pragma unroll 1
     for (int seg = -1; seg < own_to; seg = seg < 0 ? own_from + (WK == 4 ? wave : 0) : seg + own_step) {
     const bool own = seg >= 0;                                // -1: what the unit's sequences share
@@ -480,7 +480,7 @@ __global__ void __launch_bounds__(kAttendThreads, (Shape<T, DP>::waves(RT))) k_a
             for (int k = 1; k < kRun; ++k) top = fmaxf(top, s[r][k / 4][k % 4]);
             top *= p.c;
             if (__any(top > ref[r] + kRaise)) {
-                // (row by row: what a row gets does not hang on the rows next to it)
+                // (row by row: a reference that one row raises is not the others')
                 top = row_largest(top);
                 const float now = top > ref[r] + kRaise ? top : ref[r];
                 const float f = now == ref[r] ? 1.0f : exp2_of(ref[r] - now);        // (-inf to -inf: nothing summed yet)

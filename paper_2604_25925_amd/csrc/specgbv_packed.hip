@@ -14,10 +14,11 @@
 // A lane has 8 adjacent entries, which are one word of the cache, and four lanes a block; the entry that another one turns with is read a second
 // time (from the cache) instead of exchanged.  Every entry is read from memory once.
 //
-// What bounds it.  5 prompts of up to 4001 tokens (32 heads, 8 kv heads of 128, bfloat16, norms): appending 82 us for 276 MB, 3.4 TB/s: waits, 74 % of the waves' time, for the chain from the
-// position over the table to the inputs, of which the registers (5 waves a SIMD) hold no more at once: inputs one pass ahead spill (87 us), 4 and 6 waves 87 us.  Keys in
-// float32 first, and in float64 only near borders: 22 us more, nearly every wave has one that lies near.  Reading back 18 us for 91 MB, 5 TB/s.  256 tokens of drafts 6.5 and 3.5 us, one
-// token 3.4 and 2.4: the same chain once.
+// What bounds it.  Memory, where tokens are many and their heads fill a wave: 5 prompts of up to 4001 tokens (32 heads, 8 kv heads of 128, bfloat16; 13622 tokens and padding), appending 82 us for 346 MB that
+// have to move (167 read, 179 written: 164 are queries, those of padding too, which become zeros), 367 by the counters (scales are bytes by themselves), 4.5 TB/s or 95 % of what a copy reaches.
+// Inputs one pass ahead spill (87 us), 4 and 6 waves a SIMD 87 us.  Keys in float32 first, and in float64 only near borders: 22 us more, nearly every wave has one that lies near.  Reading back 19 us for
+// 97 MB, 5.2 TB/s.  256 tokens of drafts 6.3 and 3.5 us, one token 3.1 and 2.3: the chain from the position over the table to the inputs, once.  Few small heads leave lanes idle, since a wave has one
+// token: of 2 heads of 32 on 2 kv heads 8 lanes of 64 work in each pass, and each token costs a whole wave's start (30 sequences of 983 tokens, with the reading back, 46 us where the bytes need 4).
 #include "specgbv_internal.hpp"
 
 namespace specgbv {

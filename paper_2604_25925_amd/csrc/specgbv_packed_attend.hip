@@ -106,7 +106,7 @@ static AttendPlan plan_for(const AttendShape &c, int64_t longest, int RT, bool i
 // turn of its own and nothing is to be joined.  Shared / alone, us: 32 prefixes of 8 drafts, a token each (32 heads, 8 kv heads of 128, bfloat16) 22 / 10 at 40 tokens,
 // 23 / 20 at 320, 25 / 24 at 640, 29 / 40 at 1280; 8 of 8, 9 tokens each, 28 / 24 at 40, 45 / 38 at 1280, 55 / 53 at 2560, 69 / 105 at 5120; 16 of 4, 5 tokens each of 10 heads on
 // 2 kv heads (float32) 21 / 13 at 40, 35 / 34 at 2560; 4 of 4, 9 tokens each, heads of 256, 18 / 14 at 40, 28 / 26 at 1280, 32 / 36 at 2560; one of 8, a token each, 8 kv heads of 128,
-// 14.6 / 14.6 at 2560, 18 / 24 at 10240.  Up to which length they are taken by themselves:
+// 14.6 / 14.6 at 2560, 18 / 24 at 10240.  (The shared side has the join of parts in it, also where each prefix is one part, as with 8 of 8 of 9 tokens.)  Up to which length they are taken by themselves:
 // Where their prefixes would be taken whole by workgroups that fill a compute unit, up to half of it: 32 of 8 17.9 / 17.9 at 200, 18 / 25 at 400; 16 of 8 15.8 / 14.6 at 400, 16.8 / 21.2 at 800.
 static int64_t alone_up_to(int sequences, int kv_heads, int head_dim, bool filled)
 {

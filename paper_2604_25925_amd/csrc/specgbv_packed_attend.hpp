@@ -19,9 +19,12 @@
 //
 // What bounds it (heads of 128, 32 on 8 kv heads, bfloat16, unless said).  4 sequences of 131072 tokens: the reads, 570 MB in 104 + 5 us, 5.5 TB/s.  32 prefixes of up to 2048 tokens with 8
 // drafts, a query each: 26 us for 43 MB; the start (positions, rows, queries, table, 3.5 us) and the join in LDS (2 us) stand beside 4 to 8 tiles a wave, each of which
-// waits for its loads.  8 prefixes of up to 4096 tokens, 8 drafts, 9 queries each (32 rows at once): 47 + 8 us for 19 GFLOP, the longest prefix's parts last longest.  With 64 rows at once a tile takes
+// waits for its loads.  8 prefixes of up to 4096 tokens, 8 drafts, 9 queries each (32 rows at once): 47 + 8 us for 19 GFLOP.  Their 72 stretches of rows a prefix fill the card's 512 places, so each prefix is
+// one part: nothing is split, the longest prefix's workgroups end the launch (1.3 waves a SIMD on average where 2 have room, the matrix unit busy for 13 % of the time, vector issue for 38 %), and the
+// form of parts only costs: 9.4 MB of partial sums and the join that copies them, 8 us.  With 64 rows at once a tile takes
 // a wave 4000 cycles, of which 1024 are the matrix unit's: scores 1270, weights 1310, values 1110 follow each other, and two waves a SIMD (the sums are 128 registers) cover little of it.
-// 24 float32 sequences, 5 queries of 14 heads on 2 kv heads of 64, window 1000: 13 us, 2 tiles a wave between the start and the join of 16 waves.  One query of 200 tokens: 5.5 us, all latency.
+// 24 float32 sequences, 5 queries of 14 heads on 2 kv heads of 64, window 1000: 13 us for 2 tiles a wave; what the start, the tiles (three products an operand) and the join of 16 waves take of it was not
+// measured apart.  One query of 200 tokens: 5.5 us, all latency.  Heads of 32 run as heads of 64, half of whose products are of zeros.
 #pragma once
 
 #include "specgbv_attend.hpp"

@@ -345,7 +345,8 @@ def specgbv_pages_advance(pool: PagePool, length, *, chosen=None, room: int = 0,
     """Enqueue the bringing of every request's pages to its length: length [prefixes] int32 tokens stay (0 and below: the request has ended)
     and `room` more may be written by the next step; chosen [prefixes] int32 (as the verification returns it): the draft whose pages the
     prefix's drafts share from here on.  Requests that need more pages than they give back are served in their order while there are enough; one that is
-    not served keeps what it has.  Returns (shared_len [prefixes], tokens in shared pages; served [prefixes]: 1, 0: too few pages, -1:
+    not served keeps what it has, and is given the same `chosen` again.  Tokens behind shared_len that stay are in the chosen draft's own page alone: append them again for
+    every draft.  Returns (shared_len [prefixes], tokens in shared pages; served [prefixes]: 1, 0: too few pages, -1:
     longer than the table; workspace)."""
     lib = load_library()
     shape = (pool.prefixes,)
